@@ -531,6 +531,125 @@ moe_status moe_policy_state(const moe_capacity_policy* p, int32_t* cap,
                             int64_t* launched, int64_t* consumed,
                             int64_t* recompiles);
 
+/* Bytes between quantised rows of n values: n rounded up to whole 16-byte
+ * vectors (0 for n < 0). [host] */
+int moe_quantized_width(int n);
+
+/*
+ * moe_quantize_rows - rows of layer values as 8-bit integers with one scale
+ * each, the form the int8 products below read: tokens, and weights (a row of
+ * a weight matrix is an output channel).
+ *   scale = max_j |x_j| * (1/127), a float32 product with the float32 nearest
+ *           to 1/127
+ *   q_j   = the integer nearest to x_j / scale (ties to even), in [-127, 127]
+ * decided exactly, not from a rounded quotient.  A row whose scale rounds to
+ * 0 gets q = 0; a row with a NaN or an infinity gets scale NaN and q = 0 (so
+ * every product with it is NaN).
+ *   x     [rows,n] layer dtype, rows ldx >= n elements apart (a multiple of 8)
+ *   q     [rows, moe_quantized_width(n)] int8 out, zeros behind the n values
+ *   scale [rows] float32 out
+ * n a multiple of 8, at most 131072.
+ */
+moe_status moe_quantize_rows(void* stream, moe_dtype dt, int64_t rows, int n,
+                             const void* x, int64_t ldx, int8_t* q,
+                             float* scale);
+
+/* Workspace bytes of moe_expert_matmul_i8 for these sizes. [host] */
+size_t moe_expert_matmul_i8_workspace_bytes(int E, int N, int64_t rows_alloc);
+
+/*
+ * moe_expert_matmul_i8 - one product per expert on 8-bit integers with a
+ * scale for each token and each output channel (E = 1: one dense product):
+ *   y[r,n] = float(sum_k xq[r,k] wq[e,n,k]) * xs(r) * w_scale[e,n]
+ * for the rows r in [offsets[e], offsets[e]+rows[e]) of expert e, rows[e]
+ * clamped as moe_expert_ffn_fwd clamps it.  The sums are exact (int32).
+ *   dt      type of y
+ *   K       bytes of a quantised row: a multiple of 16, at most 131072
+ *   xq      [rows_alloc,K] int8, wq [E,N,K] int8, w_scale [E,N] float32
+ *   x_scale float32.  src NULL: [rows_alloc], xs(r) = x_scale[r].  Else src
+ *           [rows_alloc] is moe_dispatch's (t*k + j per row) and x_scale
+ *           [T] holds one scale per token: xs(r) = x_scale[src[r] / k].  So
+ *           tokens are quantised once, before the dispatch copies them.
+ *   y       [rows_alloc,N] out; rows outside every expert's rows are left
+ *           untouched.
+ */
+moe_status moe_expert_matmul_i8(void* stream, moe_dtype dt, int E, int K, int N,
+                                const int32_t* offsets, const int32_t* rows,
+                                int64_t rows_alloc, const int8_t* xq,
+                                const float* x_scale, const int32_t* src, int T,
+                                int k, const int8_t* wq, const float* w_scale,
+                                void* y, void* workspace,
+                                size_t workspace_bytes);
+
+/* Workspace bytes of moe_expert_ffn_fwd_i8 for these sizes. [host] */
+size_t moe_ffn_fwd_i8_workspace_bytes(moe_dtype dt, moe_act act, int E, int d,
+                                      int f, int64_t rows_alloc);
+
+/*
+ * moe_expert_ffn_fwd_i8 - moe_expert_ffn_fwd for serving, on weights and
+ * tokens in 8-bit integers: H (H1, H3) by moe_expert_matmul_i8's formula in
+ * float32, A = act(H) (silu(H1)*H3) rounded to the layer dtype, A quantised
+ * as moe_quantize_rows does, Y from it by the same formula.
+ *   xq, x_scale, src, T, k: as for moe_expert_matmul_i8, K = the quantised
+ *   width of d
+ *   w1q, w3q [E,f,width(d)], w2q [E,d,width(f)] int8, with scales
+ *   w1_scale, w3_scale [E,f], w2_scale [E,d] (w3 NULL unless SwiGLU)
+ *   y_disp  [rows_alloc,d] layer dtype, out
+ */
+moe_status moe_expert_ffn_fwd_i8(void* stream, moe_dtype dt, moe_act act, int E,
+                                 int d, int f, const int32_t* offsets,
+                                 const int32_t* rows, int64_t rows_alloc,
+                                 const int8_t* xq, const float* x_scale,
+                                 const int32_t* src, int T, int k,
+                                 const int8_t* w1q, const float* w1_scale,
+                                 const int8_t* w3q, const float* w3_scale,
+                                 const int8_t* w2q, const float* w2_scale,
+                                 void* y_disp, void* workspace,
+                                 size_t workspace_bytes);
+
+/* Workspace bytes of the dense gated block's calls for these sizes. [host] */
+size_t moe_gated_ffn_fwd_workspace_bytes(moe_dtype dt, int T, int d, int f);
+size_t moe_gated_ffn_bwd_workspace_bytes(moe_dtype dt, int T, int d, int f);
+
+/*
+ * moe_gated_ffn_fwd - the dense gated feed-forward block, an expert that
+ * every token passes (a shared expert beside the routed ones):
+ *   H1 = X w1^T, H3 = X w3^T, A = act(H1) * H3, Y = add + A w2^T
+ * with act MOE_SWIGLU: silu, MOE_GELU_TANH: GELU (tanh form), MOE_RELU: ReLU.
+ * bf16: A and Y are rounded to bf16; with h_save so are H1 and H3, and A is
+ * computed from the rounded values (as the backward reads them).
+ *   x, y    [T,d] layer dtype, rows ldx, ldy elements apart
+ *   w1, w3  [f,d], w2 [d,f] layer dtype
+ *   add     NULL, or [T,d] layer dtype, rows ldadd apart (the routed experts'
+ *           output, say); y itself is allowed
+ *   h_save  NULL for inference, else out [3,T,f]: H1, H3, A for the backward
+ * Row distances are at least d and multiples of 8.
+ */
+moe_status moe_gated_ffn_fwd(void* stream, moe_dtype dt, moe_act act, int T,
+                             int d, int f, const void* x, int64_t ldx,
+                             const void* w1, const void* w3, const void* w2,
+                             const void* add, int64_t ldadd, void* h_save,
+                             void* y, int64_t ldy, void* workspace,
+                             size_t workspace_bytes);
+
+/*
+ * moe_gated_ffn_bwd - its gradients, from the planes the forward saved:
+ *   dA = dY w2, dH1 = dA * H3 * act'(H1), dH3 = dA * act(H1)  (bf16: rounded)
+ *   dX = add + dH1 w1 + dH3 w3, dW1 = dH1^T X, dW3 = dH3^T X, dW2 = dY^T A
+ *   dy, dx  [T,d] layer dtype, rows lddy, lddx elements apart; add NULL, or
+ *           [T,d], rows ldadd apart (dx itself is allowed)
+ *   dw_dt   type of the weight gradients: MOE_F32, or the layer dtype
+ *   dw1, dw3 [f,d], dw2 [d,f] out, overwritten (zeros for T = 0)
+ */
+moe_status moe_gated_ffn_bwd(void* stream, moe_dtype dt, moe_act act, int T,
+                             int d, int f, const void* x, int64_t ldx,
+                             const void* h_save, const void* w1, const void* w3,
+                             const void* w2, const void* dy, int64_t lddy,
+                             const void* add, int64_t ldadd, void* dx,
+                             int64_t lddx, moe_dtype dw_dt, void* dw1,
+                             void* dw3, void* dw2, void* workspace,
+                             size_t workspace_bytes);
+
 /*
  * Kernel timing (instrumentation; not part of the method).  While enabled,
  * every kernel the library launches is bracketed by two HIP events recorded

@@ -10,6 +10,8 @@ using Dynamic Recompilations", MLSys 2022) that it follows.
 from .moe_oracle import *  # noqa: F401,F403
 from .losses import *  # noqa: F401,F403
 from .policies import *  # noqa: F401,F403
-from . import losses as _losses, moe_oracle as _core, policies as _policies
+from .blocks import *  # noqa: F401,F403
+from . import blocks as _blocks, losses as _losses, moe_oracle as _core, policies as _policies
 
-__all__ = list(_core.__all__) + list(_losses.__all__) + list(_policies.__all__)
+__all__ = (list(_core.__all__) + list(_losses.__all__) + list(_policies.__all__) +
+           list(_blocks.__all__))

@@ -90,6 +90,22 @@ SIGNATURES = {
     "moe_policy_begin": (_c_int, [_p, _p, _p, _p, _p, _p]),
     "moe_policy_end": (_c_int, [_p, _p, _p]),
     "moe_policy_state": (_c_int, [_p, _p, _p, _p, _p]),
+    "moe_quantized_width": (_c_int, [_c_int]),
+    "moe_quantize_rows": (_c_int, [_p, _c_int, _c_i64, _c_int, _p, _c_i64, _p, _p]),
+    "moe_expert_matmul_i8_workspace_bytes": (_c_size, [_c_int, _c_int, _c_i64]),
+    "moe_expert_matmul_i8": (_c_int, [_p, _c_int, _c_int, _c_int, _c_int, _p, _p, _c_i64, _p, _p,
+                                      _p, _c_int, _c_int, _p, _p, _p, _p, _c_size]),
+    "moe_ffn_fwd_i8_workspace_bytes": (_c_size, [_c_int, _c_int, _c_int, _c_int, _c_int, _c_i64]),
+    "moe_expert_ffn_fwd_i8": (_c_int, [_p, _c_int, _c_int, _c_int, _c_int, _c_int, _p, _p, _c_i64,
+                                       _p, _p, _p, _c_int, _c_int, _p, _p, _p, _p, _p, _p, _p,
+                                       _p, _c_size]),
+    "moe_gated_ffn_fwd_workspace_bytes": (_c_size, [_c_int, _c_int, _c_int, _c_int]),
+    "moe_gated_ffn_bwd_workspace_bytes": (_c_size, [_c_int, _c_int, _c_int, _c_int]),
+    "moe_gated_ffn_fwd": (_c_int, [_p, _c_int, _c_int, _c_int, _c_int, _c_int, _p, _c_i64, _p, _p,
+                                   _p, _p, _c_i64, _p, _p, _c_i64, _p, _c_size]),
+    "moe_gated_ffn_bwd": (_c_int, [_p, _c_int, _c_int, _c_int, _c_int, _c_int, _p, _c_i64, _p, _p,
+                                   _p, _p, _p, _c_i64, _p, _c_i64, _p, _c_i64, _c_int, _p, _p, _p,
+                                   _p, _c_size]),
     "moe_timing_enable": (_c_int, [_c_int]),
     "moe_set_gemm_tiles": (_c_int, [_c_int]),
     "moe_set_dx_weight_copy": (_c_int, [_c_int]),
@@ -402,6 +418,175 @@ def moe_expert_ffn_bwd(act, offsets, rows, x_disp, h_save, w1, w3, w2, dy_disp, 
                                     _ptr(w3), _ptr(w2), _ptr(dy_disp), _ptr(dx_disp), _ptr(dw1),
                                     _ptr(dw3), _ptr(dw2), _ptr(ws), _nbytes(ws)),
            "moe_expert_ffn_bwd")
+
+
+# ---- 8-bit integer products and the dense gated block ------------------------
+# These check that their tensors share one device and run on that device's
+# current stream, whichever device is current.
+def _device_of(*tensors):
+    """The one device all the call's tensors live on."""
+    ts = [t for t in tensors if t is not None]
+    for t in ts:
+        if not t.is_cuda:
+            raise MoEError("tensor must live in device memory")
+        if t.device != ts[0].device:
+            raise MoEError(f"tensors on {ts[0].device} and {t.device}: one device is needed")
+    return ts[0].device
+
+
+def _rows(t: Optional[torch.Tensor], name, T, d, dtype, optional=False):
+    """Row distance in elements of a [T, d] tensor whose rows are contiguous."""
+    if t is None:
+        if optional:
+            return 0
+        raise MoEError(f"{name} is required")
+    if t.dtype != dtype:
+        raise MoEError(f"{name}: element type {t.dtype}, expected {dtype}")
+    if tuple(t.shape) != (T, d):
+        raise MoEError(f"{name} has shape {tuple(t.shape)}, expected {(T, d)}")
+    if T == 0:
+        return d
+    if t.stride(1) != 1 and d > 1:
+        raise MoEError(f"{name}: the elements of a row must be contiguous")
+    if T == 1:
+        return d
+    if t.stride(0) < d or t.stride(0) % 8:
+        raise MoEError(f"{name}: rows are {t.stride(0)} elements apart, a multiple of 8 not below "
+                       f"{d} is needed")
+    return t.stride(0)
+
+
+def _at(t: Optional[torch.Tensor]):
+    return None if t is None else ctypes.c_void_p(t.data_ptr())
+
+
+def quantized_width(n: int) -> int:
+    """Bytes between quantised rows of n values."""
+    return (n + 15) // 16 * 16
+
+
+def moe_quantize_rows(x, q, scale):
+    """x [rows, n] (rows may be further apart) -> q [rows, quantized_width(n)], scale [rows]."""
+    rows, n = x.shape
+    ld = _rows(x, "x", rows, n, x.dtype)
+    dt = _dt(x)
+    _need(q, rows * quantized_width(n), "q", torch.int8)
+    _need(scale, rows, "scale", _F32)
+    with torch.cuda.device(_device_of(x, q, scale)):
+        _check(lib().moe_quantize_rows(_stream(), dt, rows, n, _at(x), ld, _ptr(q), _ptr(scale)),
+               "moe_quantize_rows")
+
+
+def moe_expert_matmul_i8_workspace_bytes(E, N, rows_alloc) -> int:
+    return lib().moe_expert_matmul_i8_workspace_bytes(E, N, rows_alloc)
+
+
+def _need_scales(x_scale, src, k, R):
+    """Elements of x_scale and src, and the number of tokens, of an int8 product."""
+    if src is None:
+        _need(x_scale, R, "x_scale", _F32)
+        return 0
+    _need(src, R, "src", _I32)
+    _need(x_scale, 1, "x_scale", _F32)
+    if k < 1:
+        raise MoEError("k picks per token are needed with src")
+    return x_scale.numel()
+
+
+def moe_expert_matmul_i8(offsets, rows, xq, x_scale, wq, w_scale, y, ws, src=None, k=1):
+    """xq [R, K] int8, wq [E, N, K] int8 -> y [R, N] over every expert's rows.  src (with k):
+    moe_dispatch's, and x_scale holds one scale per token."""
+    E, N, K = wq.shape
+    R = xq.shape[0]
+    dt = _dt(y)
+    _need(offsets, E + 1, "offsets", _I32)
+    _need(rows, E, "rows", _I32)
+    _need(xq, R * K, "xq", torch.int8)
+    _need(wq, E * N * K, "wq", torch.int8)
+    _need(w_scale, E * N, "w_scale", _F32)
+    _need(y, R * N, "y")
+    T = _need_scales(x_scale, src, k, R)
+    with torch.cuda.device(_device_of(offsets, rows, xq, x_scale, wq, w_scale, y, ws, src)):
+        _check(lib().moe_expert_matmul_i8(_stream(), dt, E, K, N, _ptr(offsets), _ptr(rows), R,
+                                          _ptr(xq), _ptr(x_scale), _ptr(src), T, k, _ptr(wq),
+                                          _ptr(w_scale), _ptr(y), _ptr(ws), _nbytes(ws)),
+               "moe_expert_matmul_i8")
+
+
+def moe_ffn_fwd_i8_workspace_bytes(dt, act, E, d, f, rows_alloc) -> int:
+    return lib().moe_ffn_fwd_i8_workspace_bytes(dt, act, E, d, f, rows_alloc)
+
+
+def moe_expert_ffn_fwd_i8(act, offsets, rows, xq, x_scale, w1q, w1_scale, w3q, w3_scale, w2q,
+                          w2_scale, y_disp, ws, src=None, k=1):
+    """The expert FFN on quantised tokens xq [R, quantized_width(d)] and weights
+    (w1q, w3q [E, f, ..], w2q [E, d, ..])."""
+    (E, f, kd), d, R = w1q.shape, w2q.shape[1], xq.shape[0]
+    dt, sw = _dt(y_disp), act == MOE_SWIGLU
+    if kd != quantized_width(d):
+        raise MoEError(f"w1q: rows of {kd} bytes, expected {quantized_width(d)} for d = {d}")
+    _need(offsets, E + 1, "offsets", _I32)
+    _need(rows, E, "rows", _I32)
+    _need(xq, R * kd, "xq", torch.int8)
+    for name, t, n, dtype, opt in (
+            ("w1q", w1q, E * f * kd, torch.int8, False), ("w1_scale", w1_scale, E * f, _F32, False),
+            ("w3q", w3q, E * f * kd, torch.int8, not sw), ("w3_scale", w3_scale, E * f, _F32, not sw),
+            ("w2q", w2q, E * d * quantized_width(f), torch.int8, False),
+            ("w2_scale", w2_scale, E * d, _F32, False)):
+        _need(t, n, name, dtype, optional=opt)
+    _need(y_disp, R * d, "y_disp")
+    T = _need_scales(x_scale, src, k, R)
+    with torch.cuda.device(_device_of(offsets, rows, xq, x_scale, w1q, w1_scale, w3q, w3_scale, w2q,
+                                      w2_scale, y_disp, ws, src)):
+        _check(lib().moe_expert_ffn_fwd_i8(
+            _stream(), dt, act, E, d, f, _ptr(offsets), _ptr(rows), R, _ptr(xq), _ptr(x_scale),
+            _ptr(src), T, k, _ptr(w1q), _ptr(w1_scale), _ptr(w3q), _ptr(w3_scale), _ptr(w2q),
+            _ptr(w2_scale), _ptr(y_disp), _ptr(ws), _nbytes(ws)), "moe_expert_ffn_fwd_i8")
+
+
+def moe_gated_ffn_fwd_workspace_bytes(dt, T, d, f) -> int:
+    return lib().moe_gated_ffn_fwd_workspace_bytes(dt, T, d, f)
+
+
+def moe_gated_ffn_bwd_workspace_bytes(dt, T, d, f) -> int:
+    return lib().moe_gated_ffn_bwd_workspace_bytes(dt, T, d, f)
+
+
+def moe_gated_ffn_fwd(act, x, w1, w3, w2, y, ws, add=None, h_save=None):
+    """y = add + w2 (act(w1 x) * (w3 x)) for every row of x [T, d]; x, y and add may be rows of
+    wider tensors."""
+    (f, d), T, dtype = w1.shape, x.shape[0], x.dtype
+    dt = _dt(x)
+    ldx, ldy = _rows(x, "x", T, d, dtype), _rows(y, "y", T, d, dtype)
+    ldadd = _rows(add, "add", T, d, dtype, optional=True)
+    for name, w in (("w1", w1), ("w3", w3), ("w2", w2)):
+        _need(w, f * d, name, dtype)
+    if h_save is not None:
+        _need(h_save, 3 * T * f, "h_save", dtype)
+    with torch.cuda.device(_device_of(x, w1, w3, w2, y, ws, add, h_save)):
+        _check(lib().moe_gated_ffn_fwd(_stream(), dt, act, T, d, f, _at(x), ldx, _ptr(w1),
+                                       _ptr(w3), _ptr(w2), _at(add), ldadd, _ptr(h_save), _at(y),
+                                       ldy, _ptr(ws), _nbytes(ws)), "moe_gated_ffn_fwd")
+
+
+def moe_gated_ffn_bwd(act, x, h_save, w1, w3, w2, dy, dx, dw1, dw3, dw2, ws, add=None):
+    """Gradients of moe_gated_ffn_fwd; dw1, dw3, dw2 all float32 or all of the layer's type."""
+    (f, d), T, dtype = w1.shape, x.shape[0], x.dtype
+    dt = _dt(x)
+    ldx, lddy, lddx = (_rows(t, n, T, d, dtype) for t, n in ((x, "x"), (dy, "dy"), (dx, "dx")))
+    ldadd = _rows(add, "add", T, d, dtype, optional=True)
+    _need(h_save, 3 * T * f, "h_save", dtype)
+    for name, w in (("w1", w1), ("w3", w3), ("w2", w2)):
+        _need(w, f * d, name, dtype)
+    if dw1 is None or dw1.dtype not in (dtype, _F32):
+        raise MoEError(f"dw1: a tensor of {dtype} or float32 is needed")
+    for name, w in (("dw1", dw1), ("dw3", dw3), ("dw2", dw2)):
+        _need(w, f * d, name, dw1.dtype)
+    with torch.cuda.device(_device_of(x, h_save, w1, w3, w2, dy, dx, dw1, dw3, dw2, ws, add)):
+        _check(lib().moe_gated_ffn_bwd(_stream(), dt, act, T, d, f, _at(x), ldx, _ptr(h_save),
+                                       _ptr(w1), _ptr(w3), _ptr(w2), _at(dy), lddy, _at(add),
+                                       ldadd, _at(dx), lddx, _dt(dw1), _ptr(dw1), _ptr(dw3),
+                                       _ptr(dw2), _ptr(ws), _nbytes(ws)), "moe_gated_ffn_bwd")
 
 
 def moe_gate_bwd_workspace_bytes(T, d, E) -> int:

@@ -78,13 +78,13 @@ __device__ __forceinline__ float rcp_fast(float x) { return __builtin_amdgcn_rcp
 __device__ __forceinline__ float tanh_fast(float u) {
   return 1.f - 2.f * rcp_fast(1.f + exp_fast(2.f * u));
 }
+constexpr float kGelu1 = -2.f * 0.7978845608028654f * 1.4426950408889634f;
+constexpr float kGelu3 = kGelu1 * 0.044715f;
 __device__ __forceinline__ float act_f(float h, int act) {
   if (act == ACT_RELU) return fmaxf(h, 0.f);
   // GELU, tanh form: 0.5 h (1 + tanh(u)) = h sigmoid(2u) = h / (1 + e^(-2u)),
-  // u = sqrt(2/pi) (h + 0.044715 h^3); -2u log2(e) = h (c1 + c3 h^2)
-  constexpr float c1 = -2.f * 0.7978845608028654f * 1.4426950408889634f;
-  constexpr float c3 = c1 * 0.044715f;
-  return h * rcp_fast(1.f + __builtin_amdgcn_exp2f(h * __builtin_fmaf(c3, h * h, c1)));
+  // u = sqrt(2/pi) (h + 0.044715 h^3); -2u log2(e) = h (kGelu1 + kGelu3 h^2)
+  return h * rcp_fast(1.f + __builtin_amdgcn_exp2f(h * __builtin_fmaf(kGelu3, h * h, kGelu1)));
 }
 __device__ __forceinline__ float act_grad_f(float h, int act) {
   if (act == ACT_RELU) return h > 0.f ? 1.f : 0.f;
@@ -94,6 +94,32 @@ __device__ __forceinline__ float act_grad_f(float h, int act) {
   return 0.5f * (1.f + th) + 0.5f * h * (1.f - th * th) * du;
 }
 __device__ __forceinline__ float sigm(float h) { return rcp_fast(1.f + exp_fast(-h)); }
+// The gate half of the dense block: silu (act SWIGLU), GELU or ReLU, and its
+// part in the backward, dh1 = da h3 act'(h1), dh3 = da act(h1).
+__device__ __forceinline__ float gate_f(float h, int act) {
+  return act == ACT_SWIGLU ? h * sigm(h) : act_f(h, act);
+}
+__device__ __forceinline__ void gate_bwd(float da, float h1, float h3, int act, float& dh1,
+                                         float& dh3) {
+  if (act == ACT_SWIGLU) {
+    const float sg = sigm(h1), t = da * sg, u = t * h3;
+    dh1 = __builtin_fmaf(u, __builtin_fmaf(-h1, sg, h1), u);
+    dh3 = t * h1;
+  } else if (act == ACT_RELU) {
+    dh1 = h1 > 0.f ? da * h3 : 0.f;
+    dh3 = da * fmaxf(h1, 0.f);
+  } else {
+    // GELU = h s with s = sigmoid(2u): s + 2 h s (1 - s) u'.  Past |h| = 10 the
+    // derivative is 1 or 0 to the last bit of a float; there u', whose h^2
+    // grows without bound, is taken at 10
+    const float s = act_f(h1, ACT_GELU), hc = fminf(fmaxf(h1, -10.f), 10.f);
+    const float sg = rcp_fast(1.f + __builtin_amdgcn_exp2f(
+                                        hc * __builtin_fmaf(kGelu3, hc * hc, kGelu1)));
+    const float du = 1.5957691216057308f * __builtin_fmaf(3.f * 0.044715f, hc * hc, 1.f);
+    dh1 = da * h3 * __builtin_fmaf(hc * du, sg * (1.f - sg), sg);
+    dh3 = da * s;
+  }
+}
 
 // ---------------------------------------------------------------------------
 // schedule
@@ -194,8 +220,37 @@ enum Mode {
   M_STORE = 2,       // plain store (Y, dX)
   M_BWD_DA = 3,      // dA = dY W2 -> dH = dA act'(H)
   M_BWD_DA_SWIGLU = 4,
-  M_DW = 5           // var-K weight gradient, fp32
+  M_DW = 5,          // var-K weight gradient, fp32
+  // on int8 operands with a scale per row of A and per row of B (ffn_i8.hip)
+  M_I8_STORE = 6,          // plain store in the layer dtype
+  M_I8_FWD1 = 7,           // A = act(H)
+  M_I8_FWD1_SWIGLU = 8,    // A = silu(H1) H3
+  // the dense gated block (gated.hip); the gate half's activation at run time
+  M_GATED_FWD = 9,         // H1, H3 -> A = act(H1) H3 [, H1 H3 saved]
+  M_GATED_DA = 10,         // dA = dY W2 -> dH1 = dA H3 act'(H1), dH3 = dA act(H1)
+  M_ADD_STORE = 11,        // store with an addend (Y, dX)
+  M_DW_LAYER = 12          // weight gradient in the layer dtype
 };
+constexpr bool is_i8(int mode) { return mode >= M_I8_STORE && mode <= M_I8_FWD1_SWIGLU; }
+// W1 and W3 share a tile
+constexpr bool is_gated(int mode) {
+  return mode == M_FWD1_SWIGLU || mode == M_I8_FWD1_SWIGLU || mode == M_GATED_FWD;
+}
+constexpr bool is_dw(int mode) { return mode == M_DW || mode == M_DW_LAYER; }
+// bytes per operand element of the 16x16 kernels
+constexpr int op_bytes(int mode) { return is_i8(mode) ? 1 : 2; }
+
+// Scales of the rows of int8 tokens: one per row, or, with moe_dispatch's src,
+// one per token (row r holds token src[r] / k of T).
+struct RowScales {
+  const float* scale;
+  const int32_t* src;
+  int T, k;
+};
+__device__ __forceinline__ float row_scale_at(const RowScales& s, int64_t row) {
+  if (!s.src) return s.scale[row];
+  return s.scale[min(max(s.src[row] / s.k, 0), s.T - 1)];
+}
 
 struct GemmParams {
   // operands (bytes).  var-M: A rows of the dispatched buffer, B the
@@ -222,6 +277,11 @@ struct GemmParams {
   const int4* seg;
   int mid_list;       // two-workgroups-per-CU kernels: the tile list
   int dw_h;           // and the units of a weight-gradient tile
+  const char* add; int64_t ldadd;  // M_ADD_STORE: addend (NULL: none), bytes per row
+  // int8 operands: scales of A's rows and of the rows of B and B2 (per expert
+  // s_gstride apart); fp32 outputs
+  RowScales a_scale; const float* b_scale; const float* b2_scale; int64_t s_gstride;
+  int out_f32;
 };
 
 // Tile order, two levels above each XCD's kGroupM x 8 block of tiles.
@@ -328,16 +388,32 @@ __device__ __forceinline__ void mfma16(floatx4& c, const uint4& a, const uint4& 
                : "v"(__builtin_bit_cast(intx4, a)), "v"(__builtin_bit_cast(intx4, b)));
 }
 
+// The same on int8: 64 products of whole numbers per lane pair, four int32
+// sums, which the floatx4 carries as bits (0.f is 0).  A fragment is the same
+// 16 bytes per lane (k = 16 G .. 16 G + 15), so tiles, loads and fragment
+// reads are those of bf16 with twice the k values per 128-byte row.
+__device__ __forceinline__ void mfma16_i8(floatx4& c, const uint4& a, const uint4& b) {
+  asm volatile("v_mfma_i32_16x16x64_i8 %0, %1, %2, %0"
+               : "+a"(c)
+               : "v"(__builtin_bit_cast(intx4, a)), "v"(__builtin_bit_cast(intx4, b)));
+}
+template <int ES>
+__device__ __forceinline__ void mfma_es(floatx4& c, const uint4& a, const uint4& b) {
+  if constexpr (ES == 1) mfma16_i8(c, a, b);
+  else mfma16(c, a, b);
+}
+
 // acc += A_tile * B_tile^T over the whole K extent (see above).  Wave w owns
 // tile rows 128 (w >> 1) .. +127 and columns 128 (w & 1) .. +127 (gated
 // forward: hidden units 64 (w & 1) .. +63 of W1, then the same units of W3).
 // The four stage objects are distinct, and the loop is unrolled by two so
 // every LDS access names its object statically: the compiler can then tell
 // the loads into one stage from the reads of the other.
-template <int ALAY, int BLAY, bool GATED, bool FULL>
+template <int ALAY, int BLAY, bool GATED, bool FULL, int ES>
 __device__ __forceinline__ void mainloop16(const TileOps& op, char* la0, char* lb0, char* la1,
                                            char* lb1, floatx4 (&acc)[8][8], int zt) {
-  constexpr int KSTEP = 64;
+  static_assert(ES == 2 || (ALAY == L_KC && BLAY == L_KC), "int8 operands are K-contiguous");
+  constexpr int KSTEP = kRowBytes / ES;
   const int lane = (static_cast<int>(threadIdx.x) & 63) + zt;
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
   const int wm = wave >> 1, wn = wave & 1;
@@ -405,7 +481,7 @@ __device__ __forceinline__ void mainloop16(const TileOps& op, char* la0, char* l
       off = static_cast<uint32_t>(l3 * ld) + co;
       soff = row0 * ld + s.kt * kRowBytes;
       if (!FULL || !s.kfull) {
-        const bool ok = (FULL || row0 + l3 < o.rows) && (s.kfull || s.kt * kRowBytes + co < K * 2);
+        const bool ok = (FULL || row0 + l3 < o.rows) && (s.kfull || s.kt * kRowBytes + co < K * ES);
         if (!ok) off = kOob;
       }
     } else {
@@ -493,7 +569,7 @@ __device__ __forceinline__ void mainloop16(const TileOps& op, char* la0, char* l
     for (int g = 0; g < 8; ++g) {
       read1(ca, cb, 1, f1a, f1b, g);
 #pragma unroll
-      for (int m = 4 * g; m < 4 * g + 4; ++m) mfma16(acc[m >> 3][m & 7], f0a[m >> 3], f0b[m & 7]);
+      for (int m = 4 * g; m < 4 * g + 4; ++m) mfma_es<ES>(acc[m >> 3][m & 7], f0a[m >> 3], f0b[m & 7]);
       __builtin_amdgcn_sched_barrier(0);
     }
     __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0)
@@ -507,7 +583,7 @@ __device__ __forceinline__ void mainloop16(const TileOps& op, char* la0, char* l
       if (g % 3 != 1) load1(s, ca, cb, g - 8 - (g - 8) / 3);
       read1(ca, cb, 1, f1a, f1b, g);
 #pragma unroll
-      for (int m = 4 * g; m < 4 * g + 4; ++m) mfma16(acc[m >> 3][m & 7], f0a[m >> 3], f0b[m & 7]);
+      for (int m = 4 * g; m < 4 * g + 4; ++m) mfma_es<ES>(acc[m >> 3][m & 7], f0a[m >> 3], f0b[m & 7]);
       __builtin_amdgcn_sched_barrier(0);
     }
     // stage kt + 1 has landed (only the 6 A loads just issued may be pending)
@@ -522,7 +598,7 @@ __device__ __forceinline__ void mainloop16(const TileOps& op, char* la0, char* l
       if (g % 3 != 1 && g < 15) load1(s, ca, cb, 6 + g - (g + 1) / 3);
       read1(na, nb, 0, f0a, f0b, g);
 #pragma unroll
-      for (int m = 4 * g; m < 4 * g + 4; ++m) mfma16(acc[m >> 3][m & 7], f1a[m >> 3], f1b[m & 7]);
+      for (int m = 4 * g; m < 4 * g + 4; ++m) mfma_es<ES>(acc[m >> 3][m & 7], f1a[m >> 3], f1b[m & 7]);
       __builtin_amdgcn_sched_barrier(0);
     }
   };
@@ -574,11 +650,12 @@ __device__ __forceinline__ void mainloop16(const TileOps& op, char* la0, char* l
 constexpr int wait_vm_lgkm0(int vm) { return (vm & 15) | ((vm >> 4) << 14) | 0x70; }
 constexpr int wait_vm(int vm) { return (vm & 15) | ((vm >> 4) << 14) | 0xF70; }
 
-template <int RB, int ALAY, int BLAY, bool GATED>
+template <int RB, int ALAY, int BLAY, bool GATED, int ES>
 __device__ __forceinline__ void mainloop_mid(const TileOps& op, char* la0, char* lb0, char* la1,
                                              char* lb1, floatx4 (&acc)[RB][4], int zt) {
   static_assert(ALAY == L_KC || RB == 4, "K-major A tiles are 128 columns wide");
-  constexpr int KSTEP = 64;
+  static_assert(ES == 2 || (ALAY == L_KC && BLAY == L_KC), "int8 operands are K-contiguous");
+  constexpr int KSTEP = kRowBytes / ES;
   constexpr int KMROW = 256;           // bytes per k-row of a KM tile
   constexpr int NM = 4 * RB;           // MFMAs per k-half: one per accumulator
   static_assert(NM >= 4, "updates of one accumulator are at least 4 MFMAs apart");
@@ -644,7 +721,7 @@ __device__ __forceinline__ void mainloop_mid(const TileOps& op, char* la0, char*
     StepLd s;
     s.kt = kt;
     s.ra = ra_t; s.rb = rb_t; s.rb2 = rb3_t;
-    s.kbad = bad(kt * kRowBytes + co >= K * 2);
+    s.kbad = bad(kt * kRowBytes + co >= K * ES);
     if constexpr (ALAY == L_KM) s.ra = km_rsrc(op.a, kt, false);
     if constexpr (BLAY == L_KM) {
       s.rb = km_rsrc(op.b, kt, false);
@@ -714,7 +791,7 @@ __device__ __forceinline__ void mainloop_mid(const TileOps& op, char* la0, char*
     for (int i = 0; i < RB; ++i) {
       read_a(ca, 1, f1a, i);
 #pragma unroll
-      for (int m = 2 * i; m < 2 * i + 2; ++m) mfma16(acc[m >> 2][m & 3], f0a[m >> 2], f0b[m & 3]);
+      for (int m = 2 * i; m < 2 * i + 2; ++m) mfma_es<ES>(acc[m >> 2][m & 3], f0a[m >> 2], f0b[m & 3]);
       __builtin_amdgcn_sched_barrier(0);
     }
     __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0)
@@ -727,7 +804,7 @@ __device__ __forceinline__ void mainloop_mid(const TileOps& op, char* la0, char*
 #pragma unroll
       for (int j = 4 * q / (2 * RB); j < 4 * (q + 1) / (2 * RB); ++j) read_b(cb, 1, f1b, j);
       const int m = 2 * RB + q;
-      mfma16(acc[m >> 2][m & 3], f0a[m >> 2], f0b[m & 3]);
+      mfma_es<ES>(acc[m >> 2][m & 3], f0a[m >> 2], f0b[m & 3]);
       __builtin_amdgcn_sched_barrier(0);
     }
     // stage kt + 1 has landed (only the RB A loads just issued may be pending)
@@ -742,7 +819,7 @@ __device__ __forceinline__ void mainloop_mid(const TileOps& op, char* la0, char*
         if (r < RB) read_a(na, 0, f0a, r);
         else read_b(nb, 0, f0b, r - RB);
       }
-      mfma16(acc[m >> 2][m & 3], f1a[m >> 2], f1b[m & 3]);
+      mfma_es<ES>(acc[m >> 2][m & 3], f1a[m >> 2], f1b[m & 3]);
       __builtin_amdgcn_sched_barrier(0);
     }
   };
@@ -826,7 +903,13 @@ __device__ __forceinline__ void epilogue16(const GemmParams& p,
     return p.dwB + static_cast<int64_t>(g) * p.dw_gstride +
            static_cast<int64_t>(orow - p.split_row) * p.N + gc;
   };
-  if constexpr (MODE == M_DW) {
+  // M_DW_LAYER, no partial sums: one expert, results in bf16
+  auto dw_dst16 = [&](int orow, int gc) -> uint16_t* {
+    return orow < p.split_row
+               ? reinterpret_cast<uint16_t*>(p.dwA) + static_cast<int64_t>(orow) * p.N + gc
+               : reinterpret_cast<uint16_t*>(p.dwB) + static_cast<int64_t>(orow - p.split_row) * p.N + gc;
+  };
+  if constexpr (is_dw(MODE)) {
     if (empty) {
       // no rows to contract over (a split expert's last segment may be
       // empty): the tile is zero; each lane stores 8 zeros per row pass straight to memory,
@@ -838,6 +921,10 @@ __device__ __forceinline__ void epilogue16(const GemmParams& p,
       for (int r = 0; r < WR; r += RG) {
         const int lm = wr0 + r + el / LR, gc = n0 + wn * WC + (el % LR) * 8;
         if (lm < m_valid && gc < p.N) {
+          if (MODE == M_DW_LAYER && slot < 0) {
+            *reinterpret_cast<uint4*>(dw_dst16(row0 + lm, gc)) = make_uint4(0, 0, 0, 0);
+            continue;
+          }
           float* dst = dw_dst(row0 + lm, gc);
           *reinterpret_cast<float4*>(dst) = zero;
           *reinterpret_cast<float4*>(dst + 4) = zero;
@@ -850,7 +937,7 @@ __device__ __forceinline__ void epilogue16(const GemmParams& p,
   // uniform branch per tile instead of one per element
   auto epilogue = [&](auto act_c) {
   constexpr int ACT = decltype(act_c)::value;
-  if constexpr (MODE == M_FWD1_SWIGLU) {
+  if constexpr (MODE == M_FWD1_SWIGLU || MODE == M_GATED_FWD) {
     // strip columns [0,U): H1, [U,2U): H3 of hidden units n0 + U wn + u, U =
     // WC / 2; LU lanes cover a row's U units, 8 each
     constexpr int U = WC / 2, LU = U / 8, RU = 64 / LU;
@@ -872,10 +959,13 @@ __device__ __forceinline__ void epilogue16(const GemmParams& p,
             h3[e] = strip[r * kP + U + u8 + e];
           }
           const uint4 b1 = pack8(h1), b3 = pack8(h3);
-          unpack8(b1, h1);
-          unpack8(b3, h3);
+          if (MODE == M_FWD1_SWIGLU || p.H1) {
+            unpack8(b1, h1);
+            unpack8(b3, h3);
+          }
 #pragma unroll
-          for (int e = 0; e < 8; ++e) a[e] = h1[e] * sigm(h1[e]) * h3[e];
+          for (int e = 0; e < 8; ++e)
+            a[e] = (ACT == ACT_SWIGLU ? h1[e] * sigm(h1[e]) : act_f(h1[e], ACT)) * h3[e];
           const int64_t grow = row0 + lm;
           if (p.H1) {
             *reinterpret_cast<uint4*>(p.H1 + grow * p.ldh + static_cast<int64_t>(gc) * ES) = b1;
@@ -885,13 +975,13 @@ __device__ __forceinline__ void epilogue16(const GemmParams& p,
         }
       }
     }
-  } else if constexpr (MODE == M_BWD_DA || MODE == M_BWD_DA_SWIGLU) {
+  } else if constexpr (MODE == M_BWD_DA || MODE == M_BWD_DA_SWIGLU || MODE == M_GATED_DA) {
     // dH = dA act'(H): (row block, row group) iterations, each reading 8
     // saved pre-activations (two planes for SwiGLU) per lane, issued kPf
     // iterations ahead of their use into a ring of kPf + 1 registers.  LR
     // lanes cover a row of the wave block, RG rows form a group, GB groups
     // a 16-row block.
-    constexpr bool SW = MODE == M_BWD_DA_SWIGLU;
+    constexpr bool SW = MODE != M_BWD_DA;
     constexpr int LR = WC / 8, RG = 64 / LR, GB = 16 / RG;
     constexpr int kIt = C::RB * GB, kPf = 4, kRing = kPf + 1;
     uint4 q1[kRing], q3[kRing];
@@ -929,6 +1019,10 @@ __device__ __forceinline__ void epilogue16(const GemmParams& p,
           for (int e = 0; e < 8; ++e) {
             // d silu(h1) h3 / dh1 = h3 sg (1 + h1 (1 - sg)), d / dh3 = h1 sg
             const float da = strip[r * kP + c8 + e];
+            if constexpr (ACT != ACT_SWIGLU) {
+              gate_bwd(da, h1[e], h3[e], ACT, g1[e], g3[e]);
+              continue;
+            }
             const float sg = sigm(h1[e]);
             const float t = da * sg, u = t * h3[e];
             g1[e] = __builtin_fmaf(u, __builtin_fmaf(-h1[e], sg, h1[e]), u);
@@ -956,7 +1050,11 @@ __device__ __forceinline__ void epilogue16(const GemmParams& p,
         const int gc = n0 + wn * WC + c8;
         if (lm < m_valid && gc < p.N) {
           const float* sp = strip + r * kP + c8;
-          if constexpr (MODE == M_DW) {
+          if constexpr (is_dw(MODE)) {
+            if (MODE == M_DW_LAYER && slot < 0) {
+              *reinterpret_cast<uint4*>(dw_dst16(row0 + lm, gc)) = pack8(sp);
+              continue;
+            }
             float* dst = dw_dst(row0 + lm, gc);
             *reinterpret_cast<float4*>(dst) = make_float4(sp[0], sp[1], sp[2], sp[3]);
             *reinterpret_cast<float4*>(dst + 4) = make_float4(sp[4], sp[5], sp[6], sp[7]);
@@ -965,6 +1063,14 @@ __device__ __forceinline__ void epilogue16(const GemmParams& p,
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = sp[e];
             const int64_t grow = row0 + lm;
+            if constexpr (MODE == M_ADD_STORE) {
+              if (p.add) {
+                float b[8];
+                unpack8(*reinterpret_cast<const uint4*>(p.add + grow * p.ldadd + static_cast<int64_t>(gc) * ES), b);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] += b[e];
+              }
+            }
             if constexpr (MODE == M_FWD1) {
               if constexpr (ACT == ACT_RELU) {
                 // ReLU commutes with the rounding to bf16 (round(max(h, 0)) =
@@ -993,8 +1099,87 @@ __device__ __forceinline__ void epilogue16(const GemmParams& p,
   if constexpr (MODE == M_FWD1 || MODE == M_BWD_DA) {
     if (p.act == ACT_RELU) epilogue(std::integral_constant<int, ACT_RELU>{});
     else epilogue(std::integral_constant<int, ACT_GELU>{});
+  } else if constexpr (MODE == M_GATED_FWD || MODE == M_GATED_DA) {
+    if (p.act == ACT_RELU) epilogue(std::integral_constant<int, ACT_RELU>{});
+    else if (p.act == ACT_GELU) epilogue(std::integral_constant<int, ACT_GELU>{});
+    else epilogue(std::integral_constant<int, ACT_SWIGLU>{});
   } else {
     epilogue(std::integral_constant<int, ACT_SWIGLU>{});
+  }
+}
+
+// Row scales of a wave's rows, behind the two strips of its operand buffer.
+template <typename C>
+__device__ __forceinline__ float* row_scales(char* buf01, char* buf23, int wave) {
+  static_assert(2 * C::kStripBytes + 2 * C::WR * 4 <= kMidN * kRowBytes || C::WR == 128, "fits");
+  static_assert(2 * C::kStripBytes + 2 * C::WR * 4 <= kTileBytes, "fits");
+  return reinterpret_cast<float*>((wave < 2 ? buf01 : buf23) + 2 * C::kStripBytes) + (wave & 1) * C::WR;
+}
+
+// Epilogue of the int8 products: int32 sums, times the scale of their row of A,
+// times the scale of their row of B, in that order, all in fp32 (an int32 sum
+// is rounded to 24 bits once).  A lane's eight columns are the same for every
+// row, so the B scales are read once per tile; the A scales of the wave's rows
+// go through rs, WR floats of LDS behind the strips, so that their memory
+// latency is paid once.
+template <int MODE, typename C>
+__device__ __forceinline__ void epilogue_i8(const GemmParams& p, const floatx4 (&acc)[C::RB][C::CB],
+                                            float* strip, float* rs, int el, int wm, int wn, int g,
+                                            int row0, int m_valid, int n0) {
+  constexpr int WR = C::WR, WC = C::WC, kP = C::kP;
+  constexpr bool GATED = is_gated(MODE);
+  constexpr int U = GATED ? WC / 2 : WC, LR = U / 8, RG = 64 / LR;
+  const int wr0 = wm * WR, c8 = (el % LR) * 8, gc = n0 + wn * U + c8;
+  for (int r = el; r < WR; r += 64) rs[r] = wr0 + r < m_valid ? row_scale_at(p.a_scale, row0 + wr0 + r) : 0.f;
+  float s1[8], s3[8];
+  if (gc < p.N) {
+    const int64_t o = static_cast<int64_t>(g) * p.s_gstride + gc;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      s1[e] = p.b_scale[o + e];
+      if constexpr (GATED) s3[e] = p.b2_scale[o + e];
+    }
+  }
+  auto run = [&](auto act_c) {
+    constexpr int ACT = decltype(act_c)::value;
+#pragma unroll
+    for (int i = 0; i < C::RB; ++i) {
+      const int c16 = el & 15, G = el >> 4;
+#pragma unroll
+      for (int j = 0; j < C::CB; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          strip[(4 * G + q) * kP + 16 * j + c16] = static_cast<float>(__float_as_int(acc[i][j][q]));
+#pragma unroll
+      for (int it = 0; it < 16 / RG; ++it) {
+        const int r = it * RG + el / LR, lr = 16 * i + r, lm = wr0 + lr;
+        if (lm < m_valid && gc < p.N) {
+          const float* sp = strip + r * kP + c8;
+          const float as = rs[lr];
+          float v[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            v[e] = sp[e] * as * s1[e];
+            if constexpr (GATED) v[e] = v[e] * sigm(v[e]) * (sp[U + e] * as * s3[e]);
+            else if constexpr (MODE == M_I8_FWD1) v[e] = act_f(v[e], ACT);
+          }
+          char* dst = p.C + static_cast<int64_t>(row0 + lm) * p.ldc;
+          if (p.out_f32) {
+            float4* d4 = reinterpret_cast<float4*>(dst + static_cast<int64_t>(gc) * 4);
+            d4[0] = make_float4(v[0], v[1], v[2], v[3]);
+            d4[1] = make_float4(v[4], v[5], v[6], v[7]);
+          } else {
+            *reinterpret_cast<uint4*>(dst + static_cast<int64_t>(gc) * 2) = pack8(v);
+          }
+        }
+      }
+    }
+  };
+  if constexpr (MODE == M_I8_FWD1) {
+    if (p.act == ACT_RELU) run(std::integral_constant<int, ACT_RELU>{});
+    else run(std::integral_constant<int, ACT_GELU>{});
+  } else {
+    run(std::integral_constant<int, ACT_SWIGLU>{});
   }
 }
 
@@ -1006,9 +1191,9 @@ __global__ __launch_bounds__(kThreads16, 1) void ffn_gemm16_kernel(const GemmPar
   __shared__ __attribute__((aligned(16))) char lb1[kTileBytes];
   using C = TileBig;
   constexpr int TM = C::TM, TN = C::TN;
-  constexpr int ES = 2;
-  constexpr bool VARK = MODE == M_DW;
-  constexpr bool GATED = MODE == M_FWD1_SWIGLU;
+  constexpr int ES = op_bytes(MODE);
+  constexpr bool VARK = is_dw(MODE);
+  constexpr bool GATED = is_gated(MODE);
   constexpr int ALAY = a_layout(PASS), BLAY = b_layout(PASS);
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
@@ -1076,14 +1261,18 @@ __global__ __launch_bounds__(kThreads16, 1) void ffn_gemm16_kernel(const GemmPar
     asm volatile("s_mov_b32 %0, 0" : "=s"(zt));
     floatx4 acc[C::RB][C::CB];
     const bool full = op.a.rows >= TM && op.b.rows >= (GATED ? TN / 2 : TN);
-    if (full) mainloop16<ALAY, BLAY, GATED, true>(op, la0, lb0, la1, lb1, acc, zt);
-    else mainloop16<ALAY, BLAY, GATED, false>(op, la0, lb0, la1, lb1, acc, zt);
+    if (full) mainloop16<ALAY, BLAY, GATED, true, ES>(op, la0, lb0, la1, lb1, acc, zt);
+    else mainloop16<ALAY, BLAY, GATED, false, ES>(op, la0, lb0, la1, lb1, acc, zt);
 
     int z;
     asm volatile("s_mov_b32 %0, 0" : "=s"(z));
     float* strip = reinterpret_cast<float*>((wave < 2 ? la0 : lb0) + (wave & 1) * C::kStripBytes + z);
-    epilogue16<MODE, C>(p, acc, strip, lane + z, wm, wn, g, slot, row0, m_valid, n0,
-                        VARK && op.K == 0);
+    if constexpr (is_i8(MODE))
+      epilogue_i8<MODE, C>(p, acc, strip, row_scales<C>(la0, lb0, wave) + z, lane + z, wm, wn, g,
+                           row0, m_valid, n0);
+    else
+      epilogue16<MODE, C>(p, acc, strip, lane + z, wm, wn, g, slot, row0, m_valid, n0,
+                          VARK && op.K == 0);
     __syncthreads();   // strips are free before the next tile's loads
   }
 }
@@ -1116,18 +1305,18 @@ struct MidTile {
 template <int MODE>
 __device__ __forceinline__ int mid_items(const GemmParams& p) {
   const Sched& sc = *p.sched;
-  return (MODE == M_DW ? sc.n_segs * p.mtiles_out : sc.n_mid[p.mid_list]) * p.ntiles;
+  return (is_dw(MODE) ? sc.n_segs * p.mtiles_out : sc.n_mid[p.mid_list]) * p.ntiles;
 }
 
 // Tile L of the launch; ES: bytes per element.
 template <int MODE, int PASS, int ES>
 __device__ __forceinline__ void mid_operands(const GemmParams& p, int L, MidTile& t) {
-  constexpr bool GATED = MODE == M_FWD1_SWIGLU;
+  constexpr bool GATED = is_gated(MODE);
   constexpr int BLAY = b_layout(PASS), TN = kMidN;
   const Sched& sc = *p.sched;
   int mt, nt;
   t.slot = -1;
-  if constexpr (MODE != M_DW) {
+  if constexpr (!is_dw(MODE)) {
     decode_banded(L, sc.n_mid[p.mid_list], p.ntiles, mt, nt);
     const int2 tm = p.mtile[mt];
     const int g = t.g = tm.x & 255;
@@ -1172,13 +1361,14 @@ __device__ __forceinline__ void mid_operands(const GemmParams& p, int L, MidTile
 
 template <int MODE, int PASS>
 __global__ __launch_bounds__(kThreads16, 2) void ffn_gemm16_mid_kernel(const GemmParams p) {
-  constexpr bool VARK = MODE == M_DW;
+  constexpr bool VARK = is_dw(MODE);
+  constexpr int ES = op_bytes(MODE);
   constexpr int kRowsA = (VARK ? kMidDwH : kMidMaxH) * kMidUnit;
   __shared__ __attribute__((aligned(16))) char la0[kRowsA * kRowBytes];
   __shared__ __attribute__((aligned(16))) char lb0[kMidN * kRowBytes];
   __shared__ __attribute__((aligned(16))) char la1[kRowsA * kRowBytes];
   __shared__ __attribute__((aligned(16))) char lb1[kMidN * kRowBytes];
-  constexpr bool GATED = MODE == M_FWD1_SWIGLU;
+  constexpr bool GATED = is_gated(MODE);
   constexpr int ALAY = a_layout(PASS), BLAY = b_layout(PASS);
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
@@ -1188,18 +1378,22 @@ __global__ __launch_bounds__(kThreads16, 2) void ffn_gemm16_mid_kernel(const Gem
     const int L = round_item(round, n_items);
     if (L < 0) break;
     MidTile t;
-    mid_operands<MODE, PASS, 2>(p, L, t);
+    mid_operands<MODE, PASS, ES>(p, L, t);
     auto run = [&](auto hc) {
       constexpr int RB = decltype(hc)::value;
       using C = Tile16<RB, 4>;
       int zt, z;   // opaque zeros: see ffn_gemm16_kernel
       asm volatile("s_mov_b32 %0, 0" : "=s"(zt));
       floatx4 acc[RB][4];
-      mainloop_mid<RB, ALAY, BLAY, GATED>(t.op, la0, lb0, la1, lb1, acc, zt);
+      mainloop_mid<RB, ALAY, BLAY, GATED, ES>(t.op, la0, lb0, la1, lb1, acc, zt);
       asm volatile("s_mov_b32 %0, 0" : "=s"(z));
       float* strip = reinterpret_cast<float*>((wave < 2 ? lb0 : lb1) + (wave & 1) * C::kStripBytes + z);
-      epilogue16<MODE, C>(p, acc, strip, lane + z, wm, wn, t.g, t.slot, t.row0, t.m_valid, t.n0,
-                          VARK && t.op.K == 0);
+      if constexpr (is_i8(MODE))
+        epilogue_i8<MODE, C>(p, acc, strip, row_scales<C>(lb0, lb1, wave) + z, lane + z, wm, wn, t.g,
+                             t.row0, t.m_valid, t.n0);
+      else
+        epilogue16<MODE, C>(p, acc, strip, lane + z, wm, wn, t.g, t.slot, t.row0, t.m_valid, t.n0,
+                            VARK && t.op.K == 0);
     };
     if constexpr (VARK) {
       run(std::integral_constant<int, kMidDwH>{});
@@ -1371,13 +1565,13 @@ __device__ __forceinline__ void mainloop_f32(const TileOps& op, char* la0, char*
 
 template <int MODE, int PASS>
 __global__ __launch_bounds__(kThreads16, 2) void ffn_gemm_f32_kernel(const GemmParams p) {
-  constexpr bool VARK = MODE == M_DW;
+  constexpr bool VARK = is_dw(MODE);
   constexpr int kRowsA = (VARK ? 4 : kMidMaxH) * kMidUnit;
   __shared__ __attribute__((aligned(16))) char la0[kRowsA * kRowBytes];
   __shared__ __attribute__((aligned(16))) char lb0[kMidN * kRowBytes];
   __shared__ __attribute__((aligned(16))) char la1[kRowsA * kRowBytes];
   __shared__ __attribute__((aligned(16))) char lb1[kMidN * kRowBytes];
-  constexpr bool GATED = MODE == M_FWD1_SWIGLU;
+  constexpr bool GATED = is_gated(MODE);
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
   const int n_items = mid_items<MODE>(p);
@@ -1405,7 +1599,7 @@ __global__ __launch_bounds__(kThreads16, 2) void ffn_gemm_f32_kernel(const GemmP
           const int lm = blk * 32 + 8 * (q >> 2) + 4 * (lane >> 5) + (q & 3);
           if (lm >= t.m_valid) continue;
           const int64_t row = t.row0 + lm;
-          if constexpr (MODE == M_DW) {
+          if constexpr (VARK) {
             float* dst;
             if (t.slot >= 0) dst = p.partial + static_cast<int64_t>(t.slot) * p.slot_elems + row * p.N;
             else if (row < p.split_row) dst = p.dwA + static_cast<int64_t>(t.g) * p.dw_gstride + row * p.N;
@@ -1420,6 +1614,20 @@ __global__ __launch_bounds__(kThreads16, 2) void ffn_gemm_f32_kernel(const GemmP
                 reinterpret_cast<float*>(p.H3 + row * p.ldh)[col] = h3;
               }
               *c = h1 * sigm(h1) * h3;
+            } else if constexpr (MODE == M_GATED_FWD) {
+              const float h1 = acc[i][q], h3 = acc3[i][q];
+              if (p.H1) {
+                reinterpret_cast<float*>(p.H1 + row * p.ldh)[col] = h1;
+                reinterpret_cast<float*>(p.H3 + row * p.ldh)[col] = h3;
+              }
+              *c = gate_f(h1, p.act) * h3;
+            } else if constexpr (MODE == M_GATED_DA) {
+              const float h1 = reinterpret_cast<const float*>(p.H1 + row * p.ldh)[col];
+              const float h3 = reinterpret_cast<const float*>(p.H3 + row * p.ldh)[col];
+              gate_bwd(acc[i][q], h1, h3, p.act, *c, c[p.f]);
+            } else if constexpr (MODE == M_ADD_STORE) {
+              const float b = p.add ? reinterpret_cast<const float*>(p.add + row * p.ldadd)[col] : 0.f;
+              *c = acc[i][q] + b;
             } else if constexpr (MODE == M_FWD1) {
               if (p.H1) reinterpret_cast<float*>(p.H1 + row * p.ldh)[col] = acc[i][q];
               *c = act_f(acc[i][q], p.act);
@@ -1529,17 +1737,24 @@ constexpr int kReduceBlocks = 1024;   // blocks per expert
 __global__ __launch_bounds__(256) void split_reduce_kernel(
     const float* __restrict__ partial, int64_t slot_elems, const Sched* __restrict__ sc,
     float* __restrict__ dwA, float* __restrict__ dwB, int64_t dw_gstride, int split_row,
-    int N) {
+    int N, bool bf16_out) {
   const int g = blockIdx.y;
   const int ns = sc->nsplit[g];
   if (ns == 1) return;
+  // results: four fp32 values, or, in the layer dtype, four bf16
+  auto put = [&](float* to, int64_t o, const float4& v) {
+    if (bf16_out)
+      *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(to) + o) =
+          make_uint2(pack2bf(v.x, v.y), pack2bf(v.z, v.w));
+    else
+      *reinterpret_cast<float4*>(to + o) = v;
+  };
   if (ns == 0) {
     const int64_t na = static_cast<int64_t>(split_row) * N;   // elements in dwA, the rest in dwB
     for (int64_t i = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 4; i < slot_elems;
          i += static_cast<int64_t>(gridDim.x) * 1024) {
-      float* dst = i < na ? dwA + static_cast<int64_t>(g) * dw_gstride + i
-                          : dwB + static_cast<int64_t>(g) * dw_gstride + (i - na);
-      *reinterpret_cast<float4*>(dst) = make_float4(0.f, 0.f, 0.f, 0.f);
+      put(i < na ? dwA : dwB, static_cast<int64_t>(g) * dw_gstride + (i < na ? i : i - na),
+          make_float4(0.f, 0.f, 0.f, 0.f));
     }
     return;
   }
@@ -1568,10 +1783,8 @@ __global__ __launch_bounds__(256) void split_reduce_kernel(
       row = i / N;
       col = i % N;
     }
-    float* dst = row < split_row
-                     ? dwA + static_cast<int64_t>(g) * dw_gstride + row * N + col
-                     : dwB + static_cast<int64_t>(g) * dw_gstride + (row - split_row) * N + col;
-    *reinterpret_cast<float4*>(dst) = acc;
+    put(row < split_row ? dwA : dwB,
+        static_cast<int64_t>(g) * dw_gstride + (row < split_row ? row : row - split_row) * N + col, acc);
   }
 }
 
@@ -1654,7 +1867,7 @@ bool make_plan(moe_dtype dt, moe_act act, int E, int d, int f, int64_t rows_allo
 SchedArgs sched_args(const FfnPlan& pl, int nt0, int nt1, int k1, const StepCost& c0,
                      const StepCost& c1, char* ws) {
   const bool f32 = pl.es == 4;
-  const int ks = f32 ? kF32Step : 64;
+  const int ks = f32 ? kF32Step : kRowBytes / static_cast<int>(pl.es);
   return {pl.E, pl.rows_alloc, pl.max_mtiles, pl.max_mid, pl.max_segs, pl.tmn_min, pl.max_slots,
           {nt0, nt1}, {cdiv(pl.d, ks), cdiv(k1, ks)}, 2 * persistent_grid(),
           {f32 ? kStepF32 : c0, f32 ? kStepF32 : c1}, reinterpret_cast<Sched*>(ws + pl.o_sched),
@@ -1696,7 +1909,9 @@ bool use_mid_tiles(const FfnPlan& pl, moe_dtype dt, bool vark, bool gated, bool 
     const int64_t mid = static_cast<int64_t>(pl.E) * cdiv(p.M_out, kMidDwH * kMidUnit) * cdiv(p.N, kMidN);
     return 13 * ((mid + 2 * G - 1) / (2 * G)) < 20 * ((big + G - 1) / G);
   }
-  return mid_pays({pl.E, pl.rows_alloc, pl.rows_most, p.N, p.K, gated, act, b_km, p.lda, p.ldb}, G);
+  // a K step is 128 bytes of a row: the rule counts bf16 values
+  const int k16 = pl.es == 1 ? cdiv(p.K, 2) : p.K;
+  return mid_pays({pl.E, pl.rows_alloc, pl.rows_most, p.N, k16, gated, act, b_km, p.lda, p.ldb}, G);
 }
 
 // dX with a transposed copy of [W1; W3] (moe_set_dx_weight_copy, g_wt_mode: 0
@@ -1723,8 +1938,8 @@ const char* pass_name(int pass) {
 // gradients) for the kernel it picks.
 template <int MODE, int PASS>
 moe_status launch_gemm(hipStream_t s, moe_dtype dt, const FfnPlan& pl, char* ws, GemmParams p) {
-  constexpr bool VARK = MODE == M_DW, GATED = MODE == M_FWD1_SWIGLU;
-  constexpr bool ACTIVE = MODE != M_STORE && MODE != M_DW;
+  constexpr bool VARK = is_dw(MODE), GATED = is_gated(MODE);
+  constexpr bool ACTIVE = MODE != M_STORE && MODE != M_ADD_STORE && MODE != M_I8_STORE && !VARK;
   const bool mid = use_mid_tiles(pl, dt, VARK, GATED, ACTIVE, b_layout(PASS) == L_KM, p);
   const int tn = mid ? kMidN : BN;
   p.ntiles = cdiv(p.N, GATED ? tn / 2 : tn);
@@ -1750,7 +1965,7 @@ moe_status launch_gemm(hipStream_t s, moe_dtype dt, const FfnPlan& pl, char* ws,
   const int grid = static_cast<int>(std::min(full, std::max<int64_t>(kXcds, (max_items + kXcds - 1) / kXcds * kXcds)));
   MOE_TIMED(pass_name(PASS), s);
   if (dt == MOE_F32) {
-    if constexpr (PASS != P_BWD_DX_T) ffn_gemm_f32_kernel<MODE, PASS><<<grid, kThreads16, 0, s>>>(p);
+    if constexpr (PASS != P_BWD_DX_T && !is_i8(MODE)) ffn_gemm_f32_kernel<MODE, PASS><<<grid, kThreads16, 0, s>>>(p);
   } else if (mid) {
     ffn_gemm16_mid_kernel<MODE, PASS><<<grid, kThreads16, 0, s>>>(p);
   } else {
@@ -1770,14 +1985,15 @@ moe_status launch_gemm(hipStream_t s, moe_dtype dt, const FfnPlan& pl, char* ws,
 // result go to dwA, the rest to dwB; dw_gstride is the per-expert stride of
 // dwA and dwB (f x d for [dW1; dW3], whose M_out is 2f under SwiGLU).
 moe_status launch_split_reduce(hipStream_t s, const FfnPlan& pl, char* ws, int M_out, int N,
-                               float* dwA, float* dwB, int split_row, int64_t dw_gstride) {
+                               float* dwA, float* dwB, int split_row, int64_t dw_gstride,
+                               bool bf16_out = false) {
   const int64_t elems = static_cast<int64_t>(M_out) * N;
   const int64_t bx = cdiv(elems, 1024);
   dim3 grid(static_cast<unsigned>(bx < kReduceBlocks ? bx : kReduceBlocks), pl.E);
   MOE_TIMED("split_reduce", s);
   split_reduce_kernel<<<grid, 256, 0, s>>>(
       reinterpret_cast<const float*>(ws + pl.o_part), elems,
-      reinterpret_cast<const Sched*>(ws + pl.o_sched), dwA, dwB, dw_gstride, split_row, N);
+      reinterpret_cast<const Sched*>(ws + pl.o_sched), dwA, dwB, dw_gstride, split_row, N, bf16_out);
   MOE_LAUNCH_CHECK();
   return MOE_OK;
 }

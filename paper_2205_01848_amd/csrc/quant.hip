@@ -1,0 +1,216 @@
+// Rows of layer values in 8-bit integers with one scale each:
+//     scale = max_j |x_j| (1/127),   q_j = rint(x_j / scale)   (ties to even).
+// The scale is the fp32 product with the fp32 nearest to 1/127 (within one
+// unit in the last place of max |x| / 127); q is the integer nearest to the exact
+// quotient of x_j and that scale, clamped to +-127.  A row of zeros (or of
+// values so small that the scale rounds to zero) has scale 0 and q 0; a row
+// that holds a NaN or an infinity has scale NaN and q 0, so every product
+// with it is NaN.
+//
+// Bound by memory: n (es + 1) bytes a row, each value read once into registers,
+// where the row's maximum is found before anything is written.
+
+#include "quant.hpp"
+
+#include <algorithm>
+
+namespace moe {
+namespace {
+
+constexpr int kQuantThreads = 256;
+constexpr int kHeld = 4;   // units of 8 values a thread keeps in registers
+
+template <typename T> struct Unit;   // 8 values
+template <> struct Unit<uint16_t> {
+  uint4 v;
+  __device__ __forceinline__ void load(const uint16_t* p) { v = *reinterpret_cast<const uint4*>(p); }
+  __device__ __forceinline__ void get(float* f) const { unpack8(v, f); }
+};
+template <> struct Unit<float> {
+  uint4 lo, hi;
+  __device__ __forceinline__ void load(const float* p) {
+    lo = reinterpret_cast<const uint4*>(p)[0];
+    hi = reinterpret_cast<const uint4*>(p)[1];
+  }
+  __device__ __forceinline__ void get(float* f) const {
+    Elem<float>::load(lo, f);
+    Elem<float>::load(hi, f + 4);
+  }
+};
+
+// Largest |value| of a unit as bits: NaNs order above infinity and infinity
+// above every number, which a maximum of floats would lose.
+template <typename T>
+__device__ __forceinline__ uint32_t abs_bits_max(const Unit<T>& u, uint32_t m) {
+  float f[8];
+  u.get(f);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) m = max(m, __float_as_uint(f[e]) & 0x7FFFFFFFu);
+  return m;
+}
+
+// How a row is divided: pre (1, or 2^64 where the row's values are so small
+// that 1 / scale would overflow; a power of two, so exact), and the scale,
+// half of it and its reciprocal, all times pre.
+struct RowScale {
+  float pre, s, half, inv;
+};
+__device__ __forceinline__ RowScale row_scale(uint32_t amax, float& scale) {
+  const float a = __uint_as_float(amax);
+  scale = a < INFINITY ? a * (1.f / 127.f) : NAN;
+  const float pre = a < 0x1p-60f ? 0x1p64f : 1.f;
+  const float s = scale * pre;
+  const bool none = !(scale > 0.f);
+  return {none ? 0.f : pre, none ? 1.f : s, none ? 0.5f : 0.5f * s, none ? 0.f : 1.f / s};
+}
+
+// q for eight values.  x times the rounded reciprocal is within 2^-16 of the
+// quotient, so its rounding is off by one at the most, and only where the
+// quotient lies next to a half.  r = x - q s is exact in fp32 (it is a multiple of
+// half the last place of s and at most about s / 2), so comparing it with
+// s / 2 settles those cases; they are rare enough to branch on.
+template <typename T>
+__device__ __forceinline__ uint2 quantize8(const Unit<T>& u, const RowScale& rs) {
+  float f[8], q[8];
+  u.get(f);
+  bool border = false;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    f[e] = rs.pre != 0.f ? f[e] * rs.pre : 0.f;
+    q[e] = __builtin_rintf(f[e] * rs.inv);
+    border |= __builtin_fabsf(__builtin_fmaf(-q[e], rs.s, f[e])) >= rs.half;
+  }
+  if (border) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float r = __builtin_fmaf(-q[e], rs.s, f[e]), a = __builtin_fabsf(r);
+      const bool odd = static_cast<int>(q[e]) & 1;
+      if (a > rs.half || (a == rs.half && odd)) q[e] += r > 0.f ? 1.f : -1.f;
+    }
+  }
+  uint32_t b[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    b[e] = static_cast<uint32_t>(static_cast<int>(fminf(fmaxf(q[e], -127.f), 127.f))) & 255u;
+  return make_uint2(b[0] | b[1] << 8 | b[2] << 16 | b[3] << 24,
+                    b[4] | b[5] << 8 | b[6] << 16 | b[7] << 24);
+}
+
+// G threads take a row, in units of 8 values; the first kHeld G units stay in
+// registers between the two passes, a longer row's others are read again (from
+// the caches).  Rows are dealt round-robin.
+template <typename T, int G>
+__global__ __launch_bounds__(kQuantThreads) void quantize_kernel(
+    const T* __restrict__ x, int64_t ldx, int64_t rows, int n, int8_t* __restrict__ q,
+    float* __restrict__ scale, int E, const int32_t* __restrict__ offsets,
+    const int32_t* __restrict__ region_rows) {
+  constexpr int kPer = kQuantThreads / G;   // rows of a workgroup at a time
+  const int t = threadIdx.x % G, lane = threadIdx.x & 63;
+  const int units = n / 8, qunits = (n + 15) / 16 * 2;   // of values, of bytes written
+  const int64_t ldq = qunits * 8;
+  int64_t r0 = 0, r1 = 0;   // the lane's region of valid rows
+  if (offsets && lane < E) {
+    r0 = offsets[lane];
+    r1 = min(static_cast<int64_t>(offsets[lane + 1]), r0 + region_rows[lane]);
+  }
+  __shared__ uint32_t part[2][kQuantThreads / kWave];
+  int turn = 0;
+  for (int64_t base = static_cast<int64_t>(blockIdx.x) * kPer; base < rows;
+       base += static_cast<int64_t>(gridDim.x) * kPer) {
+    const int64_t row = base + threadIdx.x / G;   // the same for a whole wavefront
+    bool live = row < rows;
+    if (offsets) live = live && __any(row >= r0 && row < r1);
+    Unit<T> held[kHeld];
+    uint32_t m = 0;
+    const T* xr = x + row * ldx;
+    if (live) {
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i)
+        if (t + i * G < units) held[i].load(xr + (t + i * G) * 8);
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i)
+        if (t + i * G < units) m = abs_bits_max<T>(held[i], m);
+      for (int u = t + kHeld * G; u < units; u += G) {
+        Unit<T> v;
+        v.load(xr + u * 8);
+        m = abs_bits_max<T>(v, m);
+      }
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), o, 64)));
+    if constexpr (G > kWave) {
+      // one row per workgroup: two sets of partial maxima in turn, so one
+      // barrier a row suffices
+      part[turn][threadIdx.x / kWave] = m;
+      __syncthreads();
+#pragma unroll
+      for (int w = 0; w < kQuantThreads / kWave; ++w) m = max(m, part[turn][w]);
+      turn ^= 1;
+    }
+    if (!live) continue;
+    float sc;
+    const RowScale rs = row_scale(m, sc);
+    if (t == 0) scale[row] = sc;
+    int8_t* qr = q + row * ldq;
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+      const int u = t + i * G;
+      if (u < units) *reinterpret_cast<uint2*>(qr + u * 8) = quantize8<T>(held[i], rs);
+      else if (u < qunits) *reinterpret_cast<uint2*>(qr + u * 8) = make_uint2(0, 0);
+    }
+    for (int u = t + kHeld * G; u < qunits; u += G) {
+      uint2 b = make_uint2(0, 0);
+      if (u < units) {
+        Unit<T> v;
+        v.load(xr + u * 8);
+        b = quantize8<T>(v, rs);
+      }
+      *reinterpret_cast<uint2*>(qr + u * 8) = b;
+    }
+  }
+}
+
+template <typename T, int G>
+moe_status launch(hipStream_t s, int64_t rows, int64_t most, int n, const void* x, int64_t ldx,
+                  int8_t* q, float* scale, int E, const int32_t* offsets,
+                  const int32_t* region_rows) {
+  constexpr int kPer = kQuantThreads / G;
+  const int64_t need = (rows + kPer - 1) / kPer;
+  const int grid = static_cast<int>(std::min<int64_t>(need, 8 * num_cus()));
+  MOE_TIMED("quantize_rows", s);
+  quantize_kernel<T, G><<<grid, kQuantThreads, 0, s>>>(static_cast<const T*>(x), ldx, rows, n, q,
+                                                        scale, E, offsets, region_rows);
+  MOE_LAUNCH_CHECK();
+  return MOE_OK;
+}
+
+}  // namespace
+
+moe_status quantize_launch(hipStream_t s, moe_dtype dt, int64_t rows, int64_t most, int n,
+                           const void* x, int64_t ldx, int8_t* q, float* scale, int E,
+                           const int32_t* offsets, const int32_t* region_rows) {
+  if (rows == 0) return MOE_OK;
+  // a wavefront a row while the row fits its registers, else a workgroup
+  const bool wave = n <= 8 * kHeld * kWave;
+  if (dt == MOE_BF16)
+    return wave ? launch<uint16_t, kWave>(s, rows, most, n, x, ldx, q, scale, E, offsets, region_rows)
+                : launch<uint16_t, kQuantThreads>(s, rows, most, n, x, ldx, q, scale, E, offsets, region_rows);
+  return wave ? launch<float, kWave>(s, rows, most, n, x, ldx, q, scale, E, offsets, region_rows)
+              : launch<float, kQuantThreads>(s, rows, most, n, x, ldx, q, scale, E, offsets, region_rows);
+}
+
+}  // namespace moe
+
+using namespace moe;
+
+extern "C" int moe_quantized_width(int n) { return n < 0 ? 0 : quantized_width(n); }
+
+extern "C" moe_status moe_quantize_rows(void* stream, moe_dtype dt, int64_t rows, int n,
+                                        const void* x, int64_t ldx, int8_t* q, float* scale) {
+  if (!dtype_ok(dt) || rows < 0 || !width_ok(n) || n > kMaxQuant || ldx < n || ldx % 8 != 0)
+    return MOE_EINVAL;
+  if (rows == 0) return MOE_OK;
+  if (!x || !q || !scale || !aligned16(x) || !aligned16(q)) return MOE_EINVAL;
+  return quantize_launch(static_cast<hipStream_t>(stream), dt, rows, rows, n, x, ldx, q, scale, 0,
+                         nullptr, nullptr);
+}

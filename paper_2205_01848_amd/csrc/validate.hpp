@@ -27,6 +27,10 @@ inline bool shape_ok(int T, int E, int k) {
 // widths: >= 1 and multiples of 8 (16-byte vectors of bf16, 32 bytes of f32)
 inline bool width_ok(int d) { return d >= 8 && (d % 8) == 0; }
 
+// longest quantised row: int32 sums of products of two int8 values (at most
+// 127 * 127 each) are exact up to 133,152 of them
+constexpr int kMaxQuant = 131072;
+
 inline bool rows_ok(int64_t rows_alloc) {
   return rows_alloc >= 0 && rows_alloc < (int64_t(1) << 31);
 }
