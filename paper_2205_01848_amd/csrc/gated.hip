@@ -9,36 +9,48 @@
 // addend (the routed experts' output, or their gradient) goes into the
 // epilogue of the last product, so y and dx are written once.
 //
-// The products are those of the experts (gemm.hpp) with one expert of T rows.
+// The products are those of the experts (gemm.hpp) on one expert of T rows.  The
+// host knows T, so it plans them itself (dense_plan) and no schedule kernel runs.
 
 #include "gemm.hpp"
 
 namespace moe {
 namespace {
 
-// The schedule of one expert of T rows, and the row layout the products read.
-__global__ __launch_bounds__(64 * kSchedTasks) void schedule_dense_kernel(int T, int32_t* offsets,
-                                                                          const SchedArgs A) {
-  if (threadIdx.x < 2) offsets[threadIdx.x] = threadIdx.x ? T : 0;
-  build_schedule<kSchedTasks>((threadIdx.x & 63) == 0 ? T : 0, A);
-}
-
-// Workspace: the products' schedule and buffers as for E = 1, then the row
-// layout (two int32).
+// The block's products, planned from the sizes alone (rows as if contiguous, so
+// that the workspace query and the calls agree), and the workspace: forward,
+// A (where h_save does not hold it) and Y's partial sums; backward, dH, the
+// partial sums of the product that has most, and the transposed weights.
 struct GatedPlan {
-  FfnPlan pl;
-  size_t o_off, total_fwd, total_bwd, total_bwd_wt;
+  DensePlan h, y, da, dx, dw2, dw13;
+  bool wt;                 // dX reads a transposed copy of [W1; W3]
+  size_t o_part_fwd, total_fwd;
+  size_t o_part, o_wt, total_bwd;
 };
 
 bool plan_gated(moe_dtype dt, int T, int d, int f, GatedPlan& g) {
-  if (T < 0 || !make_plan(dt, MOE_SWIGLU, 1, d, f, T, g.pl)) return false;
-  g.o_off = g.pl.o_end_sched;
-  // every buffer behind the schedule moves by the layout's 256 bytes
-  FfnPlan& pl = g.pl;
-  pl.o_abuf += 256; pl.o_dh += 256; pl.o_part += 256; pl.o_wt13 += 256;
-  g.total_fwd = pl.total_fwd + 256;
-  g.total_bwd = pl.total_bwd + 256;
-  g.total_bwd_wt = pl.total_bwd_wt + 256;
+  FfnPlan pl;   // its limits on the sizes
+  if (T < 0 || !make_plan(dt, MOE_SWIGLU, 1, d, f, T, pl)) return false;
+  const int F = 2 * f;
+  const int64_t es = static_cast<int64_t>(pl.es), rd = d * es, rf = f * es, rF = F * es;
+  g = {};
+  g.total_fwd = g.total_bwd = 256;
+  if (T == 0) return true;
+  g.wt = use_wt13(pl, dt);
+  g.h = dense_plan<M_GATED_FWD, P_FWD_H>(dt, T, T, f, d, rd, rd);
+  g.y = dense_plan<M_ADD_STORE, P_FWD_Y>(dt, T, T, d, f, rf, rf);
+  g.da = dense_plan<M_GATED_DA, P_BWD_DA>(dt, T, T, f, d, rd, rf);
+  g.dx = g.wt ? dense_plan<M_ADD_STORE, P_BWD_DX_T>(dt, T, T, d, F, rF, rF)
+              : dense_plan<M_ADD_STORE, P_BWD_DX>(dt, T, T, d, F, rF, rd);
+  g.dw2 = dense_plan<M_DENSE_DW, P_BWD_DW2>(dt, T, d, f, T, rd, rf);
+  g.dw13 = dense_plan<M_DENSE_DW, P_BWD_DW13>(dt, T, F, d, T, rF, rd);
+  const size_t rows = static_cast<size_t>(T);
+  g.o_part_fwd = align_up(rows * f * pl.es, 256);
+  g.total_fwd = g.o_part_fwd + dense_partial_bytes(g.y, T, d) + 256;
+  g.o_part = align_up(rows * F * pl.es, 256);
+  g.o_wt = g.o_part + std::max({dense_partial_bytes(g.dx, T, d), dense_partial_bytes(g.dw2, d, f),
+                                dense_partial_bytes(g.dw13, F, d)});
+  g.total_bwd = g.o_wt + (g.wt ? align_up(static_cast<size_t>(d) * F * pl.es, 256) : 0) + 256;
   return true;
 }
 
@@ -46,18 +58,26 @@ int gate_act(moe_act act) {
   return act == MOE_RELU ? ACT_RELU : act == MOE_GELU_TANH ? ACT_GELU : ACT_SWIGLU;
 }
 
+// Zeros by a kernel, which a captured graph replays like any other.
+__global__ __launch_bounds__(256) void zero_kernel(uint4* p, int64_t n) {
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < n;
+       i += static_cast<int64_t>(gridDim.x) * 256)
+    p[i] = make_uint4(0, 0, 0, 0);
+}
+moe_status launch_zero(hipStream_t s, void* p, size_t bytes) {   // a multiple of 16
+  const int64_t n = static_cast<int64_t>(bytes / 16);
+  MOE_TIMED("zero_dw", s);
+  zero_kernel<<<static_cast<int>(std::min<int64_t>(8 * num_cus(), (n + 255) / 256)), 256, 0, s>>>(
+      static_cast<uint4*>(p), n);
+  MOE_LAUNCH_CHECK();
+  return MOE_OK;
+}
+
 bool act_ok(moe_act act) { return act == MOE_RELU || act == MOE_GELU_TANH || act == MOE_SWIGLU; }
 
 // Rows ld elements apart: whole 16-byte vectors, 256 rows within 2^31 bytes.
 bool pitch_ok(int64_t ld, int d, size_t es) {
   return ld >= d && ld % 8 == 0 && ld * static_cast<int64_t>(es) <= kMaxOperandRowBytes;
-}
-
-moe_status schedule_dense(hipStream_t s, int T, const SchedArgs& a, int32_t* offsets) {
-  MOE_TIMED("ffn_schedule", s);
-  schedule_dense_kernel<<<1, 64 * kSchedTasks, 0, s>>>(T, offsets, a);
-  MOE_LAUNCH_CHECK();
-  return MOE_OK;
 }
 
 }  // namespace
@@ -72,8 +92,7 @@ extern "C" size_t moe_gated_ffn_fwd_workspace_bytes(moe_dtype dt, int T, int d, 
 
 extern "C" size_t moe_gated_ffn_bwd_workspace_bytes(moe_dtype dt, int T, int d, int f) {
   GatedPlan g;
-  if (!plan_gated(dt, T, d, f, g)) return 0;
-  return use_wt13(g.pl, dt) ? g.total_bwd_wt : g.total_bwd;
+  return plan_gated(dt, T, d, f, g) ? g.total_bwd : 0;
 }
 
 extern "C" moe_status moe_gated_ffn_fwd(void* stream, moe_dtype dt, moe_act act, int T, int d,
@@ -83,7 +102,7 @@ extern "C" moe_status moe_gated_ffn_fwd(void* stream, moe_dtype dt, moe_act act,
                                         void* workspace, size_t workspace_bytes) {
   GatedPlan g;
   if (!act_ok(act) || !plan_gated(dt, T, d, f, g)) return MOE_EINVAL;
-  const size_t e = g.pl.es;
+  const size_t e = esize(dt);
   if (!pitch_ok(ldx, d, e) || !pitch_ok(ldy, d, e) || (add && !pitch_ok(ldadd, d, e)))
     return MOE_EINVAL;
   if (T == 0) return MOE_OK;
@@ -94,14 +113,9 @@ extern "C" moe_status moe_gated_ffn_fwd(void* stream, moe_dtype dt, moe_act act,
   if (!workspace || workspace_bytes < g.total_fwd || !aligned16(workspace)) return MOE_EWORKSPACE;
   hipStream_t s = static_cast<hipStream_t>(stream);
   char* ws = static_cast<char*>(workspace);
-  const FfnPlan& pl = g.pl;
   const int64_t es = static_cast<int64_t>(e), plane = static_cast<int64_t>(T) * f * es;
-  int32_t* offsets = reinterpret_cast<int32_t*>(ws + g.o_off);
-  MOE_TRY(schedule_dense(s, T, sched_args(pl, cdiv(f, kMidN / 2), cdiv(d, kMidN), f,
-                                          step16(ldx * es, d * es, false),
-                                          step16(f * es, f * es, false), ws), offsets));
-  char* a = h_save ? static_cast<char*>(h_save) + 2 * plane : ws + pl.o_abuf;
-  GemmParams p = base_params(pl, offsets, ws);
+  char* a = h_save ? static_cast<char*>(h_save) + 2 * plane : ws;
+  GemmParams p{};
   p.A = static_cast<const char*>(x);
   p.lda = ldx * es;
   p.B = static_cast<const char*>(w1);
@@ -115,8 +129,8 @@ extern "C" moe_status moe_gated_ffn_fwd(void* stream, moe_dtype dt, moe_act act,
   p.H1 = static_cast<char*>(h_save);
   p.H3 = h_save ? static_cast<char*>(h_save) + plane : nullptr;
   p.ldh = f * es;
-  MOE_TRY(launch_gemm<M_GATED_FWD, P_FWD_H>(s, dt, pl, ws, p));
-  GemmParams q = base_params(pl, offsets, ws);
+  MOE_TRY(launch_dense<M_GATED_FWD, P_FWD_H>(s, dt, g.h, T, T, p));
+  GemmParams q{};
   q.A = a;
   q.lda = f * es;
   q.B = static_cast<const char*>(w2);
@@ -127,7 +141,8 @@ extern "C" moe_status moe_gated_ffn_fwd(void* stream, moe_dtype dt, moe_act act,
   q.ldc = ldy * es;
   q.add = static_cast<const char*>(add);
   q.ldadd = ldadd * es;
-  return launch_gemm<M_ADD_STORE, P_FWD_Y>(s, dt, pl, ws, q);
+  q.partial = reinterpret_cast<float*>(ws + g.o_part_fwd);
+  return launch_dense<M_ADD_STORE, P_FWD_Y>(s, dt, g.y, T, T, q);
 }
 
 extern "C" moe_status moe_gated_ffn_bwd(void* stream, moe_dtype dt, moe_act act, int T, int d,
@@ -140,7 +155,7 @@ extern "C" moe_status moe_gated_ffn_bwd(void* stream, moe_dtype dt, moe_act act,
   GatedPlan g;
   if (!act_ok(act) || !plan_gated(dt, T, d, f, g)) return MOE_EINVAL;
   if (dw_dt != dt && dw_dt != MOE_F32) return MOE_EINVAL;
-  const size_t e = g.pl.es;
+  const size_t e = esize(dt);
   if (!pitch_ok(ldx, d, e) || !pitch_ok(lddy, d, e) || !pitch_ok(lddx, d, e) ||
       (add && !pitch_ok(ldadd, d, e)))
     return MOE_EINVAL;
@@ -153,22 +168,23 @@ extern "C" moe_status moe_gated_ffn_bwd(void* stream, moe_dtype dt, moe_act act,
   if (!workspace || workspace_bytes < g.total_bwd || !aligned16(workspace)) return MOE_EWORKSPACE;
   hipStream_t s = static_cast<hipStream_t>(stream);
   char* ws = static_cast<char*>(workspace);
-  const FfnPlan& pl = g.pl;
   const int64_t es = static_cast<int64_t>(e), plane = static_cast<int64_t>(T) * f * es;
   const int F = 2 * f;
-  const bool wt = use_wt13(pl, dt) && workspace_bytes >= g.total_bwd_wt;
-  int32_t* offsets = reinterpret_cast<int32_t*>(ws + g.o_off);
-  MOE_TRY(schedule_dense(s, T, sched_args(pl, cdiv(f, kMidN), cdiv(d, kMidN), F,
-                                          step16(lddy * es, f * es, true),
-                                          step16(F * es, (wt ? F : d) * es, !wt), ws), offsets));
+  float* partial = reinterpret_cast<float*>(ws + g.o_part);
   const char* h1 = static_cast<const char*>(h_save);
   const char* a = h1 + 2 * plane;
-  char* dh = ws + pl.o_dh;      // [T, 2f]: dH1 | dH3
-  char* wt13 = ws + pl.o_wt13;
-  if (wt) MOE_TRY(launch_transpose_w(s, 1, w1, w3, f, f, d, wt13));
+  char* dh = ws;   // [T, 2f]: dH1 | dH3
+  char* wt13 = ws + g.o_wt;
+  if (T == 0) {
+    // nothing to contract over: the weight gradients are zero
+    const size_t bytes = static_cast<size_t>(d) * f * esize(dw_dt);
+    for (void* w : {dw1, dw3, dw2}) MOE_TRY(launch_zero(s, w, bytes));
+    return MOE_OK;
+  }
+  if (g.wt) MOE_TRY(launch_transpose_w(s, 1, w1, w3, f, f, d, wt13));
 
   // dH from dA = dY W2 (W2 read K-major)
-  GemmParams p = base_params(pl, offsets, ws);
+  GemmParams p{};
   p.A = static_cast<const char*>(dy);
   p.lda = lddy * es;
   p.B = static_cast<const char*>(w2);
@@ -182,10 +198,10 @@ extern "C" moe_status moe_gated_ffn_bwd(void* stream, moe_dtype dt, moe_act act,
   p.H3 = const_cast<char*>(h1) + plane;
   p.ldh = f * es;
   p.f = f;
-  MOE_TRY(launch_gemm<M_GATED_DA, P_BWD_DA>(s, dt, pl, ws, p));
+  MOE_TRY(launch_dense<M_GATED_DA, P_BWD_DA>(s, dt, g.da, T, T, p));
 
   // dX = add + [dH1 | dH3] [W1; W3]
-  GemmParams q = base_params(pl, offsets, ws);
+  GemmParams q{};
   q.A = dh;
   q.lda = F * es;
   q.K = F;
@@ -194,39 +210,38 @@ extern "C" moe_status moe_gated_ffn_bwd(void* stream, moe_dtype dt, moe_act act,
   q.ldc = lddx * es;
   q.add = static_cast<const char*>(add);
   q.ldadd = ldadd * es;
-  if (wt) {
+  q.partial = partial;
+  if (g.wt) {
     q.B = wt13;
     q.ldb = F * es;
-    MOE_TRY(launch_gemm<M_ADD_STORE, P_BWD_DX_T>(s, dt, pl, ws, q));
+    MOE_TRY(launch_dense<M_ADD_STORE, P_BWD_DX_T>(s, dt, g.dx, T, T, q));
   } else {
     q.B = static_cast<const char*>(w1);
     q.B2 = static_cast<const char*>(w3);
     q.kmsplit = f;
     q.ldb = d * es;
-    MOE_TRY(launch_gemm<M_ADD_STORE, P_BWD_DX>(s, dt, pl, ws, q));
+    MOE_TRY(launch_dense<M_ADD_STORE, P_BWD_DX>(s, dt, g.dx, T, T, q));
   }
 
   // dW2 [d, f] = dY^T A, then [dW1; dW3] [2f, d] = [dH1 dH3]^T X
-  const bool layer_dw = dw_dt == MOE_BF16;
-  auto launch_dw = [&](auto pass, const void* l, int64_t ldl, const void* r, int64_t ldr, int m,
-                       int n, void* to1, void* to2, int split) -> moe_status {
-    constexpr int PASS = decltype(pass)::value;
-    GemmParams u = base_params(pl, offsets, ws);
+  auto weights = [&](const void* l, int64_t ldl, const void* r, int64_t ldr, int m, int n, void* to1,
+                     void* to2, int split) {
+    GemmParams u{};
     u.A = static_cast<const char*>(l);
     u.lda = ldl * es;
     u.M_out = m;
     u.B = static_cast<const char*>(r);
     u.ldb = ldr * es;
     u.N = n;
+    u.out_f32 = dw_dt == MOE_F32;
     u.dwA = static_cast<float*>(to1);
     u.dwB = static_cast<float*>(to2);
     u.split_row = split;
-    u.partial = reinterpret_cast<float*>(ws + pl.o_part);
-    u.slot_elems = static_cast<int64_t>(m) * n;
-    if (layer_dw) MOE_TRY(launch_gemm<M_DW_LAYER, PASS>(s, dt, pl, ws, u));
-    else MOE_TRY(launch_gemm<M_DW, PASS>(s, dt, pl, ws, u));
-    return launch_split_reduce(s, pl, ws, m, n, u.dwA, u.dwB, split, 0, layer_dw);
+    u.partial = partial;
+    return u;
   };
-  MOE_TRY(launch_dw(std::integral_constant<int, P_BWD_DW2>{}, dy, lddy, a, f, d, f, dw2, dw2, d));
-  return launch_dw(std::integral_constant<int, P_BWD_DW13>{}, dh, F, x, ldx, F, d, dw1, dw3, f);
+  MOE_TRY(launch_dense<M_DENSE_DW, P_BWD_DW2>(s, dt, g.dw2, T, d,
+                                              weights(dy, lddy, a, f, d, f, dw2, dw2, d)));
+  return launch_dense<M_DENSE_DW, P_BWD_DW13>(s, dt, g.dw13, T, F,
+                                              weights(dh, F, x, ldx, F, d, dw1, dw3, f));
 }

@@ -225,18 +225,20 @@ enum Mode {
   M_I8_STORE = 6,          // plain store in the layer dtype
   M_I8_FWD1 = 7,           // A = act(H)
   M_I8_FWD1_SWIGLU = 8,    // A = silu(H1) H3
-  // the dense gated block (gated.hip); the gate half's activation at run time
+  // the dense gated block (gated.hip): no routing arrays, see Dense; the gate
+  // half's activation at run time
   M_GATED_FWD = 9,         // H1, H3 -> A = act(H1) H3 [, H1 H3 saved]
   M_GATED_DA = 10,         // dA = dY W2 -> dH1 = dA H3 act'(H1), dH3 = dA act(H1)
-  M_ADD_STORE = 11,        // store with an addend (Y, dX)
-  M_DW_LAYER = 12          // weight gradient in the layer dtype
+  M_ADD_STORE = 11,        // store with an addend (Y, dX), or partial sums
+  M_DENSE_DW = 12          // weight gradient in fp32 or bf16, or partial sums
 };
+constexpr bool is_dense(int mode) { return mode >= M_GATED_FWD; }
 constexpr bool is_i8(int mode) { return mode >= M_I8_STORE && mode <= M_I8_FWD1_SWIGLU; }
 // W1 and W3 share a tile
 constexpr bool is_gated(int mode) {
   return mode == M_FWD1_SWIGLU || mode == M_I8_FWD1_SWIGLU || mode == M_GATED_FWD;
 }
-constexpr bool is_dw(int mode) { return mode == M_DW || mode == M_DW_LAYER; }
+constexpr bool is_dw(int mode) { return mode == M_DW || mode == M_DENSE_DW; }
 // bytes per operand element of the 16x16 kernels
 constexpr int op_bytes(int mode) { return is_i8(mode) ? 1 : 2; }
 
@@ -251,6 +253,15 @@ __device__ __forceinline__ float row_scale_at(const RowScales& s, int64_t row) {
   if (!s.src) return s.scale[row];
   return s.scale[min(max(s.src[row] / s.k, 0), s.T - 1)];
 }
+
+// A dense product: the host knows its rows, so it needs no device schedule.  Its
+// tiles are those of one expert of T rows; K (the weight gradients': T) is
+// split into `splits` ranges of klen, whose partial sums go to slots.
+struct Dense {
+  int T;        // rows of the tokens' operands
+  int n_mt;     // tiles along M
+  int splits, klen;
+};
 
 struct GemmParams {
   // operands (bytes).  var-M: A rows of the dispatched buffer, B the
@@ -282,6 +293,7 @@ struct GemmParams {
   // s_gstride apart); fp32 outputs
   RowScales a_scale; const float* b_scale; const float* b2_scale; int64_t s_gstride;
   int out_f32;
+  Dense dense;
 };
 
 // Tile order, two levels above each XCD's kGroupM x 8 block of tiles.
@@ -903,7 +915,7 @@ __device__ __forceinline__ void epilogue16(const GemmParams& p,
     return p.dwB + static_cast<int64_t>(g) * p.dw_gstride +
            static_cast<int64_t>(orow - p.split_row) * p.N + gc;
   };
-  // M_DW_LAYER, no partial sums: one expert, results in bf16
+  // M_DENSE_DW, no partial sums: one expert, results in bf16
   auto dw_dst16 = [&](int orow, int gc) -> uint16_t* {
     return orow < p.split_row
                ? reinterpret_cast<uint16_t*>(p.dwA) + static_cast<int64_t>(orow) * p.N + gc
@@ -921,7 +933,7 @@ __device__ __forceinline__ void epilogue16(const GemmParams& p,
       for (int r = 0; r < WR; r += RG) {
         const int lm = wr0 + r + el / LR, gc = n0 + wn * WC + (el % LR) * 8;
         if (lm < m_valid && gc < p.N) {
-          if (MODE == M_DW_LAYER && slot < 0) {
+          if (MODE == M_DENSE_DW && slot < 0 && !p.out_f32) {
             *reinterpret_cast<uint4*>(dw_dst16(row0 + lm, gc)) = make_uint4(0, 0, 0, 0);
             continue;
           }
@@ -1051,7 +1063,7 @@ __device__ __forceinline__ void epilogue16(const GemmParams& p,
         if (lm < m_valid && gc < p.N) {
           const float* sp = strip + r * kP + c8;
           if constexpr (is_dw(MODE)) {
-            if (MODE == M_DW_LAYER && slot < 0) {
+            if (MODE == M_DENSE_DW && slot < 0 && !p.out_f32) {
               *reinterpret_cast<uint4*>(dw_dst16(row0 + lm, gc)) = pack8(sp);
               continue;
             }
@@ -1064,6 +1076,12 @@ __device__ __forceinline__ void epilogue16(const GemmParams& p,
             for (int e = 0; e < 8; ++e) v[e] = sp[e];
             const int64_t grow = row0 + lm;
             if constexpr (MODE == M_ADD_STORE) {
+              if (slot >= 0) {
+                float* dst = p.partial + slot * p.slot_elems + grow * p.N + gc;
+                *reinterpret_cast<float4*>(dst) = make_float4(v[0], v[1], v[2], v[3]);
+                *reinterpret_cast<float4*>(dst + 4) = make_float4(v[4], v[5], v[6], v[7]);
+                continue;
+              }
               if (p.add) {
                 float b[8];
                 unpack8(*reinterpret_cast<const uint4*>(p.add + grow * p.ldadd + static_cast<int64_t>(gc) * ES), b);
@@ -1183,6 +1201,49 @@ __device__ __forceinline__ void epilogue_i8(const GemmParams& p, const floatx4 (
   }
 }
 
+// Items of a dense product: its tiles, once for every range of K.
+template <int MODE>
+__device__ __forceinline__ int dense_items(const GemmParams& p) {
+  return p.dense.splits * (is_dw(MODE) ? p.mtiles_out : p.dense.n_mt) * p.ntiles;
+}
+// Tile of item L; returns its K range.
+template <int MODE>
+__device__ __forceinline__ int dense_tile(const GemmParams& p, int L, int& mt, int& nt) {
+  const int n_mt = is_dw(MODE) ? p.mtiles_out : p.dense.n_mt, tiles = n_mt * p.ntiles;
+  const int si = L / tiles;
+  decode_banded(L - si * tiles, n_mt, p.ntiles, mt, nt);
+  return si;
+}
+// Operands of K range si of the tile at row0, n0 (tn columns, the gated forward's
+// half of W1 and half of W3); ES: bytes per element.
+template <int MODE, int PASS, int ES>
+__device__ __forceinline__ TileOps dense_ops(const GemmParams& p, int row0, int m_valid, int n0,
+                                             int tn, int si) {
+  TileOps op;
+  const int k0 = si * p.dense.klen;
+  if constexpr (is_dw(MODE)) {
+    op.K = min(p.dense.klen, p.dense.T - k0);
+    op.a = {p.A + k0 * p.lda + static_cast<int64_t>(row0) * ES, nullptr, p.lda, m_valid, 0x7FFFFFFF};
+    op.b = {p.B + k0 * p.ldb + static_cast<int64_t>(n0) * ES, nullptr, p.ldb, min(tn, p.N - n0),
+            0x7FFFFFFF};
+  } else {
+    op.K = min(p.dense.klen, p.K - k0);
+    op.a = {p.A + row0 * p.lda + static_cast<int64_t>(k0) * ES, nullptr, p.lda, m_valid, 0};
+    if constexpr (is_gated(MODE)) {
+      op.b = {p.B + n0 * p.ldb, p.B2 + n0 * p.ldb, p.ldb, min(tn / 2, p.N - n0), 0};
+    } else if constexpr (b_layout(PASS) == L_KC) {
+      op.b = {p.B + n0 * p.ldb + static_cast<int64_t>(k0) * ES, nullptr, p.ldb, min(tn, p.N - n0), 0};
+    } else {
+      // k-rows below kmsplit come from B, the others from B2; this range starts at k0
+      const int64_t o = static_cast<int64_t>(n0) * ES;
+      op.b = {p.B + o + k0 * p.ldb,
+              p.B2 ? p.B2 + o + max(k0 - p.kmsplit, 0) * p.ldb : nullptr, p.ldb,
+              min(tn, p.N - n0), p.B2 ? max(p.kmsplit - k0, 0) : 0x7FFFFFFF};
+    }
+  }
+  return op;
+}
+
 template <int MODE, int PASS>
 __global__ __launch_bounds__(kThreads16, 1) void ffn_gemm16_kernel(const GemmParams p) {
   __shared__ __attribute__((aligned(16))) char la0[kTileBytes];
@@ -1198,9 +1259,11 @@ __global__ __launch_bounds__(kThreads16, 1) void ffn_gemm16_kernel(const GemmPar
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
   const int wm = wave >> 1, wn = wave & 1;
-  const Sched& sc = *p.sched;
-  const int n_mt = sc.n_mtiles;
-  const int n_items = VARK ? sc.n_segs * p.mtiles_out * p.ntiles : n_mt * p.ntiles;
+  constexpr bool DENSE = is_dense(MODE);
+  const Sched& sc = *p.sched;   // not read by dense products
+  const int n_mt = DENSE ? p.dense.n_mt : sc.n_mtiles;
+  const int n_items = DENSE ? dense_items<MODE>(p)
+                            : VARK ? sc.n_segs * p.mtiles_out * p.ntiles : n_mt * p.ntiles;
   const int G = gridDim.x;
   const int lbase = (blockIdx.x % kXcds) * (G / kXcds) + blockIdx.x / kXcds;
 
@@ -1210,7 +1273,15 @@ __global__ __launch_bounds__(kThreads16, 1) void ffn_gemm16_kernel(const GemmPar
     TileOps op;
     int g, row0, m_valid, n0;
     int slot = -1, mt, nt;
-    if constexpr (!VARK) {
+    if constexpr (DENSE) {
+      const int si = dense_tile<MODE>(p, L, mt, nt);
+      g = 0;
+      row0 = mt * TM;
+      n0 = nt * (GATED ? TN / 2 : TN);
+      m_valid = min(TM, (VARK ? p.M_out : p.dense.T) - row0);
+      slot = p.dense.splits > 1 ? si : -1;
+      op = dense_ops<MODE, PASS, ES>(p, row0, m_valid, n0, TN, si);
+    } else if constexpr (!VARK) {
       int mti;
       decode_banded(L, n_mt, p.ntiles, mti, nt);
       const int2 tm = p.mtile[mti];
@@ -1304,6 +1375,7 @@ struct MidTile {
 
 template <int MODE>
 __device__ __forceinline__ int mid_items(const GemmParams& p) {
+  if constexpr (is_dense(MODE)) return dense_items<MODE>(p);
   const Sched& sc = *p.sched;
   return (is_dw(MODE) ? sc.n_segs * p.mtiles_out : sc.n_mid[p.mid_list]) * p.ntiles;
 }
@@ -1313,10 +1385,26 @@ template <int MODE, int PASS, int ES>
 __device__ __forceinline__ void mid_operands(const GemmParams& p, int L, MidTile& t) {
   constexpr bool GATED = is_gated(MODE);
   constexpr int BLAY = b_layout(PASS), TN = kMidN;
-  const Sched& sc = *p.sched;
+  const Sched& sc = *p.sched;   // not read by dense products
   int mt, nt;
   t.slot = -1;
-  if constexpr (!is_dw(MODE)) {
+  if constexpr (is_dense(MODE)) {
+    constexpr bool VARK = is_dw(MODE);
+    const int si = dense_tile<MODE>(p, L, mt, nt);
+    t.g = 0;
+    if constexpr (VARK) {
+      t.h = p.dw_h;
+      t.row0 = mt * t.h * kMidUnit;
+    } else {
+      const int2 tm = mid_tile(p.dense.T, p.dense.n_mt, mt, 0);
+      t.h = tm.x >> 8;
+      t.row0 = tm.y;
+    }
+    t.m_valid = min(t.h * kMidUnit, (VARK ? p.M_out : p.dense.T) - t.row0);
+    t.n0 = nt * (GATED ? TN / 2 : TN);
+    t.slot = p.dense.splits > 1 ? si : -1;
+    t.op = dense_ops<MODE, PASS, ES>(p, t.row0, t.m_valid, t.n0, TN, si);
+  } else if constexpr (!is_dw(MODE)) {
     decode_banded(L, sc.n_mid[p.mid_list], p.ntiles, mt, nt);
     const int2 tm = p.mtile[mt];
     const int g = t.g = tm.x & 255;
@@ -1626,6 +1714,10 @@ __global__ __launch_bounds__(kThreads16, 2) void ffn_gemm_f32_kernel(const GemmP
               const float h3 = reinterpret_cast<const float*>(p.H3 + row * p.ldh)[col];
               gate_bwd(acc[i][q], h1, h3, p.act, *c, c[p.f]);
             } else if constexpr (MODE == M_ADD_STORE) {
+              if (t.slot >= 0) {
+                p.partial[t.slot * p.slot_elems + row * p.N + col] = acc[i][q];
+                continue;
+              }
               const float b = p.add ? reinterpret_cast<const float*>(p.add + row * p.ldadd)[col] : 0.f;
               *c = acc[i][q] + b;
             } else if constexpr (MODE == M_FWD1) {
@@ -1737,24 +1829,17 @@ constexpr int kReduceBlocks = 1024;   // blocks per expert
 __global__ __launch_bounds__(256) void split_reduce_kernel(
     const float* __restrict__ partial, int64_t slot_elems, const Sched* __restrict__ sc,
     float* __restrict__ dwA, float* __restrict__ dwB, int64_t dw_gstride, int split_row,
-    int N, bool bf16_out) {
+    int N) {
   const int g = blockIdx.y;
   const int ns = sc->nsplit[g];
   if (ns == 1) return;
-  // results: four fp32 values, or, in the layer dtype, four bf16
-  auto put = [&](float* to, int64_t o, const float4& v) {
-    if (bf16_out)
-      *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(to) + o) =
-          make_uint2(pack2bf(v.x, v.y), pack2bf(v.z, v.w));
-    else
-      *reinterpret_cast<float4*>(to + o) = v;
-  };
   if (ns == 0) {
     const int64_t na = static_cast<int64_t>(split_row) * N;   // elements in dwA, the rest in dwB
     for (int64_t i = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) * 4; i < slot_elems;
          i += static_cast<int64_t>(gridDim.x) * 1024) {
-      put(i < na ? dwA : dwB, static_cast<int64_t>(g) * dw_gstride + (i < na ? i : i - na),
-          make_float4(0.f, 0.f, 0.f, 0.f));
+      float* dst = i < na ? dwA + static_cast<int64_t>(g) * dw_gstride + i
+                          : dwB + static_cast<int64_t>(g) * dw_gstride + (i - na);
+      *reinterpret_cast<float4*>(dst) = make_float4(0.f, 0.f, 0.f, 0.f);
     }
     return;
   }
@@ -1783,8 +1868,10 @@ __global__ __launch_bounds__(256) void split_reduce_kernel(
       row = i / N;
       col = i % N;
     }
-    put(row < split_row ? dwA : dwB,
-        static_cast<int64_t>(g) * dw_gstride + (row < split_row ? row : row - split_row) * N + col, acc);
+    float* dst = row < split_row
+                     ? dwA + static_cast<int64_t>(g) * dw_gstride + row * N + col
+                     : dwB + static_cast<int64_t>(g) * dw_gstride + (row - split_row) * N + col;
+    *reinterpret_cast<float4*>(dst) = acc;
   }
 }
 
@@ -1975,6 +2062,149 @@ moe_status launch_gemm(hipStream_t s, moe_dtype dt, const FfnPlan& pl, char* ws,
   return MOE_OK;
 }
 
+// ---- dense products ---------------------------------------------------------------
+// The kernel, tile height and number of K ranges of a dense product, by the
+// estimates of tiles.hpp: the host knows every size.  Splitting K gives a
+// product of few tiles to more CUs and costs the write and the read of the
+// partial sums and a launch.
+struct DensePlan {
+  bool mid;
+  int h;          // units of rows per tile (mid)
+  int n_mt, nt;   // tiles along M and N
+  int splits, klen;
+};
+
+template <int MODE, int PASS>
+DensePlan dense_plan(moe_dtype dt, int T, int M, int N, int K, int64_t lda, int64_t ldb) {
+  constexpr bool VARK = is_dw(MODE), GATED = is_gated(MODE), BKM = b_layout(PASS) == L_KM;
+  constexpr bool ACTIVE = MODE == M_GATED_FWD || MODE == M_GATED_DA;
+  const bool f32 = dt == MOE_F32;
+  const int ks = f32 ? kF32Step : 64, steps = cdiv(K, ks), cus = persistent_grid();
+  const int out_bytes = f32 ? 4 : 2;
+  StepCost c = f32 ? kStepF32 : step16(lda, ldb, BKM);
+  if (VARK && !f32) {   // both operands K-major: 64 k-rows of 256 bytes each
+    c.lines_fixed = (lda % 128 ? 600 : 400) + (ldb % 128 ? 600 : 400);
+    c.lines_per_unit = 0;
+  }
+  const int most = ACTIVE ? 1 : std::max(1, std::min(16, steps / 4));
+  DensePlan best{};
+  int64_t t_best = -1;
+  auto take = [&](int64_t t, const DensePlan& p) {
+    if (t_best < 0 || t < t_best) { t_best = t; best = p; }
+  };
+  for (int want = 1; want <= most; ++want) {
+    const int per = cdiv(steps, want), splits = cdiv(steps, per);   // K steps of a range
+    if (splits != want) continue;
+    // partial sums: written and read at about 4.5 bytes per ns, and a launch
+    const int64_t join = splits == 1 ? 0 : static_cast<int64_t>(M) * N * (8 * splits + out_bytes) / 4500 + 4000;
+    const int n_units = cdiv(M, kMidUnit), nt = cdiv(N, GATED ? kMidN / 2 : kMidN);
+    const int64_t big = static_cast<int64_t>(cdiv(M, BM)) * cdiv(N, GATED ? BN / 2 : BN) * splits;
+    const int64_t rounds = cdiv(big, cus), r = std::min<int64_t>(rounds, 6);
+    const bool whole = M % BM == 0;
+    for (int h = 1; h <= kMidMaxH && (f32 || g_tile_mode != 1); ++h) {
+      if (VARK && (f32 ? h > 4 || h == 3 : h != kMidDwH)) continue;
+      const int n = cdiv(n_units, h), high = VARK ? h : cdiv(n_units, n);
+      // the gated fp32 kernel gives a wave every other block of 32 rows
+      const int cost_h = f32 && GATED ? high + (high & 1) : high;
+      int64_t t = mid_time(static_cast<int64_t>(n) * nt * splits, cost_h, 2 * cus, per, c);
+      if (!f32) t = t * (whole ? 47 + 3 * r : 35 + 5 * r) / 50;
+      take(t + join, {true, high, n, nt, splits, per * ks});
+    }
+    if (!f32 && g_tile_mode != 2) {
+      const bool few = 2 * big <= cus;
+      const int step = VARK ? std::max(1700, big_step16(lda, ldb, true, few)) : big_step16(lda, ldb, BKM, few);
+      take(rounds * (static_cast<int64_t>(step) * per + (ACTIVE ? 13000 : 10000)) + join,
+           {false, 0, cdiv(M, BM), cdiv(N, GATED ? BN / 2 : BN), splits, per * ks});
+    }
+  }
+  return best;
+}
+
+// Sums the `splits` slots of an [M, N] product in order, adds the addend and
+// writes rows [0, split_row) to c1 and the others to c2, ldc elements apart.
+struct JoinArgs {
+  const float* partial;
+  int64_t slot_elems;
+  int splits, M, N;
+  const char* add; int64_t ldadd;   // bytes
+  char *c1, *c2; int64_t ldc;       // bytes
+  int split_row;
+};
+template <typename T>
+__global__ __launch_bounds__(256) void dense_join_kernel(const JoinArgs a) {
+  const int per_row = a.N / 4;
+  const int64_t total = static_cast<int64_t>(a.M) * per_row;
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < total;
+       i += static_cast<int64_t>(gridDim.x) * 256) {
+    const int row = static_cast<int>(i / per_row), col = static_cast<int>(i - static_cast<int64_t>(row) * per_row) * 4;
+    const float* p = a.partial + i * 4;
+    float4 v = *reinterpret_cast<const float4*>(p);
+    for (int s = 1; s < a.splits; ++s) {
+      const float4 u = *reinterpret_cast<const float4*>(p + s * a.slot_elems);
+      v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
+    }
+    if (a.add) {
+      const T* b = reinterpret_cast<const T*>(a.add + row * a.ldadd) + col;
+      if constexpr (sizeof(T) == 4) {
+        const float4 u = *reinterpret_cast<const float4*>(b);
+        v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
+      } else {
+        const uint2 u = *reinterpret_cast<const uint2*>(b);
+        v.x += __uint_as_float(u.x << 16); v.y += __uint_as_float(u.x & 0xFFFF0000u);
+        v.z += __uint_as_float(u.y << 16); v.w += __uint_as_float(u.y & 0xFFFF0000u);
+      }
+    }
+    T* c = reinterpret_cast<T*>(row < a.split_row ? a.c1 + row * a.ldc : a.c2 + (row - a.split_row) * a.ldc) + col;
+    if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(c) = v;
+    else *reinterpret_cast<uint2*>(c) = make_uint2(pack2bf(v.x, v.y), pack2bf(v.z, v.w));
+  }
+}
+
+// Bytes of partial sums of a planned product.
+inline size_t dense_partial_bytes(const DensePlan& d, int M, int N) {
+  return d.splits > 1 ? align_up(static_cast<size_t>(d.splits) * M * N * 4, 256) : 0;
+}
+
+// Launches one dense product of M x N results by plan d, its partial sums in p.partial.
+template <int MODE, int PASS>
+moe_status launch_dense(hipStream_t s, moe_dtype dt, const DensePlan& d, int T, int M, GemmParams p) {
+  constexpr bool VARK = is_dw(MODE);
+  p.ntiles = d.nt;
+  p.dense = {T, d.n_mt, d.splits, d.klen};
+  p.mtiles_out = d.n_mt;
+  p.dw_h = d.h;
+  p.slot_elems = static_cast<int64_t>(M) * p.N;
+  const int64_t items = static_cast<int64_t>(d.splits) * d.n_mt * d.nt;
+  const int64_t full = (d.mid ? 2 : 1) * static_cast<int64_t>(persistent_grid());
+  const int grid = static_cast<int>(std::min(full, (items + kXcds - 1) / kXcds * kXcds));
+  {
+    MOE_TIMED(pass_name(PASS), s);
+    if (dt == MOE_F32) {
+      if constexpr (PASS != P_BWD_DX_T) ffn_gemm_f32_kernel<MODE, PASS><<<grid, kThreads16, 0, s>>>(p);
+    } else if (d.mid) {
+      ffn_gemm16_mid_kernel<MODE, PASS><<<grid, kThreads16, 0, s>>>(p);
+    } else {
+      ffn_gemm16_kernel<MODE, PASS><<<grid, kThreads16, 0, s>>>(p);
+    }
+    MOE_LAUNCH_CHECK();
+  }
+  if (d.splits == 1) return MOE_OK;
+  const bool f32 = VARK ? p.out_f32 : dt == MOE_F32;
+  JoinArgs j{p.partial, p.slot_elems, d.splits, M, p.N, p.add, p.ldadd, p.C, p.C, p.ldc, M};
+  if (VARK) {
+    j.c1 = reinterpret_cast<char*>(p.dwA);
+    j.c2 = reinterpret_cast<char*>(p.dwB);
+    j.ldc = static_cast<int64_t>(p.N) * (f32 ? 4 : 2);
+    j.split_row = p.split_row;
+  }
+  const int jgrid = static_cast<int>(std::min<int64_t>(8 * num_cus(), (p.slot_elems / 4 + 255) / 256));
+  MOE_TIMED("split_reduce", s);
+  if (f32) dense_join_kernel<float><<<jgrid, 256, 0, s>>>(j);
+  else dense_join_kernel<uint16_t><<<jgrid, 256, 0, s>>>(j);
+  MOE_LAUNCH_CHECK();
+  return MOE_OK;
+}
+
 #define MOE_TRY(...)                       \
   do {                                     \
     moe_status st_ = (__VA_ARGS__);        \
@@ -1985,15 +2215,14 @@ moe_status launch_gemm(hipStream_t s, moe_dtype dt, const FfnPlan& pl, char* ws,
 // result go to dwA, the rest to dwB; dw_gstride is the per-expert stride of
 // dwA and dwB (f x d for [dW1; dW3], whose M_out is 2f under SwiGLU).
 moe_status launch_split_reduce(hipStream_t s, const FfnPlan& pl, char* ws, int M_out, int N,
-                               float* dwA, float* dwB, int split_row, int64_t dw_gstride,
-                               bool bf16_out = false) {
+                               float* dwA, float* dwB, int split_row, int64_t dw_gstride) {
   const int64_t elems = static_cast<int64_t>(M_out) * N;
   const int64_t bx = cdiv(elems, 1024);
   dim3 grid(static_cast<unsigned>(bx < kReduceBlocks ? bx : kReduceBlocks), pl.E);
   MOE_TIMED("split_reduce", s);
   split_reduce_kernel<<<grid, 256, 0, s>>>(
       reinterpret_cast<const float*>(ws + pl.o_part), elems,
-      reinterpret_cast<const Sched*>(ws + pl.o_sched), dwA, dwB, dw_gstride, split_row, N, bf16_out);
+      reinterpret_cast<const Sched*>(ws + pl.o_sched), dwA, dwB, dw_gstride, split_row, N);
   MOE_LAUNCH_CHECK();
   return MOE_OK;
 }
