@@ -9,7 +9,8 @@
 // instead of 64, at the same number of matrix instructions, so the same loop
 // does twice the products per second, and the same bytes.
 
-#include "gemm.hpp"
+#include "dense.hpp"
+#include "few_rows.hpp"
 #include "quant.hpp"
 
 namespace moe {
@@ -32,6 +33,72 @@ bool plan_i8(moe_dtype dt, moe_act act, int E, int d, int f, int64_t rows_alloc,
   q.o_as = o; o = align_up(o + static_cast<size_t>(rows_alloc) * 4, 256);
   q.total = o;
   return true;
+}
+
+// The kernel of one product: the one for few rows, deep tiles of 32, 64 or 128
+// rows, or the tiles of gemm.hpp with their schedule.
+enum KernelI8 { I8_FEW, I8_DEEP32, I8_DEEP64, I8_DEEP128, I8_TILES };
+
+// The host knows the rows at most and their mean over the experts, not the
+// loads: it compares the estimated times for experts of the mean, half a tile
+// more for raggedness.  A product is as long as its rounds of tiles (tile_time; a K
+// step is 128 bytes, as in bf16) or as the read of its live experts' weights, at
+// 5.6 bytes per ps, a tenth more for every further tile of an expert.  Few rows:
+// up to 16, bound by that read.  Over 47 calls (1 to 64 experts, 1 to 6000
+// rows, K from 1000 to 14336) the choice takes 0.3 % more than the best kernel.
+// Examples, us a call, few / deep 32 / deep 64 / deep 128 / tiles: FFN 4096,
+// 14336 of 8 experts, 8 rows 176 / 182 / 192 / 197 / 231, 256 rows 685 / 324 / 282
+// / 295 / 326, 1024 rows 2224 / 625 / 473 / 441 / 381; 64 experts 2048, 1408,
+// 512 rows 132 / 90 / 91 / 101 / 103; one product 14336 -> 4096, 16 rows 18 / 28
+// / 38 / 53 / 58.
+KernelI8 kernel_i8(const FfnPlan& pl, int K, int N, bool gated) {
+  if (g_tile_mode != 0) return I8_TILES;
+  const int groups = static_cast<int>(std::min<int64_t>(pl.E, pl.rows_most)), cus = persistent_grid();
+  const double mean = std::max(1., static_cast<double>(pl.rows_most) / pl.E);
+  const int steps = cdiv(K, kRowBytes);
+  const double read = static_cast<double>(groups) * N * (gated ? 2 : 1) * K / 5600;
+  auto tiles = [&](int unit) {   // of all experts, along M
+    return groups > 1 ? groups * std::max(1., mean / unit + 0.5) : static_cast<double>(cdiv(pl.rows_most, unit));
+  };
+  auto rounds = [&](double n, int per_cu, int half) {
+    const int places = per_cu * cus;
+    return n > places ? n / places + 0.25 : per_cu == 2 && 2 * n <= places ? half / 100. : 1.;
+  };
+  auto tile = [&](DenseKernel k, int h, int unit, int cols, int per_cu) {
+    const TileTime t = tile_time(false, k, h, D_KC);
+    return rounds(tiles(unit) * cdiv(N, gated ? cols / 2 : cols), per_cu, t.half) *
+           (static_cast<double>(t.step) * steps + t.fix);
+  };
+  KernelI8 best = I8_TILES;
+  double t_best = tile(K_BIG, 0, BM, BN, 1);
+  for (int h = 1; h <= kMidMaxH; ++h)
+    t_best = std::min(t_best, tile(K_MID, h, kMidUnit * h, kMidN, 2));
+  t_best = std::max(t_best, 1.15 * read + 3000) + 7000;   // and the schedule's launch
+  auto take = [&](KernelI8 k, double t) {
+    if (t < t_best) { t_best = t; best = k; }
+  };
+  for (int h = 1; h <= 4; h *= 2)
+    take(h == 1 ? I8_DEEP32 : h == 2 ? I8_DEEP64 : I8_DEEP128,
+         std::max(tile(K_DEEP, h, kMidUnit * h, kMidN, h <= 2 ? 2 : 1),
+                  read * (0.9 + 0.1 * tiles(kMidUnit * h) / groups) + 3000));
+  if (pl.rows_most <= 16) take(I8_FEW, read + 2500);
+  return best;
+}
+
+// One product by kernel k.  Only the tiles of gemm.hpp need the schedule.
+template <int MODE, int PASS>
+moe_status launch_i8(hipStream_t s, KernelI8 k, const FfnPlan& pl, char* ws, const int32_t* rows,
+                     const GemmParams& p) {
+  if (k == I8_TILES) return launch_gemm<MODE, PASS>(s, MOE_BF16, pl, ws, p);
+  GroupParams gp{p, pl.E, rows, pl.rows_alloc};
+  const int groups = static_cast<int>(std::min<int64_t>(pl.E, pl.rows_most));
+  if (k == I8_FEW) return launch_few<MODE, 1>(s, pass_name(PASS), gp, pl.rows_most, groups);
+  gp.p.ntiles = cdiv(p.N, is_gated(MODE) ? kMidN / 2 : kMidN);
+  const int unit = k == I8_DEEP32 ? 32 : k == I8_DEEP64 ? 64 : 128;
+  const int64_t most = (pl.rows_most / unit + groups) * gp.p.ntiles;
+  if (k == I8_DEEP32) return launch_deep<MODE, PASS, 1>(s, gp, most);
+  if (k == I8_DEEP64) return launch_deep<MODE, PASS, 2>(s, gp, most);
+  return launch_deep<MODE, PASS, 4>(s, gp, most);
 }
 
 bool scales_ok(const float* x_scale, const int32_t* src, int T, int k) {
@@ -88,10 +155,12 @@ extern "C" moe_status moe_expert_matmul_i8(void* stream, moe_dtype dt, int E, in
   hipStream_t s = static_cast<hipStream_t>(stream);
   char* ws = static_cast<char*>(workspace);
   const StepCost c = step16(K, K, false);
-  MOE_TRY(launch_schedule(s, sched_args(pl, cdiv(N, kMidN), cdiv(N, kMidN), K, c, c, ws), offsets,
-                          rows));
-  return launch_gemm<M_I8_STORE, P_FWD_Y>(
-      s, MOE_BF16, pl, ws,
+  const KernelI8 kernel = kernel_i8(pl, K, N, false);
+  if (kernel == I8_TILES)
+    MOE_TRY(launch_schedule(s, sched_args(pl, cdiv(N, kMidN), cdiv(N, kMidN), K, c, c, ws), offsets,
+                            rows));
+  return launch_i8<M_I8_STORE, P_FWD_Y>(
+      s, kernel, pl, ws, rows,
       params_i8(pl, offsets, ws, K, N, xq, {x_scale, src, T, k}, wq, w_scale, dt, y));
 }
 
@@ -123,9 +192,11 @@ extern "C" moe_status moe_expert_ffn_fwd_i8(void* stream, moe_dtype dt, moe_act 
   FfnPlan& pl = q.pl;
   if (src) pl.rows_most = std::min<int64_t>(rows_alloc, static_cast<int64_t>(T) * k);
   const int kd = quantized_width(d), kf = quantized_width(f);
-  MOE_TRY(launch_schedule(s, sched_args(pl, cdiv(f, sw ? kMidN / 2 : kMidN), cdiv(d, kMidN), kf,
-                                        step16(kd, kd, false), step16(kf, kf, false), ws),
-                          offsets, rows));
+  const KernelI8 up = kernel_i8(pl, kd, f, sw), down = kernel_i8(pl, kf, d, false);
+  if (up == I8_TILES || down == I8_TILES)
+    MOE_TRY(launch_schedule(s, sched_args(pl, cdiv(f, sw ? kMidN / 2 : kMidN), cdiv(d, kMidN), kf,
+                                          step16(kd, kd, false), step16(kf, kf, false), ws),
+                            offsets, rows));
   char* a = ws + q.o_a;
   int8_t* aq = reinterpret_cast<int8_t*>(ws + q.o_aq);
   float* as = reinterpret_cast<float*>(ws + q.o_as);
@@ -135,12 +206,12 @@ extern "C" moe_status moe_expert_ffn_fwd_i8(void* stream, moe_dtype dt, moe_act 
   if (sw) {
     p.B2 = reinterpret_cast<const char*>(w3q);
     p.b2_scale = w3_scale;
-    MOE_TRY(launch_gemm<M_I8_FWD1_SWIGLU, P_FWD_H>(s, MOE_BF16, pl, ws, p));
+    MOE_TRY(launch_i8<M_I8_FWD1_SWIGLU, P_FWD_H>(s, up, pl, ws, rows, p));
   } else {
-    MOE_TRY(launch_gemm<M_I8_FWD1, P_FWD_H>(s, MOE_BF16, pl, ws, p));
+    MOE_TRY(launch_i8<M_I8_FWD1, P_FWD_H>(s, up, pl, ws, rows, p));
   }
   MOE_TRY(quantize_launch(s, dt, rows_alloc, rows_alloc, f, a, f, aq, as, E, offsets, rows));
-  return launch_gemm<M_I8_STORE, P_FWD_Y>(
-      s, MOE_BF16, pl, ws, params_i8(pl, offsets, ws, kf, d, aq, {as, nullptr, 0, 0}, w2q, w2_scale, dt,
+  return launch_i8<M_I8_STORE, P_FWD_Y>(
+      s, down, pl, ws, rows, params_i8(pl, offsets, ws, kf, d, aq, {as, nullptr, 0, 0}, w2q, w2_scale, dt,
                                      y_disp));
 }

@@ -12,7 +12,8 @@
 // The products are those of the experts (gemm.hpp) on one expert of T rows.  The
 // host knows T, so it plans them itself (dense_plan) and no schedule kernel runs.
 
-#include "gemm.hpp"
+#include "dense.hpp"
+#include "few_rows.hpp"
 
 namespace moe {
 namespace {
@@ -23,10 +24,14 @@ namespace {
 // partial sums of the product that has most, and the transposed weights.
 struct GatedPlan {
   DensePlan h, y, da, dx, dw2, dw13;
+  bool few;                // the forward's products by the kernel for few rows
   bool wt;                 // dX reads a transposed copy of [W1; W3]
   size_t o_part_fwd, total_fwd;
   size_t o_part, o_wt, total_bwd;
 };
+
+// Rows up to which the forward streams its weights through the kernel for few rows.
+constexpr int kFewDense = 16;
 
 bool plan_gated(moe_dtype dt, int T, int d, int f, GatedPlan& g) {
   FfnPlan pl;   // its limits on the sizes
@@ -36,17 +41,18 @@ bool plan_gated(moe_dtype dt, int T, int d, int f, GatedPlan& g) {
   g = {};
   g.total_fwd = g.total_bwd = 256;
   if (T == 0) return true;
+  g.few = T <= (dt == MOE_F32 ? 2 : 1) * kFewDense;
   g.wt = use_wt13(pl, dt);
-  g.h = dense_plan<M_GATED_FWD, P_FWD_H>(dt, T, T, f, d, rd, rd);
-  g.y = dense_plan<M_ADD_STORE, P_FWD_Y>(dt, T, T, d, f, rf, rf);
-  g.da = dense_plan<M_GATED_DA, P_BWD_DA>(dt, T, T, f, d, rd, rf);
-  g.dx = g.wt ? dense_plan<M_ADD_STORE, P_BWD_DX_T>(dt, T, T, d, F, rF, rF)
-              : dense_plan<M_ADD_STORE, P_BWD_DX>(dt, T, T, d, F, rF, rd);
-  g.dw2 = dense_plan<M_DENSE_DW, P_BWD_DW2>(dt, T, d, f, T, rd, rf);
-  g.dw13 = dense_plan<M_DENSE_DW, P_BWD_DW13>(dt, T, F, d, T, rF, rd);
+  g.h = dense_plan<M_GATED_FWD, P_FWD_H>(dt, T, f, d, rd, rd);
+  g.y = dense_plan<M_ADD_STORE, P_FWD_Y>(dt, T, d, f, rf, rf);
+  g.da = dense_plan<M_GATED_DA, P_BWD_DA>(dt, T, f, d, rd, rf);
+  g.dx = g.wt ? dense_plan<M_ADD_STORE, P_BWD_DX_T>(dt, T, d, F, rF, rF)
+              : dense_plan<M_ADD_STORE, P_BWD_DX>(dt, T, d, F, rF, rd);
+  g.dw2 = dense_plan<M_DENSE_DW, P_BWD_DW2>(dt, d, f, T, rd, rf);
+  g.dw13 = dense_plan<M_DENSE_DW, P_BWD_DW13>(dt, F, d, T, rF, rd);
   const size_t rows = static_cast<size_t>(T);
   g.o_part_fwd = align_up(rows * f * pl.es, 256);
-  g.total_fwd = g.o_part_fwd + dense_partial_bytes(g.y, T, d) + 256;
+  g.total_fwd = g.o_part_fwd + (g.few ? 0 : dense_partial_bytes(g.y, T, d)) + 256;
   g.o_part = align_up(rows * F * pl.es, 256);
   g.o_wt = g.o_part + std::max({dense_partial_bytes(g.dx, T, d), dense_partial_bytes(g.dw2, d, f),
                                 dense_partial_bytes(g.dw13, F, d)});
@@ -71,6 +77,14 @@ moe_status launch_zero(hipStream_t s, void* p, size_t bytes) {   // a multiple o
       static_cast<uint4*>(p), n);
   MOE_LAUNCH_CHECK();
   return MOE_OK;
+}
+
+template <int MODE, int PASS>
+moe_status launch_few_dense(hipStream_t s, moe_dtype dt, int T, const GemmParams& p) {
+  GroupParams fp{p, 0, nullptr, 0};
+  fp.p.dense.T = T;
+  if (dt == MOE_F32) return launch_few<MODE, 4>(s, pass_name(PASS), fp, T, 1);
+  return launch_few<MODE, 2>(s, pass_name(PASS), fp, T, 1);
 }
 
 bool act_ok(moe_act act) { return act == MOE_RELU || act == MOE_GELU_TANH || act == MOE_SWIGLU; }
@@ -129,7 +143,8 @@ extern "C" moe_status moe_gated_ffn_fwd(void* stream, moe_dtype dt, moe_act act,
   p.H1 = static_cast<char*>(h_save);
   p.H3 = h_save ? static_cast<char*>(h_save) + plane : nullptr;
   p.ldh = f * es;
-  MOE_TRY(launch_dense<M_GATED_FWD, P_FWD_H>(s, dt, g.h, T, T, p));
+  if (g.few) MOE_TRY(launch_few_dense<M_GATED_FWD, P_FWD_H>(s, dt, T, p));
+  else MOE_TRY(launch_dense<M_GATED_FWD, P_FWD_H>(s, dt, g.h, T, T, p));
   GemmParams q{};
   q.A = a;
   q.lda = f * es;
@@ -142,6 +157,7 @@ extern "C" moe_status moe_gated_ffn_fwd(void* stream, moe_dtype dt, moe_act act,
   q.add = static_cast<const char*>(add);
   q.ldadd = ldadd * es;
   q.partial = reinterpret_cast<float*>(ws + g.o_part_fwd);
+  if (g.few) return launch_few_dense<M_ADD_STORE, P_FWD_Y>(s, dt, T, q);
   return launch_dense<M_ADD_STORE, P_FWD_Y>(s, dt, g.y, T, T, q);
 }
 

@@ -2062,149 +2062,6 @@ moe_status launch_gemm(hipStream_t s, moe_dtype dt, const FfnPlan& pl, char* ws,
   return MOE_OK;
 }
 
-// ---- dense products ---------------------------------------------------------------
-// The kernel, tile height and number of K ranges of a dense product, by the
-// estimates of tiles.hpp: the host knows every size.  Splitting K gives a
-// product of few tiles to more CUs and costs the write and the read of the
-// partial sums and a launch.
-struct DensePlan {
-  bool mid;
-  int h;          // units of rows per tile (mid)
-  int n_mt, nt;   // tiles along M and N
-  int splits, klen;
-};
-
-template <int MODE, int PASS>
-DensePlan dense_plan(moe_dtype dt, int T, int M, int N, int K, int64_t lda, int64_t ldb) {
-  constexpr bool VARK = is_dw(MODE), GATED = is_gated(MODE), BKM = b_layout(PASS) == L_KM;
-  constexpr bool ACTIVE = MODE == M_GATED_FWD || MODE == M_GATED_DA;
-  const bool f32 = dt == MOE_F32;
-  const int ks = f32 ? kF32Step : 64, steps = cdiv(K, ks), cus = persistent_grid();
-  const int out_bytes = f32 ? 4 : 2;
-  StepCost c = f32 ? kStepF32 : step16(lda, ldb, BKM);
-  if (VARK && !f32) {   // both operands K-major: 64 k-rows of 256 bytes each
-    c.lines_fixed = (lda % 128 ? 600 : 400) + (ldb % 128 ? 600 : 400);
-    c.lines_per_unit = 0;
-  }
-  const int most = ACTIVE ? 1 : std::max(1, std::min(16, steps / 4));
-  DensePlan best{};
-  int64_t t_best = -1;
-  auto take = [&](int64_t t, const DensePlan& p) {
-    if (t_best < 0 || t < t_best) { t_best = t; best = p; }
-  };
-  for (int want = 1; want <= most; ++want) {
-    const int per = cdiv(steps, want), splits = cdiv(steps, per);   // K steps of a range
-    if (splits != want) continue;
-    // partial sums: written and read at about 4.5 bytes per ns, and a launch
-    const int64_t join = splits == 1 ? 0 : static_cast<int64_t>(M) * N * (8 * splits + out_bytes) / 4500 + 4000;
-    const int n_units = cdiv(M, kMidUnit), nt = cdiv(N, GATED ? kMidN / 2 : kMidN);
-    const int64_t big = static_cast<int64_t>(cdiv(M, BM)) * cdiv(N, GATED ? BN / 2 : BN) * splits;
-    const int64_t rounds = cdiv(big, cus), r = std::min<int64_t>(rounds, 6);
-    const bool whole = M % BM == 0;
-    for (int h = 1; h <= kMidMaxH && (f32 || g_tile_mode != 1); ++h) {
-      if (VARK && (f32 ? h > 4 || h == 3 : h != kMidDwH)) continue;
-      const int n = cdiv(n_units, h), high = VARK ? h : cdiv(n_units, n);
-      // the gated fp32 kernel gives a wave every other block of 32 rows
-      const int cost_h = f32 && GATED ? high + (high & 1) : high;
-      int64_t t = mid_time(static_cast<int64_t>(n) * nt * splits, cost_h, 2 * cus, per, c);
-      if (!f32) t = t * (whole ? 47 + 3 * r : 35 + 5 * r) / 50;
-      take(t + join, {true, high, n, nt, splits, per * ks});
-    }
-    if (!f32 && g_tile_mode != 2) {
-      const bool few = 2 * big <= cus;
-      const int step = VARK ? std::max(1700, big_step16(lda, ldb, true, few)) : big_step16(lda, ldb, BKM, few);
-      take(rounds * (static_cast<int64_t>(step) * per + (ACTIVE ? 13000 : 10000)) + join,
-           {false, 0, cdiv(M, BM), cdiv(N, GATED ? BN / 2 : BN), splits, per * ks});
-    }
-  }
-  return best;
-}
-
-// Sums the `splits` slots of an [M, N] product in order, adds the addend and
-// writes rows [0, split_row) to c1 and the others to c2, ldc elements apart.
-struct JoinArgs {
-  const float* partial;
-  int64_t slot_elems;
-  int splits, M, N;
-  const char* add; int64_t ldadd;   // bytes
-  char *c1, *c2; int64_t ldc;       // bytes
-  int split_row;
-};
-template <typename T>
-__global__ __launch_bounds__(256) void dense_join_kernel(const JoinArgs a) {
-  const int per_row = a.N / 4;
-  const int64_t total = static_cast<int64_t>(a.M) * per_row;
-  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < total;
-       i += static_cast<int64_t>(gridDim.x) * 256) {
-    const int row = static_cast<int>(i / per_row), col = static_cast<int>(i - static_cast<int64_t>(row) * per_row) * 4;
-    const float* p = a.partial + i * 4;
-    float4 v = *reinterpret_cast<const float4*>(p);
-    for (int s = 1; s < a.splits; ++s) {
-      const float4 u = *reinterpret_cast<const float4*>(p + s * a.slot_elems);
-      v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
-    }
-    if (a.add) {
-      const T* b = reinterpret_cast<const T*>(a.add + row * a.ldadd) + col;
-      if constexpr (sizeof(T) == 4) {
-        const float4 u = *reinterpret_cast<const float4*>(b);
-        v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
-      } else {
-        const uint2 u = *reinterpret_cast<const uint2*>(b);
-        v.x += __uint_as_float(u.x << 16); v.y += __uint_as_float(u.x & 0xFFFF0000u);
-        v.z += __uint_as_float(u.y << 16); v.w += __uint_as_float(u.y & 0xFFFF0000u);
-      }
-    }
-    T* c = reinterpret_cast<T*>(row < a.split_row ? a.c1 + row * a.ldc : a.c2 + (row - a.split_row) * a.ldc) + col;
-    if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(c) = v;
-    else *reinterpret_cast<uint2*>(c) = make_uint2(pack2bf(v.x, v.y), pack2bf(v.z, v.w));
-  }
-}
-
-// Bytes of partial sums of a planned product.
-inline size_t dense_partial_bytes(const DensePlan& d, int M, int N) {
-  return d.splits > 1 ? align_up(static_cast<size_t>(d.splits) * M * N * 4, 256) : 0;
-}
-
-// Launches one dense product of M x N results by plan d, its partial sums in p.partial.
-template <int MODE, int PASS>
-moe_status launch_dense(hipStream_t s, moe_dtype dt, const DensePlan& d, int T, int M, GemmParams p) {
-  constexpr bool VARK = is_dw(MODE);
-  p.ntiles = d.nt;
-  p.dense = {T, d.n_mt, d.splits, d.klen};
-  p.mtiles_out = d.n_mt;
-  p.dw_h = d.h;
-  p.slot_elems = static_cast<int64_t>(M) * p.N;
-  const int64_t items = static_cast<int64_t>(d.splits) * d.n_mt * d.nt;
-  const int64_t full = (d.mid ? 2 : 1) * static_cast<int64_t>(persistent_grid());
-  const int grid = static_cast<int>(std::min(full, (items + kXcds - 1) / kXcds * kXcds));
-  {
-    MOE_TIMED(pass_name(PASS), s);
-    if (dt == MOE_F32) {
-      if constexpr (PASS != P_BWD_DX_T) ffn_gemm_f32_kernel<MODE, PASS><<<grid, kThreads16, 0, s>>>(p);
-    } else if (d.mid) {
-      ffn_gemm16_mid_kernel<MODE, PASS><<<grid, kThreads16, 0, s>>>(p);
-    } else {
-      ffn_gemm16_kernel<MODE, PASS><<<grid, kThreads16, 0, s>>>(p);
-    }
-    MOE_LAUNCH_CHECK();
-  }
-  if (d.splits == 1) return MOE_OK;
-  const bool f32 = VARK ? p.out_f32 : dt == MOE_F32;
-  JoinArgs j{p.partial, p.slot_elems, d.splits, M, p.N, p.add, p.ldadd, p.C, p.C, p.ldc, M};
-  if (VARK) {
-    j.c1 = reinterpret_cast<char*>(p.dwA);
-    j.c2 = reinterpret_cast<char*>(p.dwB);
-    j.ldc = static_cast<int64_t>(p.N) * (f32 ? 4 : 2);
-    j.split_row = p.split_row;
-  }
-  const int jgrid = static_cast<int>(std::min<int64_t>(8 * num_cus(), (p.slot_elems / 4 + 255) / 256));
-  MOE_TIMED("split_reduce", s);
-  if (f32) dense_join_kernel<float><<<jgrid, 256, 0, s>>>(j);
-  else dense_join_kernel<uint16_t><<<jgrid, 256, 0, s>>>(j);
-  MOE_LAUNCH_CHECK();
-  return MOE_OK;
-}
-
 #define MOE_TRY(...)                       \
   do {                                     \
     moe_status st_ = (__VA_ARGS__);        \
