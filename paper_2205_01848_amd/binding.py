@@ -487,7 +487,7 @@ def _need_scales(x_scale, src, k, R):
         _need(x_scale, R, "x_scale", _F32)
         return 0
     _need(src, R, "src", _I32)
-    _need(x_scale, 1, "x_scale", _F32)
+    _need(x_scale, 0, "x_scale", _F32)
     if k < 1:
         raise MoEError("k picks per token are needed with src")
     return x_scale.numel()

@@ -102,7 +102,7 @@ moe_status launch_i8(hipStream_t s, KernelI8 k, const FfnPlan& pl, char* ws, con
 }
 
 bool scales_ok(const float* x_scale, const int32_t* src, int T, int k) {
-  return x_scale && (!src || (T > 0 && k > 0));
+  return src ? T >= 0 && k > 0 && (x_scale || T == 0) : x_scale != nullptr;
 }
 
 // The product of one expert region's rows xq (K bytes each) with wq, wq3.
@@ -149,6 +149,7 @@ extern "C" moe_status moe_expert_matmul_i8(void* stream, moe_dtype dt, int E, in
   if (rows_alloc == 0) return MOE_OK;
   if (!xq || !scales_ok(x_scale, src, T, k) || !y || !aligned16(xq) || !aligned16(y)) return MOE_EINVAL;
   if (!workspace || workspace_bytes < pl.o_end_sched || !aligned16(workspace)) return MOE_EWORKSPACE;
+  if (src && T == 0) return MOE_OK;   // no tokens, so no rows
   pl.es = 1;
   pl.d = K;
   if (src) pl.rows_most = std::min<int64_t>(rows_alloc, static_cast<int64_t>(T) * k);
@@ -187,6 +188,7 @@ extern "C" moe_status moe_expert_ffn_fwd_i8(void* stream, moe_dtype dt, moe_act 
   if (rows_alloc == 0) return MOE_OK;
   if (!xq || !scales_ok(x_scale, src, T, k) || !y_disp || !aligned16(xq) || !aligned16(y_disp)) return MOE_EINVAL;
   if (!workspace || workspace_bytes < q.total || !aligned16(workspace)) return MOE_EWORKSPACE;
+  if (src && T == 0) return MOE_OK;   // no tokens, so no rows
   hipStream_t s = static_cast<hipStream_t>(stream);
   char* ws = static_cast<char*>(workspace);
   FfnPlan& pl = q.pl;

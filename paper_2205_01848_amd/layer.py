@@ -42,10 +42,37 @@ def rows_alloc_for(kind: str, T: int, k: int, E: int, num: int = 1, den: int = 1
     raise ValueError(kind)
 
 
+def quantize_rows(x):
+    """x [..., n] as int8 rows of quantized_width(n) bytes and float32 scales [...]
+    (moe_quantize_rows): the form the int8 products read weights and tokens in."""
+    n = x.shape[-1]
+    q = torch.empty(*x.shape[:-1], B.quantized_width(n), dtype=torch.int8, device=x.device)
+    scale = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+    B.moe_quantize_rows(x.reshape(-1, n), q, scale)
+    return q, scale
+
+
+class QuantizedExperts:
+    """Expert weights in 8-bit integers with a scale per output channel, laid out
+    once for MoELayer.forward_i8: w1, w3 [E, f, d] (w3 None unless SwiGLU),
+    w2 [E, d, f]."""
+
+    def __init__(self, w1, w3, w2):
+        self.E, self.f, self.d = w1.shape
+        self.w1, self.s1 = quantize_rows(w1)
+        self.w3, self.s3 = (None, None) if w3 is None else quantize_rows(w3)
+        self.w2, self.s2 = quantize_rows(w2)
+
+
 class MoELayer:
+    """shared_f > 0 adds a shared expert of that width: the dense gated block
+    (act shared_act) on every token, its output added to the routed experts',
+    given its weights as shared=(w1, w3, w2) in the calls."""
+
     def __init__(self, T: int, d: int, E: int, k: int, f: int, act: str,
                  dtype: torch.dtype, rows_alloc: int, backward: bool = False,
-                 gate: bool = True, device="cuda", row_align: int = ROW_ALIGN):
+                 gate: bool = True, device="cuda", row_align: int = ROW_ALIGN,
+                 shared_f: int = 0, shared_act: str = "swiglu"):
         self.T, self.d, self.E, self.k, self.f = T, d, E, k, f
         self.row_align = row_align
         self.act = B.ACTS[act]
@@ -92,7 +119,21 @@ class MoELayer:
                 self.dlogits = e(T, E, t=f32)
                 self.dw_g = e(E, d, t=f32)
                 self.ws_gate_bwd = B.workspace(B.moe_gate_bwd_workspace_bytes(T, d, E), self.dev)
-        # loss-side operators and caching: allocated on first use
+        # the shared expert: its saved planes H1, H3, A and float32 gradients
+        self.shared_f, self.shared_act = shared_f, B.ACTS[shared_act]
+        if shared_f:
+            sf = shared_f
+            need = B.moe_gated_ffn_fwd_workspace_bytes(dt, T, d, sf)
+            self.sh_save = None
+            if backward:
+                need = max(need, B.moe_gated_ffn_bwd_workspace_bytes(dt, T, d, sf))
+                self.sh_save = e(3, T, sf)
+                self.dsw1, self.dsw3 = e(sf, d, t=f32), e(sf, d, t=f32)
+                self.dsw2 = e(d, sf, t=f32)
+            self.ws_shared = B.workspace(need, self.dev)
+        # the experts in 8-bit integers, loss-side operators and caching:
+        # allocated on first use
+        self.xq = None
         self.balance_loss = self.dprob_coef = self.ws_balance = None
         self._balance_on = False
         self.spec_loss_value = self.ws_spec = None
@@ -141,6 +182,26 @@ class MoELayer:
     def combine(self, weights: Optional[torch.Tensor] = None):
         B.moe_combine(self.y_disp, self.dest_row, self.weights if weights is None else weights,
                       self.y)
+
+    # ---- shared expert ------------------------------------------------------------
+    def shared_fwd(self, x, shared):
+        """y += the shared expert's output, shared = (w1 [sf, d], w3 [sf, d], w2 [d, sf])."""
+        self._need_shared(shared)
+        B.moe_gated_ffn_fwd(self.shared_act, x, *shared, self.y, self.ws_shared, add=self.y,
+                            h_save=self.sh_save)
+
+    def shared_bwd(self, x, dy, shared):
+        """dx += the shared expert's part; its weight gradients go to dsw1, dsw3, dsw2."""
+        self._need_shared(shared)
+        B.moe_gated_ffn_bwd(self.shared_act, x, self.sh_save, *shared, dy, self.dx, self.dsw1,
+                            self.dsw3, self.dsw2, self.ws_shared, add=self.dx)
+
+    def _need_shared(self, shared):
+        if not self.shared_f:
+            raise ValueError("the layer was made without a shared expert (shared_f)")
+        if tuple(shared[0].shape) != (self.shared_f, self.d):
+            raise ValueError(f"shared w1 has shape {tuple(shared[0].shape)}, expected "
+                             f"{(self.shared_f, self.d)}")
 
     # ---- loss-side operators ----------------------------------------------------
     def balance(self, lam: float):
@@ -250,7 +311,7 @@ class MoELayer:
 
     def forward(self, x, w1, w3, w2, *, w_g=None, bias=None, renorm=0, ids=None, weights=None,
                 capacity=("dynamic", 1, 1), counts_from_batch=True, rows="fill",
-                balance: Optional[float] = None):
+                balance: Optional[float] = None, shared=None):
         """gate (or cached ids) -> [count ->] capacity -> dispatch -> FFN -> combine
         (one library call, which calls none of the step methods, unless the
         capacities or the rows come from elsewhere or a step is overridden).
@@ -260,7 +321,8 @@ class MoELayer:
         else the counts left in self.counts by the previous dispatch (a lagged
         capacity update); "policy" uses capacities a CapacityPolicy uploaded.
         balance = lambda adds the Eq. 3 balance term (self.balance_loss) and
-        its gradient to the gate backward."""
+        its gradient to the gate backward.  shared: the shared expert's weights
+        (w1, w3, w2), its output added to the combine's."""
         self._balance_on = False
         if ((ids is None) == (w_g is not None) and
                 self._fusable(x, w1, capacity, rows, counts_from_batch, ids, w_g)):
@@ -268,6 +330,8 @@ class MoELayer:
                         else weights, self.y, capacity=capacity, renorm=renorm, w_g=w_g, bias=bias)
             if balance is not None:
                 self.balance(balance)
+            if shared is not None:
+                self.shared_fwd(x, shared)
             return self.y
         if ids is None:
             self.gate(x, w_g, bias, renorm)
@@ -277,10 +341,56 @@ class MoELayer:
             self.balance(balance)
         self.ffn_fwd(w1, w3, w2, rows=rows)
         self.combine(weights)
+        if shared is not None:
+            self.shared_fwd(x, shared)
+        return self.y
+
+    def forward_i8(self, x, experts: QuantizedExperts, *, w_g=None, bias=None, renorm=0, ids=None,
+                   weights=None, capacity=("dynamic", 1, 1), shared=None):
+        """The forward for serving, with the routed experts in 8-bit integers:
+        gate (or cached ids) in the layer dtype -> quantise x, a scale per
+        token -> count, capacity, dispatch of the quantised rows (half the
+        bytes of bf16) -> int8 FFN -> combine [-> shared expert in the layer
+        dtype].  Arguments as for forward; no backward follows it."""
+        T, d, E, k, R = self.T, self.d, self.E, self.k, self.rows_alloc
+        if (experts.E, experts.f, experts.d) != (E, self.f, d):
+            raise ValueError(f"quantised experts of sizes {(experts.E, experts.f, experts.d)}, the "
+                             f"layer's are {(E, self.f, d)}")
+        if self.xq is None:
+            width = B.quantized_width(d)
+            new = lambda rows: torch.empty(rows, width, dtype=torch.int8, device=self.dev)
+            self.xq, self.xq_disp = new(T), new(max(R, 1))
+            self.xq_scale = torch.empty(T, dtype=torch.float32, device=self.dev)
+            dt = B.MOE_BF16 if self.dtype == torch.bfloat16 else B.MOE_F32
+            self.ws_i8 = B.workspace(B.moe_ffn_fwd_i8_workspace_bytes(dt, self.act, E, d, self.f, R),
+                                     self.dev)
+        self._balance_on = False
+        if ids is None:
+            self.gate(x, w_g, bias, renorm)
+            ids, weights = self.ids, self.weights
+        B.moe_quantize_rows(x, self.xq, self.xq_scale)
+        # the dispatch moves rows of 16-byte vectors: two int8 values ride as one bf16
+        rows, disp = self.xq.view(torch.bfloat16), self.xq_disp.view(torch.bfloat16)
+        kind, num, den = capacity
+        if kind == "policy":
+            B.moe_dispatch(rows, ids, E, self.capacity, self.offsets, R, self.counts, self.fill,
+                           self.dest_row, self.src, disp, self.status, self.ws_dispatch)
+        else:
+            B.moe_route(rows, ids, E, kind != "static", num, den, 0, R, self.capacity, self.offsets,
+                        self.counts, self.fill, self.dest_row, self.src, disp, self.status,
+                        self.ws_dispatch, row_align=self.row_align)
+        q = experts
+        B.moe_expert_ffn_fwd_i8(self.act, self.offsets, self.fill, self.xq_disp[:R], self.xq_scale,
+                                q.w1, q.s1, q.w3, q.s3, q.w2, q.s2, self.y_disp, self.ws_i8,
+                                src=self.src, k=k)
+        self.combine(weights)
+        if shared is not None:
+            self.shared_fwd(x, shared)
         return self.y
 
     def forward_cached(self, x, w1, w3, w2, *, cached, cache_out, unchanged, w_g, bias=None,
-                       renorm=0, capacity=("dynamic", 1, 1), gate_stream=None, rows="fill"):
+                       renorm=0, capacity=("dynamic", 1, 1), gate_stream=None, rows="fill",
+                       shared=None):
         """Forward with sample assignment caching on (Section 4.2): the expert
         batches are built from the cached picks while the gate runs on
         gate_stream; the combine waits for the gate and weighs the cached
@@ -316,15 +426,19 @@ class MoELayer:
             self.ffn_fwd(w1, w3, w2, rows=rows)
         main.wait_event(gate_done)
         self.combine(self.cached_weights)
+        if shared is not None:
+            self.shared_fwd(x, shared)
         return self.y
 
     def backward(self, x, dy, w1, w3, w2, *, w_g=None, renorm=0, ids=None, weights=None,
-                 rows="fill", target=None):
+                 rows="fill", target=None, shared=None):
         """combine_bwd (or, given target, the Eq. 2 specification loss in its
         place) -> gate backward -> FFN backward -> dispatch backward.  The
         gate backward needs only dweights, so it runs before the FFN
         backward, whose last product (dx_disp) the dispatch backward then
-        reads straight after it was written."""
+        reads straight after it was written.  shared: the shared expert's
+        weights; it takes the same dy (and needs one, also beside target, whose
+        loss has predictions of the routed experts alone)."""
         if target is not None:
             self.spec_loss(target, self.weights if weights is None else weights)
         else:
@@ -333,6 +447,8 @@ class MoELayer:
             self.gate_bwd(x, renorm, ids)
         self.ffn_bwd(w1, w3, w2, rows=rows)
         self.dispatch_bwd(w_g)
+        if shared is not None:
+            self.shared_bwd(x, dy, shared)
         return self.dx
 
 

@@ -83,7 +83,7 @@ def test_picks_instead_of_rows():
     passes_checks(B.moe_expert_matmul_i8, **dict(MATMUL, src=z(9, dt=i32), k=2, x_scale=z(3)))
     refuses("src holds", B.moe_expert_matmul_i8, **dict(MATMUL, src=z(8, dt=i32), k=2))
     refuses("k picks", B.moe_expert_matmul_i8, **dict(MATMUL, src=z(9, dt=i32), k=0))
-    refuses("x_scale holds", B.moe_expert_ffn_fwd_i8, **dict(FFN, src=z(9, dt=i32), k=2, x_scale=z(0)))
+    refuses("x_scale", B.moe_expert_ffn_fwd_i8, **dict(FFN, src=z(9, dt=i32), k=2, x_scale=None))
 
 
 def test_widths_and_optional_operands():
@@ -132,7 +132,7 @@ def test_c_quantize(change):
                                     dict(N=0), dict(N=12), dict(R=-1), dict(R=1 << 31), dict(offsets=None),
                                     dict(rows=None), dict(xq=None), dict(x_scale=None), dict(wq=None),
                                     dict(w_scale=None), dict(y=None), dict(xq=ODD), dict(wq=ODD), dict(y=ODD),
-                                    dict(src=ODD, T=0), dict(src=ODD, T=4, k=0)])
+                                    dict(src=ODD, T=-1), dict(src=ODD, T=4, k=0)])
 def test_c_matmul(change):
     assert _c("moe_expert_matmul_i8", **change) == EINVAL
 
@@ -142,7 +142,7 @@ def test_c_matmul(change):
                                     dict(rows=None), dict(xq=None), dict(x_scale=None), dict(w1=None),
                                     dict(s1=None), dict(w3=None), dict(s3=None), dict(w2=None), dict(s2=None),
                                     dict(y=None), dict(xq=ODD), dict(w1=ODD), dict(w3=ODD), dict(w2=ODD),
-                                    dict(y=ODD), dict(src=ODD, T=0), dict(src=ODD, T=4, k=0)])
+                                    dict(y=ODD), dict(src=ODD, T=-1), dict(src=ODD, T=4, k=0)])
 def test_c_ffn(change):
     assert _c("moe_expert_ffn_fwd_i8", **change) == EINVAL
 
