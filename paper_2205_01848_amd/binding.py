@@ -423,15 +423,41 @@ def moe_expert_ffn_bwd(act, offsets, rows, x_disp, h_save, w1, w3, w2, dy_disp, 
 # ---- 8-bit integer products and the dense gated block ------------------------
 # These check that their tensors share one device and run on that device's
 # current stream, whichever device is current.
-def _device_of(*tensors):
-    """The one device all the call's tensors live on."""
-    ts = [t for t in tensors if t is not None]
-    for t in ts:
-        if not t.is_cuda:
+def _device_of(*tensors) -> int:
+    """Index of the one device all the call's tensors live on."""
+    first = -1
+    for t in tensors:
+        if t is None:
+            continue
+        i = t.get_device()          # -1: not in device memory
+        if i < 0:
             raise MoEError("tensor must live in device memory")
-        if t.device != ts[0].device:
-            raise MoEError(f"tensors on {ts[0].device} and {t.device}: one device is needed")
-    return ts[0].device
+        if first < 0:
+            first = i
+        elif i != first:
+            raise MoEError(f"tensors on devices {first} and {i}: one device is needed")
+    return first
+
+
+class _Here:
+    """`with _Here(index) as stream`: on that device, with its current stream.
+    Where it is the current device (the usual case) torch's guard, which costs
+    as much as a small launch, is left out."""
+
+    __slots__ = ("index", "guard")
+
+    def __init__(self, index):
+        self.index = index
+        self.guard = None if index == torch.cuda.current_device() else torch.cuda.device(index)
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+        return torch.cuda.current_stream(self.index).cuda_stream
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
 
 
 def _rows(t: Optional[torch.Tensor], name, T, d, dtype, optional=False):
@@ -457,7 +483,7 @@ def _rows(t: Optional[torch.Tensor], name, T, d, dtype, optional=False):
 
 
 def _at(t: Optional[torch.Tensor]):
-    return None if t is None else ctypes.c_void_p(t.data_ptr())
+    return None if t is None else t.data_ptr()
 
 
 def quantized_width(n: int) -> int:
@@ -472,8 +498,8 @@ def moe_quantize_rows(x, q, scale):
     dt = _dt(x)
     _need(q, rows * quantized_width(n), "q", torch.int8)
     _need(scale, rows, "scale", _F32)
-    with torch.cuda.device(_device_of(x, q, scale)):
-        _check(lib().moe_quantize_rows(_stream(), dt, rows, n, _at(x), ld, _ptr(q), _ptr(scale)),
+    with _Here(_device_of(x, q, scale)) as stream:
+        _check(lib().moe_quantize_rows(stream, dt, rows, n, _at(x), ld, _ptr(q), _ptr(scale)),
                "moe_quantize_rows")
 
 
@@ -506,8 +532,8 @@ def moe_expert_matmul_i8(offsets, rows, xq, x_scale, wq, w_scale, y, ws, src=Non
     _need(w_scale, E * N, "w_scale", _F32)
     _need(y, R * N, "y")
     T = _need_scales(x_scale, src, k, R)
-    with torch.cuda.device(_device_of(offsets, rows, xq, x_scale, wq, w_scale, y, ws, src)):
-        _check(lib().moe_expert_matmul_i8(_stream(), dt, E, K, N, _ptr(offsets), _ptr(rows), R,
+    with _Here(_device_of(offsets, rows, xq, x_scale, wq, w_scale, y, ws, src)) as stream:
+        _check(lib().moe_expert_matmul_i8(stream, dt, E, K, N, _ptr(offsets), _ptr(rows), R,
                                           _ptr(xq), _ptr(x_scale), _ptr(src), T, k, _ptr(wq),
                                           _ptr(w_scale), _ptr(y), _ptr(ws), _nbytes(ws)),
                "moe_expert_matmul_i8")
@@ -536,10 +562,10 @@ def moe_expert_ffn_fwd_i8(act, offsets, rows, xq, x_scale, w1q, w1_scale, w3q, w
         _need(t, n, name, dtype, optional=opt)
     _need(y_disp, R * d, "y_disp")
     T = _need_scales(x_scale, src, k, R)
-    with torch.cuda.device(_device_of(offsets, rows, xq, x_scale, w1q, w1_scale, w3q, w3_scale, w2q,
-                                      w2_scale, y_disp, ws, src)):
+    with _Here(_device_of(offsets, rows, xq, x_scale, w1q, w1_scale, w3q, w3_scale, w2q,
+                                      w2_scale, y_disp, ws, src)) as stream:
         _check(lib().moe_expert_ffn_fwd_i8(
-            _stream(), dt, act, E, d, f, _ptr(offsets), _ptr(rows), R, _ptr(xq), _ptr(x_scale),
+            stream, dt, act, E, d, f, _ptr(offsets), _ptr(rows), R, _ptr(xq), _ptr(x_scale),
             _ptr(src), T, k, _ptr(w1q), _ptr(w1_scale), _ptr(w3q), _ptr(w3_scale), _ptr(w2q),
             _ptr(w2_scale), _ptr(y_disp), _ptr(ws), _nbytes(ws)), "moe_expert_ffn_fwd_i8")
 
@@ -563,8 +589,8 @@ def moe_gated_ffn_fwd(act, x, w1, w3, w2, y, ws, add=None, h_save=None):
         _need(w, f * d, name, dtype)
     if h_save is not None:
         _need(h_save, 3 * T * f, "h_save", dtype)
-    with torch.cuda.device(_device_of(x, w1, w3, w2, y, ws, add, h_save)):
-        _check(lib().moe_gated_ffn_fwd(_stream(), dt, act, T, d, f, _at(x), ldx, _ptr(w1),
+    with _Here(_device_of(x, w1, w3, w2, y, ws, add, h_save)) as stream:
+        _check(lib().moe_gated_ffn_fwd(stream, dt, act, T, d, f, _at(x), ldx, _ptr(w1),
                                        _ptr(w3), _ptr(w2), _at(add), ldadd, _ptr(h_save), _at(y),
                                        ldy, _ptr(ws), _nbytes(ws)), "moe_gated_ffn_fwd")
 
@@ -582,8 +608,8 @@ def moe_gated_ffn_bwd(act, x, h_save, w1, w3, w2, dy, dx, dw1, dw3, dw2, ws, add
         raise MoEError(f"dw1: a tensor of {dtype} or float32 is needed")
     for name, w in (("dw1", dw1), ("dw3", dw3), ("dw2", dw2)):
         _need(w, f * d, name, dw1.dtype)
-    with torch.cuda.device(_device_of(x, h_save, w1, w3, w2, dy, dx, dw1, dw3, dw2, ws, add)):
-        _check(lib().moe_gated_ffn_bwd(_stream(), dt, act, T, d, f, _at(x), ldx, _ptr(h_save),
+    with _Here(_device_of(x, h_save, w1, w3, w2, dy, dx, dw1, dw3, dw2, ws, add)) as stream:
+        _check(lib().moe_gated_ffn_bwd(stream, dt, act, T, d, f, _at(x), ldx, _ptr(h_save),
                                        _ptr(w1), _ptr(w3), _ptr(w2), _at(dy), lddy, _at(add),
                                        ldadd, _at(dx), lddx, _dt(dw1), _ptr(dw1), _ptr(dw3),
                                        _ptr(dw2), _ptr(ws), _nbytes(ws)), "moe_gated_ffn_bwd")

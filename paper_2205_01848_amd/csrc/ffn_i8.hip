@@ -212,7 +212,7 @@ extern "C" moe_status moe_expert_ffn_fwd_i8(void* stream, moe_dtype dt, moe_act 
   } else {
     MOE_TRY(launch_i8<M_I8_FWD1, P_FWD_H>(s, up, pl, ws, rows, p));
   }
-  MOE_TRY(quantize_launch(s, dt, rows_alloc, rows_alloc, f, a, f, aq, as, E, offsets, rows));
+  MOE_TRY(quantize_launch(s, dt, rows_alloc, f, a, f, aq, as, E, offsets, rows));
   return launch_i8<M_I8_STORE, P_FWD_Y>(
       s, down, pl, ws, rows, params_i8(pl, offsets, ws, kf, d, aq, {as, nullptr, 0, 0}, w2q, w2_scale, dt,
                                      y_disp));

@@ -18,7 +18,6 @@ namespace moe {
 namespace {
 
 constexpr int kQuantThreads = 256;
-constexpr int kHeld = 4;   // units of 8 values a thread keeps in registers
 
 template <typename T> struct Unit;   // 8 values
 template <> struct Unit<uint16_t> {
@@ -99,7 +98,7 @@ __device__ __forceinline__ uint2 quantize8(const Unit<T>& u, const RowScale& rs)
 // G threads take a row, in units of 8 values; the first kHeld G units stay in
 // registers between the two passes, a longer row's others are read again (from
 // the caches).  Rows are dealt round-robin.
-template <typename T, int G>
+template <typename T, int G, int kHeld>
 __global__ __launch_bounds__(kQuantThreads) void quantize_kernel(
     const T* __restrict__ x, int64_t ldx, int64_t rows, int n, int8_t* __restrict__ q,
     float* __restrict__ scale, int E, const int32_t* __restrict__ offsets,
@@ -170,33 +169,51 @@ __global__ __launch_bounds__(kQuantThreads) void quantize_kernel(
   }
 }
 
-template <typename T, int G>
-moe_status launch(hipStream_t s, int64_t rows, int64_t most, int n, const void* x, int64_t ldx,
-                  int8_t* q, float* scale, int E, const int32_t* offsets,
-                  const int32_t* region_rows) {
+struct QuantArgs {
+  int64_t rows;
+  int n;
+  const void* x;
+  int64_t ldx;
+  int8_t* q;
+  float* scale;
+  int E;
+  const int32_t *offsets, *region_rows;
+};
+
+template <typename T, int G, int kHeld>
+moe_status launch(hipStream_t s, const QuantArgs& a) {
   constexpr int kPer = kQuantThreads / G;
-  const int64_t need = (rows + kPer - 1) / kPer;
-  const int grid = static_cast<int>(std::min<int64_t>(need, 8 * num_cus()));
+  const int grid = static_cast<int>(std::min<int64_t>((a.rows + kPer - 1) / kPer, 16 * num_cus()));
   MOE_TIMED("quantize_rows", s);
-  quantize_kernel<T, G><<<grid, kQuantThreads, 0, s>>>(static_cast<const T*>(x), ldx, rows, n, q,
-                                                        scale, E, offsets, region_rows);
+  quantize_kernel<T, G, kHeld><<<grid, kQuantThreads, 0, s>>>(static_cast<const T*>(a.x), a.ldx, a.rows,
+                                                               a.n, a.q, a.scale, a.E, a.offsets,
+                                                               a.region_rows);
   MOE_LAUNCH_CHECK();
   return MOE_OK;
 }
 
+// A wavefront a row up to 2048 values, else a workgroup, and just the
+// registers that hold the row (up to 16384 values), as fewer of them leave room for
+// more rows in flight.
+template <typename T>
+moe_status launch_width(hipStream_t s, const QuantArgs& a) {
+  const int units = a.n / 8;
+  if (units <= kWave) return launch<T, kWave, 1>(s, a);
+  if (units <= 2 * kWave) return launch<T, kWave, 2>(s, a);
+  if (units <= 4 * kWave) return launch<T, kWave, 4>(s, a);
+  if (units <= 2 * kQuantThreads) return launch<T, kQuantThreads, 2>(s, a);
+  if (units <= 4 * kQuantThreads) return launch<T, kQuantThreads, 4>(s, a);
+  return launch<T, kQuantThreads, 8>(s, a);
+}
+
 }  // namespace
 
-moe_status quantize_launch(hipStream_t s, moe_dtype dt, int64_t rows, int64_t most, int n,
-                           const void* x, int64_t ldx, int8_t* q, float* scale, int E,
-                           const int32_t* offsets, const int32_t* region_rows) {
+moe_status quantize_launch(hipStream_t s, moe_dtype dt, int64_t rows, int n, const void* x,
+                           int64_t ldx, int8_t* q, float* scale, int E, const int32_t* offsets,
+                           const int32_t* region_rows) {
   if (rows == 0) return MOE_OK;
-  // a wavefront a row while the row fits its registers, else a workgroup
-  const bool wave = n <= 8 * kHeld * kWave;
-  if (dt == MOE_BF16)
-    return wave ? launch<uint16_t, kWave>(s, rows, most, n, x, ldx, q, scale, E, offsets, region_rows)
-                : launch<uint16_t, kQuantThreads>(s, rows, most, n, x, ldx, q, scale, E, offsets, region_rows);
-  return wave ? launch<float, kWave>(s, rows, most, n, x, ldx, q, scale, E, offsets, region_rows)
-              : launch<float, kQuantThreads>(s, rows, most, n, x, ldx, q, scale, E, offsets, region_rows);
+  const QuantArgs a = {rows, n, x, ldx, q, scale, E, offsets, region_rows};
+  return dt == MOE_BF16 ? launch_width<uint16_t>(s, a) : launch_width<float>(s, a);
 }
 
 }  // namespace moe
@@ -211,6 +228,6 @@ extern "C" moe_status moe_quantize_rows(void* stream, moe_dtype dt, int64_t rows
     return MOE_EINVAL;
   if (rows == 0) return MOE_OK;
   if (!x || !q || !scale || !aligned16(x) || !aligned16(q)) return MOE_EINVAL;
-  return quantize_launch(static_cast<hipStream_t>(stream), dt, rows, rows, n, x, ldx, q, scale, 0,
+  return quantize_launch(static_cast<hipStream_t>(stream), dt, rows, n, x, ldx, q, scale, 0,
                          nullptr, nullptr);
 }

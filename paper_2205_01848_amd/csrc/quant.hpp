@@ -13,9 +13,9 @@ inline int quantized_width(int n) { return (n + 15) / 16 * 16; }
 // Quantises rows of n values (x, ldx elements apart) to q (quantized_width(n)
 // apart) and scale.  offsets, region_rows (with E regions): only the rows
 // [offsets[e], offsets[e] + region_rows[e]) below rows; the others keep what
-// they held.  most: at most so many of the rows are quantised.
-moe_status quantize_launch(hipStream_t s, moe_dtype dt, int64_t rows, int64_t most, int n,
-                           const void* x, int64_t ldx, int8_t* q, float* scale, int E,
-                           const int32_t* offsets, const int32_t* region_rows);
+// they held.
+moe_status quantize_launch(hipStream_t s, moe_dtype dt, int64_t rows, int n, const void* x,
+                           int64_t ldx, int8_t* q, float* scale, int E, const int32_t* offsets,
+                           const int32_t* region_rows);
 
 }  // namespace moe
