@@ -24,6 +24,9 @@ struct GroupParams {
   int E;
   const int32_t* rows;
   int64_t rows_alloc;
+  // few rows, quantised in place: the values of a row (K counts the quantised
+  // bytes) and the rows that LDS holds at a time
+  int k_values = 0, quant_rows = 0;
 };
 
 // The rows of expert `lane`, clamped to its region and to rows_alloc, and

@@ -15,6 +15,7 @@
 #pragma once
 
 #include "deep.hpp"
+#include "quant.hpp"
 
 namespace moe {
 namespace {
@@ -40,15 +41,63 @@ template <int ES> __device__ __forceinline__ void few_mma(floatx4& c, const uint
   }
 }
 
-// RB blocks of 16 rows, W wavefronts.
-template <int MODE, int ES, int RB, int W>
+// LDS the quantised tokens of a product may take (with the partial sums of 16
+// wavefronts, 56 KB of the 64 a launch may ask for).
+constexpr int kFewQuant = 40960;
+// Bytes between those rows: 16 more than a row, so that a fragment's 16 rows
+// fall on different banks.
+inline __host__ __device__ int few_pitch(int kbytes) { return kbytes + 16; }
+
+// The rows of A (values of type T, K of them; K a multiple of 8, kb bytes once
+// quantised) as int8 in LDS, with their scales: what quantize_kernel does, for
+// the at most 16 rows of a workgroup.  Every thread takes units of 8
+// values, first for the rows' maxima, then (read again, from the caches) for the
+// integers.
+template <typename T, int THREADS>
+__device__ __forceinline__ void few_quantize(const char* a, int64_t lda, int rows, int K, int kb,
+                                             char* q, uint32_t* amax, float* scales) {
+  const int units = K / 8, all = kb / 8, pitch = few_pitch(kb);
+  auto at = [&](int row, int u) { return reinterpret_cast<const T*>(a + row * lda) + u * 8; };
+  if (threadIdx.x < 16) amax[threadIdx.x] = 0;
+  __syncthreads();
+  for (int i = threadIdx.x; i < rows * units; i += THREADS) {
+    const int row = i / units;
+    Unit<T> v;
+    v.load(at(row, i - row * units));
+    atomicMax(&amax[row], abs_bits_max<T>(v, 0));   // a maximum: any order gives it
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < rows * all; i += THREADS) {
+    const int row = i / all, u = i - row * all;
+    float sc;
+    const RowScale rs = row_scale(amax[row], sc);
+    uint2 b = make_uint2(0, 0);
+    if (u < units) {
+      Unit<T> v;
+      v.load(at(row, u));
+      b = quantize8<T>(v, rs);
+    }
+    *reinterpret_cast<uint2*>(q + row * pitch + u * 8) = b;
+    if (u == 0) scales[row] = sc;
+  }
+  __syncthreads();
+}
+
+// RB blocks of 16 rows, W wavefronts.  QUANT (int8, RB = 1): A holds values of
+// the layer dtype, which every workgroup quantises for itself while its first
+// weights are on their way.
+template <int MODE, int ES, int RB, int W, bool QUANT = false>
 __global__ __launch_bounds__(64 * W) void ffn_few_rows_kernel(const GroupParams fp) {
   constexpr bool GATED = is_gated(MODE), I8 = ES == 1;
   constexpr int NB = GATED ? 2 : 1;                     // weight matrices
   constexpr int D = 2;                                 // steps in flight per wavefront
   using Acc = FewAcc<ES>;
   static_assert(W >= RB, "a wavefront finishes each block of rows");
+  static_assert(!QUANT || (I8 && RB == 1 && !GATED), "quantised in place: one int8 product");
   __shared__ Acc part[W][RB * NB][64];
+  __shared__ uint32_t amax[QUANT ? 16 : 1];
+  __shared__ float scales[QUANT ? 16 : 1];
+  extern __shared__ __attribute__((aligned(16))) char quantised[];   // QUANT: kFewQuant at most
   const GemmParams& p = fp.p;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
@@ -82,7 +131,9 @@ __global__ __launch_bounds__(64 * W) void ffn_few_rows_kernel(const GroupParams 
     const __amdgpu_buffer_rsrc_t rb[2] = {tile_rsrc(b1), tile_rsrc(b2)};
     const uint32_t ob = static_cast<uint32_t>(c16 * static_cast<int>(p.ldb) + G * 16) |
                         bad(n0 + c16 >= p.N);
-    for (int r0 = 0; r0 < m; r0 += 16 * RB) {
+    // rows at a time (as many as LDS was asked for, where they are quantised)
+    const int block = QUANT ? min(16, fp.quant_rows) : 16 * RB;
+    for (int r0 = 0; r0 < m; r0 += block) {
       const __amdgpu_buffer_rsrc_t ra = tile_rsrc(p.A + (first + r0) * p.lda);
       uint32_t oa[RB];
 #pragma unroll
@@ -109,7 +160,8 @@ __global__ __launch_bounds__(64 * W) void ffn_few_rows_kernel(const GroupParams 
             fb[d][j][h] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rb[j], ob | kbad, soff, 0));
 #pragma unroll
           for (int i = 0; i < RB; ++i)
-            fa[d][i][h] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(ra, oa[i] | kbad, soff, 0));
+            if constexpr (!QUANT)
+              fa[d][i][h] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(ra, oa[i] | kbad, soff, 0));
         }
       };
       // (the scheduling barriers keep the ring in order: a step's products wait
@@ -119,9 +171,26 @@ __global__ __launch_bounds__(64 * W) void ffn_few_rows_kernel(const GroupParams 
         load(d, wave + d * W);
         __builtin_amdgcn_sched_barrier(0);
       }
+      if constexpr (QUANT) {
+        const int rows = min(block, m - r0);
+        const char* a = p.A + (first + r0) * p.lda;
+        if (p.out_f32) few_quantize<float, 64 * W>(a, p.lda, rows, fp.k_values, kb, quantised, amax, scales);
+        else few_quantize<uint16_t, 64 * W>(a, p.lda, rows, fp.k_values, kb, quantised, amax, scales);
+      }
+      // this lane's 16 bytes of the quantised rows at half h of K step s, zeros outside
+      auto quant_frag = [&](int s, int h) {
+        const int kt = s + turn >= steps ? s + turn - steps : s + turn, o = kt * kRowBytes + h * 64 + G * 16;
+        const bool ok = s < steps && o < kb && c16 < block && r0 + c16 < m;
+        const uint4 v = *reinterpret_cast<const uint4*>(quantised + (ok ? c16 * few_pitch(kb) + o : 0));
+        return ok ? v : make_uint4(0, 0, 0, 0);
+      };
       for (int kt = wave; kt < steps; kt += D * W) {
 #pragma unroll
         for (int d = 0; d < D; ++d) {
+          if constexpr (QUANT) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) fa[d][0][h] = quant_frag(kt + d * W, h);
+          }
 #pragma unroll
           for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -160,11 +229,11 @@ __global__ __launch_bounds__(64 * W) void ffn_few_rows_kernel(const GroupParams 
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
             const int lr = r0 + 16 * wave + 4 * G + q;
-            if (lr >= m) continue;
+            if (lr >= m || (QUANT && lr >= r0 + block)) continue;
             const int64_t row = first + lr;
             float v = static_cast<float>(sum[0][q]), v3 = GATED ? static_cast<float>(sum[NB - 1][q]) : 0.f;
             if constexpr (I8) {
-              const float as = row_scale_at(p.a_scale, row);
+              const float as = QUANT ? scales[lr - r0] : row_scale_at(p.a_scale, row);
               v = v * as * s1;
               v3 = v3 * as * s3;
             }
@@ -218,20 +287,36 @@ inline int few_waves(int64_t items, int steps) {
 
 // Launches a product of few rows: most_rows rows in one expert at the most,
 // most_groups experts with rows.
+// quantise: A holds values of the layer dtype.  That saves a launch (32 experts of
+// 1024 -> 2048, 16 rows: 31.8 -> 28.6 us a call) while the rows are short; two
+// passes over a long one in every workgroup cost more (2 rows of 14336 values: 67.5
+// -> 70.3 us).
+inline bool few_fits_quant(int64_t most_rows, int kbytes) {
+  return kbytes <= 8192 && most_rows <= 16 && most_rows * few_pitch(kbytes) <= kFewQuant;
+}
 template <int MODE, int ES>
 moe_status launch_few(hipStream_t s, const char* name, const GroupParams& fp, int64_t most_rows,
-                      int most_groups) {
+                      int most_groups, bool quantise = false) {
   const int64_t items = static_cast<int64_t>(most_groups) * cdiv(fp.p.N, kFewCols);
   const int steps = cdiv(static_cast<int64_t>(fp.p.K) * ES, kRowBytes), w = few_waves(items, steps);
   const int grid = static_cast<int>(std::min<int64_t>(items, 16 * num_cus()));
   MOE_TIMED(name, s);
   auto go = [&](auto rb_c, auto w_c) {
     constexpr int RB = decltype(rb_c)::value, W = decltype(w_c)::value;
+    if constexpr (MODE == M_I8_STORE && RB == 1) {
+      if (quantise) {
+        ffn_few_rows_kernel<MODE, ES, RB, W, true>
+            <<<grid, 64 * W, most_rows * few_pitch(fp.p.K), s>>>(fp);
+        return;
+      }
+    }
     ffn_few_rows_kernel<MODE, ES, RB, W><<<grid, 64 * W, 0, s>>>(fp);
   };
   auto rows = [&](auto w_c) {
-    if (most_rows <= 16) go(std::integral_constant<int, 1>{}, w_c);
-    else go(std::integral_constant<int, 2>{}, w_c);
+    if constexpr (ES == 4) {   // only the fp32 block takes it for more than 16 rows
+      if (most_rows > 16) return go(std::integral_constant<int, 2>{}, w_c);
+    }
+    go(std::integral_constant<int, 1>{}, w_c);
   };
   if (w == 16) rows(std::integral_constant<int, 16>{});
   else if (w == 8) rows(std::integral_constant<int, 8>{});

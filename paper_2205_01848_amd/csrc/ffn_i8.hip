@@ -212,6 +212,15 @@ extern "C" moe_status moe_expert_ffn_fwd_i8(void* stream, moe_dtype dt, moe_act 
   } else {
     MOE_TRY(launch_i8<M_I8_FWD1, P_FWD_H>(s, up, pl, ws, rows, p));
   }
+  if (down == I8_FEW && few_fits_quant(pl.rows_most, kf)) {
+    // A straight into the second product, quantised there
+    GroupParams gp{params_i8(pl, offsets, ws, kf, d, nullptr, {}, w2q, w2_scale, dt, y_disp), E, rows,
+                   rows_alloc, f, static_cast<int>(pl.rows_most)};
+    gp.p.A = a;
+    gp.p.lda = f * static_cast<int64_t>(esize(dt));
+    return launch_few<M_I8_STORE, 1>(s, pass_name(P_FWD_Y), gp, pl.rows_most,
+                                     static_cast<int>(std::min<int64_t>(E, pl.rows_most)), true);
+  }
   MOE_TRY(quantize_launch(s, dt, rows_alloc, f, a, f, aq, as, E, offsets, rows));
   return launch_i8<M_I8_STORE, P_FWD_Y>(
       s, down, pl, ws, rows, params_i8(pl, offsets, ws, kf, d, aq, {as, nullptr, 0, 0}, w2q, w2_scale, dt,

@@ -214,3 +214,42 @@ def test_empty_calls():
     B.moe_expert_ffn_fwd_i8(B.MOE_RELU, i32(0, 0), i32(0), q8(0, 16), f(0), q8(1, 8, 16), f(1, 8), None,
                             None, q8(1, 16, 16), f(1, 16), f(0, 16), ws)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("act", ["swiglu", "relu"])
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("T,k,rows,d,f", [(1, 2, [1, 0, 1], 136, 200),        # decoding: quantised in the second product
+                                          (8, 2, [9, 7, 0], 64, 1000),
+                                          (3, 1, [0, 0, 3], 72, 4104),
+                                          (1, 2, [20, 1, 16], 72, 264),       # padded regions: more rows than picks
+                                          (2, 1, [1, 1, 0], 16, 24576)])      # too wide for LDS
+def test_ffn_few_rows(T, k, rows, d, f, dt, act):
+    """Decoding, with scales by token: rows[e] need not be the picks alone."""
+    rng = np.random.default_rng(T * d + f)
+    rows, off, R = _layout(rows, [2, 0, 1])
+    x = _d(rng.standard_normal((T, d)).astype(np.float32)).to(DT[dt])
+    xq, xs = torch.empty(T, B.quantized_width(d), dtype=torch.int8, device=dev()), torch.empty(T, device=dev())
+    B.moe_quantize_rows(x, xq, xs)
+    src = rng.integers(0, T * k, R).astype(np.int32)
+    w1, s1 = _quantised(rng, d, 3, f)
+    w3, s3 = _quantised(rng, d, 3, f) if act == "swiglu" else (None, None)
+    w2, s2 = _quantised(rng, f, 3, d)
+    y = torch.full((R, d), 3.0, dtype=DT[dt], device=dev())
+    code = B.MOE_BF16 if dt == "bf16" else B.MOE_F32
+    ws = B.workspace(B.moe_ffn_fwd_i8_workspace_bytes(code, B.ACTS[act], 3, d, f, R), dev())
+    opt = lambda a: None if a is None else _d(a)
+    xd = xq[_d(src // k).long()]
+    B.moe_expert_ffn_fwd_i8(B.ACTS[act], _d(off.astype(np.int32)), _d(rows.astype(np.int32)), xd, xs, _d(w1),
+                            _d(s1), opt(w3), opt(s3), _d(w2), _d(s2), y, ws, src=_d(src), k=k)
+    got, used = to_np(y), np.zeros(R, bool)
+    q, sc = xd.cpu().numpy()[:, :d], xs.cpu().numpy()[src // k]
+    for e in range(3):
+        r = slice(int(off[e]), int(off[e] + rows[e]))
+        used[r] = True
+        if rows[e] == 0:
+            continue
+        part = lambda a, n: None if a is None else a[e][..., :n]
+        ref, slack_e = O.ffn_i8_bounds(q[r], sc[r], part(w1, d), s1[e], part(w3, d),
+                                       None if s3 is None else s3[e], part(w2, f), s2[e], act, dt)
+        assert (np.abs(got[r] - ref) <= slack_e * 1.001 + np.abs(ref) * (4 * U32 + ROUND[dt]) + 1e-30).all()
+    assert (got[~used] == 3).all()
