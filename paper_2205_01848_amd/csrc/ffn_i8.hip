@@ -9,6 +9,8 @@
 // instead of 64, at the same number of matrix instructions, so the same loop
 // does twice the products per second, and the same bytes.
 
+#include <cmath>
+
 #include "dense.hpp"
 #include "few_rows.hpp"
 #include "quant.hpp"
@@ -36,8 +38,10 @@ bool plan_i8(moe_dtype dt, moe_act act, int E, int d, int f, int64_t rows_alloc,
 }
 
 // The kernel of one product: the one for few rows, deep tiles of 32, 64 or 128
-// rows, or the tiles of gemm.hpp with their schedule.
-enum KernelI8 { I8_FEW, I8_DEEP32, I8_DEEP64, I8_DEEP128, I8_TILES };
+// rows, or, with a schedule, the tiles of gemm.hpp (128 columns and up to 192
+// rows, or 256 x 256).
+enum KernelI8 { I8_FEW, I8_DEEP32, I8_DEEP64, I8_DEEP128, I8_MID, I8_BIG };
+bool scheduled(KernelI8 k) { return k >= I8_MID; }
 
 // The host knows the rows at most and their mean over the experts, not the
 // loads: it compares the estimated times for experts of the mean, half a tile
@@ -50,9 +54,10 @@ enum KernelI8 { I8_FEW, I8_DEEP32, I8_DEEP64, I8_DEEP128, I8_TILES };
 // 14336 of 8 experts, 8 rows 176 / 182 / 192 / 197 / 231, 256 rows 685 / 324 / 282
 // / 295 / 326, 1024 rows 2224 / 625 / 473 / 441 / 381; 64 experts 2048, 1408,
 // 512 rows 132 / 90 / 91 / 101 / 103; one product 14336 -> 4096, 16 rows 18 / 28
-// / 38 / 53 / 58.
+// / 38 / 53 / 58.  The two tiles, us, 256 x 256 / 128 columns: 8192 rows on 8
+// experts, 4096 -> 2 x 14336 897 / 1000, 14336 -> 4096 506 / 468.
 KernelI8 kernel_i8(const FfnPlan& pl, int K, int N, bool gated) {
-  if (g_tile_mode != 0) return I8_TILES;
+  if (g_tile_mode != 0) return g_tile_mode == 1 ? I8_BIG : I8_MID;
   const int groups = static_cast<int>(std::min<int64_t>(pl.E, pl.rows_most)), cus = persistent_grid();
   const double mean = std::max(1., static_cast<double>(pl.rows_most) / pl.E);
   const int steps = cdiv(K, kRowBytes);
@@ -64,32 +69,39 @@ KernelI8 kernel_i8(const FfnPlan& pl, int K, int N, bool gated) {
     const int places = per_cu * cus;
     return n > places ? n / places + 0.25 : per_cu == 2 && 2 * n <= places ? half / 100. : 1.;
   };
-  auto tile = [&](DenseKernel k, int h, int unit, int cols, int per_cu) {
+  auto tile = [&](DenseKernel k, int h, int unit, int cols, int per_cu, int slower) {
     const TileTime t = tile_time(false, k, h, D_KC);
-    return rounds(tiles(unit) * cdiv(N, gated ? cols / 2 : cols), per_cu, t.half) *
-           (static_cast<double>(t.step) * steps + t.fix);
+    const double n = tiles(unit) * cdiv(N, gated ? cols / 2 : cols);
+    // the tiles of gemm.hpp are for many rows: whole rounds
+    const double r = k != K_DEEP && n > per_cu * cus ? std::ceil(n / (per_cu * cus)) : rounds(n, per_cu, t.half);
+    return r * (static_cast<double>(t.step) * slower / 100 * steps + t.fix);
   };
-  KernelI8 best = I8_TILES;
-  double t_best = tile(K_BIG, 0, BM, BN, 1);
-  for (int h = 1; h <= kMidMaxH; ++h)
-    t_best = std::min(t_best, tile(K_MID, h, kMidUnit * h, kMidN, 2));
-  t_best = std::max(t_best, 1.15 * read + 3000) + 7000;   // and the schedule's launch
+  // the int8 matrix instructions draw more power than the bf16 ones: a step of
+  // the large tiles takes 7 to 10 % longer
+  const double big = tile(K_BIG, 0, BM, BN, 1, 107);
+  double mid = 0;
+  for (int h = 1; h <= kMidMaxH; ++h) {
+    const double t = tile(K_MID, h, kMidUnit * h, kMidN, 2, 110);
+    if (h == 1 || t < mid) mid = t;
+  }
+  KernelI8 best = big <= mid ? I8_BIG : I8_MID;
+  double t_best = std::max(std::min(big, mid), 1.15 * read + 3000) + 7000;   // and the schedule's launch
   auto take = [&](KernelI8 k, double t) {
     if (t < t_best) { t_best = t; best = k; }
   };
   for (int h = 1; h <= 4; h *= 2)
     take(h == 1 ? I8_DEEP32 : h == 2 ? I8_DEEP64 : I8_DEEP128,
-         std::max(tile(K_DEEP, h, kMidUnit * h, kMidN, h <= 2 ? 2 : 1),
+         std::max(tile(K_DEEP, h, kMidUnit * h, kMidN, h <= 2 ? 2 : 1, 100),
                   read * (0.9 + 0.1 * tiles(kMidUnit * h) / groups) + 3000));
   if (pl.rows_most <= 16) take(I8_FEW, read + 2500);
   return best;
 }
 
-// One product by kernel k.  Only the tiles of gemm.hpp need the schedule.
+// One product by kernel k.
 template <int MODE, int PASS>
 moe_status launch_i8(hipStream_t s, KernelI8 k, const FfnPlan& pl, char* ws, const int32_t* rows,
                      const GemmParams& p) {
-  if (k == I8_TILES) return launch_gemm<MODE, PASS>(s, MOE_BF16, pl, ws, p);
+  if (scheduled(k)) return launch_gemm<MODE, PASS>(s, MOE_BF16, pl, ws, p, k == I8_MID);
   GroupParams gp{p, pl.E, rows, pl.rows_alloc};
   const int groups = static_cast<int>(std::min<int64_t>(pl.E, pl.rows_most));
   if (k == I8_FEW) return launch_few<MODE, 1>(s, pass_name(PASS), gp, pl.rows_most, groups);
@@ -157,7 +169,7 @@ extern "C" moe_status moe_expert_matmul_i8(void* stream, moe_dtype dt, int E, in
   char* ws = static_cast<char*>(workspace);
   const StepCost c = step16(K, K, false);
   const KernelI8 kernel = kernel_i8(pl, K, N, false);
-  if (kernel == I8_TILES)
+  if (scheduled(kernel))
     MOE_TRY(launch_schedule(s, sched_args(pl, cdiv(N, kMidN), cdiv(N, kMidN), K, c, c, ws), offsets,
                             rows));
   return launch_i8<M_I8_STORE, P_FWD_Y>(
@@ -195,7 +207,7 @@ extern "C" moe_status moe_expert_ffn_fwd_i8(void* stream, moe_dtype dt, moe_act 
   if (src) pl.rows_most = std::min<int64_t>(rows_alloc, static_cast<int64_t>(T) * k);
   const int kd = quantized_width(d), kf = quantized_width(f);
   const KernelI8 up = kernel_i8(pl, kd, f, sw), down = kernel_i8(pl, kf, d, false);
-  if (up == I8_TILES || down == I8_TILES)
+  if (scheduled(up) || scheduled(down))
     MOE_TRY(launch_schedule(s, sched_args(pl, cdiv(f, sw ? kMidN / 2 : kMidN), cdiv(d, kMidN), kf,
                                           step16(kd, kd, false), step16(kf, kf, false), ws),
                             offsets, rows));

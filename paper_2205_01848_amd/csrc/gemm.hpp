@@ -1996,9 +1996,7 @@ bool use_mid_tiles(const FfnPlan& pl, moe_dtype dt, bool vark, bool gated, bool 
     const int64_t mid = static_cast<int64_t>(pl.E) * cdiv(p.M_out, kMidDwH * kMidUnit) * cdiv(p.N, kMidN);
     return 13 * ((mid + 2 * G - 1) / (2 * G)) < 20 * ((big + G - 1) / G);
   }
-  // a K step is 128 bytes of a row: the rule counts bf16 values
-  const int k16 = pl.es == 1 ? cdiv(p.K, 2) : p.K;
-  return mid_pays({pl.E, pl.rows_alloc, pl.rows_most, p.N, k16, gated, act, b_km, p.lda, p.ldb}, G);
+  return mid_pays({pl.E, pl.rows_alloc, pl.rows_most, p.N, p.K, gated, act, b_km, p.lda, p.ldb}, G);
 }
 
 // dX with a transposed copy of [W1; W3] (moe_set_dx_weight_copy, g_wt_mode: 0
@@ -2022,12 +2020,13 @@ const char* pass_name(int pass) {
 }
 
 // Launches one product; sets the tile counts along N (and M for the weight
-// gradients) for the kernel it picks.
+// gradients) for the kernel it picks (int8: for the one the caller picked).
 template <int MODE, int PASS>
-moe_status launch_gemm(hipStream_t s, moe_dtype dt, const FfnPlan& pl, char* ws, GemmParams p) {
+moe_status launch_gemm(hipStream_t s, moe_dtype dt, const FfnPlan& pl, char* ws, GemmParams p,
+                       bool mid_i8 = false) {
   constexpr bool VARK = is_dw(MODE), GATED = is_gated(MODE);
   constexpr bool ACTIVE = MODE != M_STORE && MODE != M_ADD_STORE && MODE != M_I8_STORE && !VARK;
-  const bool mid = use_mid_tiles(pl, dt, VARK, GATED, ACTIVE, b_layout(PASS) == L_KM, p);
+  const bool mid = is_i8(MODE) ? mid_i8 : use_mid_tiles(pl, dt, VARK, GATED, ACTIVE, b_layout(PASS) == L_KM, p);
   const int tn = mid ? kMidN : BN;
   p.ntiles = cdiv(p.N, GATED ? tn / 2 : tn);
   p.dw_h = kMidDwH;
