@@ -170,36 +170,7 @@ __device__ __forceinline__ void mainloop_deep(const TileOps& op, char* const (&s
         for (int j = 0; j < 4; ++j) mma16<ES>(acc[i][j], fa[h][i], fb[h][j]);
   };
 
-#pragma unroll
-  for (int s = 0; s < NS - 1; ++s) load(s, sa[s], sb[s]);
-  auto step = [&](int kt, auto slot) {
-    constexpr int S = decltype(slot)::value, T = (S + NS - 1) % NS;
-    // stage kt has landed when only the NS - 2 stages after it may be pending;
-    // past the barrier that holds for every wave's part of it, and every wave
-    // has read stage kt - 1, whose place step kt + NS - 1 takes over
-    __builtin_amdgcn_s_waitcnt(wait_vm_lgkm0((NS - 2) * (RB + 4)));
-    __builtin_amdgcn_s_barrier();
-    __builtin_amdgcn_sched_barrier(0);
-    load(kt + NS - 1, sa[T], sb[T]);
-    compute(sa[S], sb[S]);
-    __builtin_amdgcn_sched_barrier(0);
-  };
-  using std::integral_constant;
-  // whole groups without a branch between the steps: the compiler then knows
-  // which loads are pending at each read and adds no wait of its own
-  int k0 = 0;
-  for (; k0 + NS <= nk; k0 += NS) {
-    step(k0, integral_constant<int, 0>{});
-    step(k0 + 1, integral_constant<int, 1>{});
-    step(k0 + 2, integral_constant<int, 2>{});
-    if constexpr (NS > 3) step(k0 + 3, integral_constant<int, 3>{});
-  }
-  if (k0 < nk) step(k0, integral_constant<int, 0>{});
-  if (k0 + 1 < nk) step(k0 + 1, integral_constant<int, 1>{});
-  if constexpr (NS > 3)
-    if (k0 + 2 < nk) step(k0 + 2, integral_constant<int, 2>{});
-  __builtin_amdgcn_s_waitcnt(0x0070);
-  __builtin_amdgcn_s_barrier();   // every load landed, every read done: stages are free
+  ring_steps<NS, RB + 4>(nk, sa, sb, load, compute);
 }
 
 template <int MODE, int PASS, int RB, int NS>
@@ -265,16 +236,62 @@ __global__ __launch_bounds__(kThreads16, RB <= 2 ? 2 : 1) void ffn_gemm16_deep_k
   }
 }
 
+// The same for fp32 (dense products): K steps of 32, tiles and fragments of the
+// two-stage fp32 kernel.  Its matrix instructions keep a step of a full CU busy (96 %
+// of their peak in a product of whole rounds), so it gains a little where a CU has one
+// workgroup (777 tokens, 1384 -> 512: Y 23.0 -> 20.6 us, dW2 24.8 -> 21.3).
+template <int MODE, int PASS, int RB, int NS>
+__global__ __launch_bounds__(kThreads16, RB <= 2 ? 2 : 1) void ffn_gemm_f32_deep_kernel(const GemmParams p) {
+  constexpr bool GATED = is_gated(MODE), VARK = is_dw(MODE);
+  constexpr int kA = 32 * RB * kRowBytes, kB = kMidN * kRowBytes, NB = GATED ? (RB + 1) / 2 : RB;
+  __shared__ __attribute__((aligned(16))) char a0[kA], b0[kB], a1[kA], b1[kB], a2[kA], b2[kB];
+  __shared__ __attribute__((aligned(16))) char a3[NS > 3 ? kA : 16], b3[NS > 3 ? kB : 16];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
+  const int n_items = dense_items<MODE>(p);
+  for (int round = 0;; ++round) {
+    const int L = round_item(round, n_items);
+    if (L < 0) break;
+    MidTile t;
+    int mt, nt;
+    const int si = dense_tile<MODE>(p, L, mt, nt);
+    t.g = 0;
+    t.h = RB;
+    t.row0 = mt * 32 * RB;
+    t.m_valid = min(32 * RB, (VARK ? p.M_out : p.dense.T) - t.row0);
+    t.n0 = nt * (GATED ? kMidN / 2 : kMidN);
+    t.slot = p.dense.splits > 1 ? si : -1;
+    t.op = dense_ops<MODE, PASS, 4>(p, t.row0, t.m_valid, t.n0, kMidN, si);
+    AccF32<NB> c1, c3;
+    if constexpr (NS == 3) {
+      char *const sa[3] = {a0, a1, a2}, *const sb[3] = {b0, b1, b2};
+      mainloop_f32<RB, PASS, GATED, NB, NS>(t.op, sa, sb, c1, c3);
+    } else {
+      char *const sa[4] = {a0, a1, a2, a3}, *const sb[4] = {b0, b1, b2, b3};
+      mainloop_f32<RB, PASS, GATED, NB, NS>(t.op, sa, sb, c1, c3);
+    }
+    epilogue_f32<MODE, RB, NB>(p, t, c1, c3, lane, wave);
+  }
+}
+
 // RB and NS of the three tiles, workgroups per CU.
 template <int RB> constexpr int kDeepStages = RB == 2 ? 3 : 4;
 template <int RB> constexpr int kDeepPerCu = RB <= 2 ? 2 : 1;
 
 template <int MODE, int PASS, int RB>
-moe_status launch_deep(hipStream_t s, const GroupParams& gp, int64_t most_items) {
+moe_status launch_deep(hipStream_t s, moe_dtype dt, const GroupParams& gp, int64_t most_items) {
   const int64_t full = kDeepPerCu<RB> * static_cast<int64_t>(persistent_grid());
   const int grid = static_cast<int>(std::min(full, (most_items + kXcds - 1) / kXcds * kXcds));
   MOE_TIMED(pass_name(PASS), s);
-  ffn_gemm16_deep_kernel<MODE, PASS, RB, kDeepStages<RB>><<<grid, kThreads16, 0, s>>>(gp);
+  if constexpr (is_dense(MODE) && PASS != P_BWD_DX_T) {
+    if (dt == MOE_F32) {
+      ffn_gemm_f32_deep_kernel<MODE, PASS, RB, kDeepStages<RB>><<<grid, kThreads16, 0, s>>>(gp.p);
+      MOE_LAUNCH_CHECK();
+      return MOE_OK;
+    }
+  }
+  if constexpr (!is_dw(MODE) || RB == 4)
+    ffn_gemm16_deep_kernel<MODE, PASS, RB, kDeepStages<RB>><<<grid, kThreads16, 0, s>>>(gp);
   MOE_LAUNCH_CHECK();
   return MOE_OK;
 }

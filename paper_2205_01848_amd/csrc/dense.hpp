@@ -18,11 +18,12 @@ struct DensePlan {
 // Time of a round of tiles on all places of the persistent grid: `step` ns per K
 // step (64 bf16 or 32 fp32 values) and `fix` ns of launch, prologue and
 // epilogue; a last round that leaves one of the two places of every CU empty takes
-// `half` percent of that.  Fitted on 10,388 bf16 and 3690 fp32 measurements of
+// `half` percent of that.  Fitted on 10,388 bf16 and 6165 fp32 measurements of
 // the block's six products (32 to 4096 tokens, d from 512 to 4096, f from 1384 to
-// 14336, every kernel, height and 1 to 8 K ranges): residual 8 to 18 % a product;
-// the plan's choice takes 1.6 % more than the best measured one on average (of
-// 168 bf16 products, 79 on the mid kernel, 69 deep, 20 on 256x256 tiles).
+// 14336, every kernel, height and 1 to 8 K ranges): residual 3 to 19 % a product;
+// the plan's choice takes 1.6 % (bf16) and 2.1 % (fp32) more than the best
+// measured one on average (of 168 bf16 products, 79 on the mid kernel, 69 deep,
+// 20 on 256x256 tiles).
 // Examples, us: 1021 tokens, 5632 -> 2048, 64-row tiles two-stage / deep 58 /
 // 34; 2048 tokens, 2816 -> 1024 26 / 20; 32 tokens, 28672 -> 4096, whole K / six
 // ranges 173 / 50; 4096 tokens, 4096 -> 2 x 14336, 256x256 / mid 677 / 832.
@@ -39,6 +40,11 @@ inline TileTime tile_time(bool f32, DenseKernel k, int h, DenseClass c) {
     static const TileTime dw[] = {{1070, 4100, 90}, {1810, 7000, 75}, {}, {3390, 12500, 73}};
     static const TileTime gated[] = {{1825, 8500, 59}, {1875, 9400, 61}, {3570, 16300, 57},
                                      {3635, 16300, 58}, {5075, 20000, 59}, {5665, 20000, 59}};
+    static const TileTime deep[4][4] = {{{925, 5900, 63}, {1775, 8700, 57}, {}, {1910, 9100, 100}},
+                                        {{1225, 8800, 62}, {2060, 13000, 58}, {}, {2050, 13400, 100}},
+                                        {{1025, 4300, 80}, {1800, 6900, 71}, {}, {1940, 9300, 100}},
+                                        {{1770, 7600, 58}, {1775, 9500, 57}, {}, {1915, 9100, 100}}};
+    if (k == K_DEEP) return deep[c][h - 1];
     return (c == D_KC ? kc : c == D_KM ? km : c == D_DW ? dw : gated)[h - 1];
   }
   if (c == D_DW) return k == K_BIG ? TileTime{1390, 21000, 100} : k == K_MID ? TileTime{800, 10000, 55} : TileTime{600, 7500, 100};
@@ -104,7 +110,7 @@ DensePlan dense_plan(moe_dtype dt, int M, int N, int K, int64_t lda, int64_t ldb
       const int n = cdiv(units, h);
       take(K_MID, VARK ? h : cdiv(units, n), n, nt, 2);
     }
-    for (int h = VARK ? 4 : 1; h <= 4 && !f32 && g_tile_mode == 0; h *= 2)
+    for (int h = VARK && !f32 ? 4 : 1; h <= 4 && g_tile_mode == 0; h *= 2)
       take(K_DEEP, h, cdiv(units, h), nt, h <= 2 ? 2 : 1);
   }
   return best;
@@ -169,11 +175,10 @@ moe_status launch_dense(hipStream_t s, moe_dtype dt, const DensePlan& d, int T, 
   const int grid = static_cast<int>(std::min(full, (items + kXcds - 1) / kXcds * kXcds));
   if (d.kernel == K_DEEP) {
     const GroupParams gp{p, 0, nullptr, 0};
-    if constexpr (!VARK) {
-      if (d.h == 1) MOE_TRY(launch_deep<MODE, PASS, 1>(s, gp, items));
-      if (d.h == 2) MOE_TRY(launch_deep<MODE, PASS, 2>(s, gp, items));
-    }
-    if (d.h == 4) MOE_TRY(launch_deep<MODE, PASS, 4>(s, gp, items));
+    // (bf16 weight gradients: 128 rows only, see mainloop_deep)
+    if (d.h == 1) MOE_TRY(launch_deep<MODE, PASS, 1>(s, dt, gp, items));
+    else if (d.h == 2) MOE_TRY(launch_deep<MODE, PASS, 2>(s, dt, gp, items));
+    else MOE_TRY(launch_deep<MODE, PASS, 4>(s, dt, gp, items));
   } else {
     MOE_TIMED(pass_name(PASS), s);
     if (dt == MOE_F32) {

@@ -108,9 +108,9 @@ moe_status launch_i8(hipStream_t s, KernelI8 k, const FfnPlan& pl, char* ws, con
   gp.p.ntiles = cdiv(p.N, is_gated(MODE) ? kMidN / 2 : kMidN);
   const int unit = k == I8_DEEP32 ? 32 : k == I8_DEEP64 ? 64 : 128;
   const int64_t most = (pl.rows_most / unit + groups) * gp.p.ntiles;
-  if (k == I8_DEEP32) return launch_deep<MODE, PASS, 1>(s, gp, most);
-  if (k == I8_DEEP64) return launch_deep<MODE, PASS, 2>(s, gp, most);
-  return launch_deep<MODE, PASS, 4>(s, gp, most);
+  if (k == I8_DEEP32) return launch_deep<MODE, PASS, 1>(s, MOE_BF16, gp, most);
+  if (k == I8_DEEP64) return launch_deep<MODE, PASS, 2>(s, MOE_BF16, gp, most);
+  return launch_deep<MODE, PASS, 4>(s, MOE_BF16, gp, most);
 }
 
 bool scales_ok(const float* x_scale, const int32_t* src, int T, int k) {

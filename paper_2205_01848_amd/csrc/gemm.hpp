@@ -1499,6 +1499,44 @@ __global__ __launch_bounds__(kThreads16, 2) void ffn_gemm16_mid_kernel(const Gem
   }
 }
 
+// The K loop with NS stages: step kt computes on stage kt mod NS while the
+// loads of step kt + NS - 1 (LOADS a wavefront) go into the stage that step
+// kt - 1 has read.
+template <int NS, int LOADS, typename Load, typename Compute>
+__device__ __forceinline__ void ring_steps(int nk, char* const (&sa)[NS], char* const (&sb)[NS],
+                                           Load&& load, Compute&& compute) {
+#pragma unroll
+  for (int s = 0; s < NS - 1; ++s) load(s, sa[s], sb[s]);
+  auto step = [&](int kt, auto slot) {
+    constexpr int S = decltype(slot)::value, T = (S + NS - 1) % NS;
+    // stage kt has landed when only the NS - 2 stages after it may be pending;
+    // past the barrier that holds for every wave's part of it, and every wave
+    // has read stage kt - 1, whose place step kt + NS - 1 takes over
+    __builtin_amdgcn_s_waitcnt(wait_vm_lgkm0((NS - 2) * LOADS));
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    load(kt + NS - 1, sa[T], sb[T]);
+    compute(sa[S], sb[S]);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  using std::integral_constant;
+  // whole groups without a branch between the steps: the compiler then knows
+  // which loads are pending at each read and adds no wait of its own
+  int k0 = 0;
+  for (; k0 + NS <= nk; k0 += NS) {
+    step(k0, integral_constant<int, 0>{});
+    step(k0 + 1, integral_constant<int, 1>{});
+    step(k0 + 2, integral_constant<int, 2>{});
+    if constexpr (NS > 3) step(k0 + 3, integral_constant<int, 3>{});
+  }
+  if (k0 < nk) step(k0, integral_constant<int, 0>{});
+  if (k0 + 1 < nk) step(k0 + 1, integral_constant<int, 1>{});
+  if constexpr (NS > 3)
+    if (k0 + 2 < nk) step(k0 + 2, integral_constant<int, 2>{});
+  __builtin_amdgcn_s_waitcnt(0x0070);
+  __builtin_amdgcn_s_barrier();   // every load landed, every read done: stages are free
+}
+
 // ---------------------------------------------------------------------------
 // fp32 products
 // ---------------------------------------------------------------------------
@@ -1522,9 +1560,11 @@ constexpr int kF32Step = 32;
 // 4 for B), segment s of k-row k stored at s ^ (k & (SEG - 1)).
 template <int NB> struct AccF32 { floatx16 v[NB]; };   // row blocks of a wave
 
-template <int RB, int PASS, bool GATED, int NB>
-__device__ __forceinline__ void mainloop_f32(const TileOps& op, char* la0, char* lb0, char* la1,
-                                             char* lb1, AccF32<NB>& acc_, AccF32<NB>& acc3_) {
+// sa, sb: the operands' NS stages (NS = 2 here; more in deep.hpp).
+template <int RB, int PASS, bool GATED, int NB, int NS>
+__device__ __forceinline__ void mainloop_f32(const TileOps& op, char* const (&stage_a)[NS],
+                                             char* const (&stage_b)[NS], AccF32<NB>& acc_,
+                                             AccF32<NB>& acc3_) {
   static_assert(NB == (GATED ? (RB + 1) / 2 : RB), "row blocks per wave");
   constexpr int ALAY = a_layout(PASS), BLAY = b_layout(PASS);
   floatx16(&acc)[NB] = acc_.v;
@@ -1634,20 +1674,97 @@ __device__ __forceinline__ void mainloop_f32(const TileOps& op, char* la0, char*
       }
     }
   };
-  load(0, la0, lb0);
-  __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
-  __builtin_amdgcn_s_barrier();
-  auto step = [&](int kt, char* ca, char* cb, char* na, char* nb) {
-    if (kt + 1 < nk) load(kt + 1, na, nb);
-    __builtin_amdgcn_sched_barrier(0);
-    compute(ca, cb);
-    __builtin_amdgcn_sched_barrier(0);
-    __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt(0) lgkmcnt(0)
+  if constexpr (NS == 2) {
+    char *const la0 = stage_a[0], *const lb0 = stage_b[0], *const la1 = stage_a[1], *const lb1 = stage_b[1];
+    load(0, la0, lb0);
+    __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0)
     __builtin_amdgcn_s_barrier();
-  };
-  for (int kt = 0; kt < nk; kt += 2) {
-    step(kt, la0, lb0, la1, lb1);
-    if (kt + 1 < nk) step(kt + 1, la1, lb1, la0, lb0);
+    auto step = [&](int kt, char* ca, char* cb, char* na, char* nb) {
+      if (kt + 1 < nk) load(kt + 1, na, nb);
+      __builtin_amdgcn_sched_barrier(0);
+      compute(ca, cb);
+      __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt(0) lgkmcnt(0)
+      __builtin_amdgcn_s_barrier();
+    };
+    for (int kt = 0; kt < nk; kt += 2) {
+      step(kt, la0, lb0, la1, lb1);
+      if (kt + 1 < nk) step(kt + 1, la1, lb1, la0, lb0);
+    }
+  } else {
+    ring_steps<NS, RB + 4>(nk, stage_a, stage_b, load, compute);
+  }
+}
+
+// Epilogue of an fp32 tile, straight from the accumulators.
+template <int MODE, int RB, int NB>
+__device__ __forceinline__ void epilogue_f32(const GemmParams& p, const MidTile& t, const AccF32<NB>& c1,
+                                             const AccF32<NB>& c3, int lane, int wave) {
+  constexpr bool GATED = is_gated(MODE), VARK = is_dw(MODE);
+  const floatx16(&acc)[NB] = c1.v;
+  const floatx16(&acc3)[NB] = c3.v;
+  // accumulator q of lane l: column l % 32, row 8 (q / 4) + 4 (l / 32) + q % 4
+  const int col = t.n0 + (GATED ? wave & 1 : wave) * 32 + (lane & 31);
+  if (col >= p.N) return;
+#pragma unroll
+  for (int i = 0; i < NB; ++i) {
+    const int blk = GATED ? 2 * i + (wave >> 1) : i;
+    if (GATED && blk >= RB) continue;
+#pragma unroll
+    for (int q = 0; q < 16; ++q) {
+      const int lm = blk * 32 + 8 * (q >> 2) + 4 * (lane >> 5) + (q & 3);
+      if (lm >= t.m_valid) continue;
+      const int64_t row = t.row0 + lm;
+      if constexpr (VARK) {
+        float* dst;
+        if (t.slot >= 0) dst = p.partial + static_cast<int64_t>(t.slot) * p.slot_elems + row * p.N;
+        else if (row < p.split_row) dst = p.dwA + static_cast<int64_t>(t.g) * p.dw_gstride + row * p.N;
+        else dst = p.dwB + static_cast<int64_t>(t.g) * p.dw_gstride + (row - p.split_row) * p.N;
+        dst[col] = acc[i][q];
+      } else {
+        float* c = reinterpret_cast<float*>(p.C + row * p.ldc) + col;
+        if constexpr (MODE == M_FWD1_SWIGLU) {
+          const float h1 = acc[i][q], h3 = acc3[i][q];
+          if (p.H1) {
+            reinterpret_cast<float*>(p.H1 + row * p.ldh)[col] = h1;
+            reinterpret_cast<float*>(p.H3 + row * p.ldh)[col] = h3;
+          }
+          *c = h1 * sigm(h1) * h3;
+        } else if constexpr (MODE == M_GATED_FWD) {
+          const float h1 = acc[i][q], h3 = acc3[i][q];
+          if (p.H1) {
+            reinterpret_cast<float*>(p.H1 + row * p.ldh)[col] = h1;
+            reinterpret_cast<float*>(p.H3 + row * p.ldh)[col] = h3;
+          }
+          *c = gate_f(h1, p.act) * h3;
+        } else if constexpr (MODE == M_GATED_DA) {
+          const float h1 = reinterpret_cast<const float*>(p.H1 + row * p.ldh)[col];
+          const float h3 = reinterpret_cast<const float*>(p.H3 + row * p.ldh)[col];
+          gate_bwd(acc[i][q], h1, h3, p.act, *c, c[p.f]);
+        } else if constexpr (MODE == M_ADD_STORE) {
+          if (t.slot >= 0) {
+            p.partial[t.slot * p.slot_elems + row * p.N + col] = acc[i][q];
+            continue;
+          }
+          const float b = p.add ? reinterpret_cast<const float*>(p.add + row * p.ldadd)[col] : 0.f;
+          *c = acc[i][q] + b;
+        } else if constexpr (MODE == M_FWD1) {
+          if (p.H1) reinterpret_cast<float*>(p.H1 + row * p.ldh)[col] = acc[i][q];
+          *c = act_f(acc[i][q], p.act);
+        } else if constexpr (MODE == M_BWD_DA_SWIGLU) {
+          const float h1 = reinterpret_cast<const float*>(p.H1 + row * p.ldh)[col];
+          const float h3 = reinterpret_cast<const float*>(p.H3 + row * p.ldh)[col];
+          // d silu(h1) h3 / dh1 = h3 sg (1 + h1 (1 - sg)), d / dh3 = h1 sg
+          const float sg = sigm(h1), x = acc[i][q] * sg, u = x * h3;
+          *c = __builtin_fmaf(u, __builtin_fmaf(-h1, sg, h1), u);
+          c[p.f] = x * h1;
+        } else if constexpr (MODE == M_BWD_DA) {
+          *c = acc[i][q] * act_grad_f(reinterpret_cast<const float*>(p.H1 + row * p.ldh)[col], p.act);
+        } else {
+          *c = acc[i][q];
+        }
+      }
+    }
   }
 }
 
@@ -1672,72 +1789,9 @@ __global__ __launch_bounds__(kThreads16, 2) void ffn_gemm_f32_kernel(const GemmP
       constexpr int RB = decltype(hc)::value;
       constexpr int NB = GATED ? (RB + 1) / 2 : RB;
       AccF32<NB> c1, c3;   // c3: the W3 half of a gated tile
-      mainloop_f32<RB, PASS, GATED, NB>(t.op, la0, lb0, la1, lb1, c1, c3);
-      floatx16(&acc)[NB] = c1.v;
-      floatx16(&acc3)[NB] = c3.v;
-      // accumulator q of lane l: column l % 32, row 8 (q / 4) + 4 (l / 32) + q % 4
-      const int col = t.n0 + (GATED ? wave & 1 : wave) * 32 + (lane & 31);
-      if (col >= p.N) return;
-#pragma unroll
-      for (int i = 0; i < NB; ++i) {
-        const int blk = GATED ? 2 * i + (wave >> 1) : i;
-        if (GATED && blk >= RB) continue;
-#pragma unroll
-        for (int q = 0; q < 16; ++q) {
-          const int lm = blk * 32 + 8 * (q >> 2) + 4 * (lane >> 5) + (q & 3);
-          if (lm >= t.m_valid) continue;
-          const int64_t row = t.row0 + lm;
-          if constexpr (VARK) {
-            float* dst;
-            if (t.slot >= 0) dst = p.partial + static_cast<int64_t>(t.slot) * p.slot_elems + row * p.N;
-            else if (row < p.split_row) dst = p.dwA + static_cast<int64_t>(t.g) * p.dw_gstride + row * p.N;
-            else dst = p.dwB + static_cast<int64_t>(t.g) * p.dw_gstride + (row - p.split_row) * p.N;
-            dst[col] = acc[i][q];
-          } else {
-            float* c = reinterpret_cast<float*>(p.C + row * p.ldc) + col;
-            if constexpr (MODE == M_FWD1_SWIGLU) {
-              const float h1 = acc[i][q], h3 = acc3[i][q];
-              if (p.H1) {
-                reinterpret_cast<float*>(p.H1 + row * p.ldh)[col] = h1;
-                reinterpret_cast<float*>(p.H3 + row * p.ldh)[col] = h3;
-              }
-              *c = h1 * sigm(h1) * h3;
-            } else if constexpr (MODE == M_GATED_FWD) {
-              const float h1 = acc[i][q], h3 = acc3[i][q];
-              if (p.H1) {
-                reinterpret_cast<float*>(p.H1 + row * p.ldh)[col] = h1;
-                reinterpret_cast<float*>(p.H3 + row * p.ldh)[col] = h3;
-              }
-              *c = gate_f(h1, p.act) * h3;
-            } else if constexpr (MODE == M_GATED_DA) {
-              const float h1 = reinterpret_cast<const float*>(p.H1 + row * p.ldh)[col];
-              const float h3 = reinterpret_cast<const float*>(p.H3 + row * p.ldh)[col];
-              gate_bwd(acc[i][q], h1, h3, p.act, *c, c[p.f]);
-            } else if constexpr (MODE == M_ADD_STORE) {
-              if (t.slot >= 0) {
-                p.partial[t.slot * p.slot_elems + row * p.N + col] = acc[i][q];
-                continue;
-              }
-              const float b = p.add ? reinterpret_cast<const float*>(p.add + row * p.ldadd)[col] : 0.f;
-              *c = acc[i][q] + b;
-            } else if constexpr (MODE == M_FWD1) {
-              if (p.H1) reinterpret_cast<float*>(p.H1 + row * p.ldh)[col] = acc[i][q];
-              *c = act_f(acc[i][q], p.act);
-            } else if constexpr (MODE == M_BWD_DA_SWIGLU) {
-              const float h1 = reinterpret_cast<const float*>(p.H1 + row * p.ldh)[col];
-              const float h3 = reinterpret_cast<const float*>(p.H3 + row * p.ldh)[col];
-              // d silu(h1) h3 / dh1 = h3 sg (1 + h1 (1 - sg)), d / dh3 = h1 sg
-              const float sg = sigm(h1), x = acc[i][q] * sg, u = x * h3;
-              *c = __builtin_fmaf(u, __builtin_fmaf(-h1, sg, h1), u);
-              c[p.f] = x * h1;
-            } else if constexpr (MODE == M_BWD_DA) {
-              *c = acc[i][q] * act_grad_f(reinterpret_cast<const float*>(p.H1 + row * p.ldh)[col], p.act);
-            } else {
-              *c = acc[i][q];
-            }
-          }
-        }
-      }
+      char *const sa[2] = {la0, la1}, *const sb[2] = {lb0, lb1};
+      mainloop_f32<RB, PASS, GATED, NB, 2>(t.op, sa, sb, c1, c3);
+      epilogue_f32<MODE, RB, NB>(p, t, c1, c3, lane, wave);
     };
     if constexpr (VARK) {
       switch (t.h) {
