@@ -564,8 +564,11 @@ size_t moe_expert_matmul_i8_workspace_bytes(int E, int N, int64_t rows_alloc);
  * for the rows r in [offsets[e], offsets[e]+rows[e]) of expert e, rows[e]
  * clamped as moe_expert_ffn_fwd clamps it.  The sums are exact (int32).
  *   dt      type of y
- *   K       bytes of a quantised row: a multiple of 16, at most 131072
- *   xq      [rows_alloc,K] int8, wq [E,N,K] int8, w_scale [E,N] float32
+ *   K       bytes of a quantised row: a multiple of 16, at most 131072; N a
+ *           multiple of 8
+ *   xq      [rows_alloc,K] int8, wq [E,N,K] int8, w_scale [E,N] float32; the
+ *           values in [-127, 127], as moe_quantize_rows leaves them (with
+ *           -128 the longest sums could leave int32)
  *   x_scale float32.  src NULL: [rows_alloc], xs(r) = x_scale[r].  Else src
  *           [rows_alloc] is moe_dispatch's (t*k + j per row) and x_scale
  *           [T] holds one scale per token: xs(r) = x_scale[src[r] / k].  So
@@ -616,13 +619,13 @@ size_t moe_gated_ffn_bwd_workspace_bytes(moe_dtype dt, int T, int d, int f);
  * every token passes (a shared expert beside the routed ones):
  *   H1 = X w1^T, H3 = X w3^T, A = act(H1) * H3, Y = add + A w2^T
  * with act MOE_SWIGLU: silu, MOE_GELU_TANH: GELU (tanh form), MOE_RELU: ReLU.
- * bf16: A and Y are rounded to bf16; with h_save so are H1 and H3, and A is
- * computed from the rounded values (as the backward reads them).
+ * bf16: A (computed from the unrounded H1 and H3) and Y are rounded to bf16.
  *   x, y    [T,d] layer dtype, rows ldx, ldy elements apart
  *   w1, w3  [f,d], w2 [d,f] layer dtype
  *   add     NULL, or [T,d] layer dtype, rows ldadd apart (the routed experts'
  *           output, say); y itself is allowed
- *   h_save  NULL for inference, else out [3,T,f]: H1, H3, A for the backward
+ *   h_save  NULL for inference, else out [3,T,f]: H3 * act'(H1), act(H1) and
+ *           A, what the backward reads, each rounded to the layer dtype once
  * Row distances are at least d and multiples of 8.
  */
 moe_status moe_gated_ffn_fwd(void* stream, moe_dtype dt, moe_act act, int T,
@@ -634,8 +637,9 @@ moe_status moe_gated_ffn_fwd(void* stream, moe_dtype dt, moe_act act, int T,
 
 /*
  * moe_gated_ffn_bwd - its gradients, from the planes the forward saved:
- *   dA = dY w2, dH1 = dA * H3 * act'(H1), dH3 = dA * act(H1)  (bf16: rounded)
+ *   dA = dY w2, dH1 = dA * (H3 * act'(H1)), dH3 = dA * act(H1)  (bf16: rounded)
  *   dX = add + dH1 w1 + dH3 w3, dW1 = dH1^T X, dW3 = dH3^T X, dW2 = dY^T A
+ *   act     the forward's
  *   dy, dx  [T,d] layer dtype, rows lddy, lddx elements apart; add NULL, or
  *           [T,d], rows ldadd apart (dx itself is allowed)
  *   dw_dt   type of the weight gradients: MOE_F32, or the layer dtype
@@ -686,9 +690,12 @@ moe_status moe_set_gemm_tiles(int mode);
  * product outweighs the copy; 1: never; 2: always.  The products are
  * identical bit for bit either way.  moe_ffn_bwd_workspace_bytes includes
  * the copy's E*d*F*2 bytes when the current mode would make it; a call
- * whose workspace lacks them reads the weights K-major.  Process-wide; read
- * when moe_expert_ffn_bwd (or the workspace query) is called.  Returns
- * MOE_EINVAL for other modes. [host]
+ * whose workspace lacks them reads the weights K-major.  moe_gated_ffn_bwd
+ * follows the same rule for its one expert of T rows; its query and its call
+ * are to see the same mode (a smaller workspace is MOE_EWORKSPACE there, as it
+ * is after a change of moe_set_gemm_tiles).  Process-wide; read when a
+ * backward (or its workspace query) is called.  Returns MOE_EINVAL for other
+ * modes. [host]
  */
 moe_status moe_set_dx_weight_copy(int mode);
 

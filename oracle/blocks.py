@@ -47,17 +47,18 @@ def gate_act_grad(h, act):
 
 
 def gated_fwd(x, w1, w3, w2, act, add=None):
-    """(H1, H3, A, Y) of the dense gated block."""
+    """(H3 act'(H1), act(H1), A, Y) of the dense gated block."""
     h1, h3 = x @ w1.T, x @ w3.T
-    a = gate_act(h1, act) * h3
+    g = gate_act(h1, act)
+    a = g * h3
     y = a @ w2.T
-    return h1, h3, a, y if add is None else add + y
+    return h3 * gate_act_grad(h1, act), g, a, y if add is None else add + y
 
 
-def gated_bwd(x, h1, h3, a, w1, w3, w2, dy, act, add=None):
-    """dict of dH1, dH3, dX, dW1, dW3, dW2 from the saved planes."""
+def gated_bwd(x, f1, f3, a, w1, w3, w2, dy, add=None):
+    """dict of dH1, dH3, dX, dW1, dW3, dW2 from the planes of gated_fwd."""
     da = dy @ w2
-    dh1, dh3 = da * h3 * gate_act_grad(h1, act), da * gate_act(h1, act)
+    dh1, dh3 = da * f1, da * f3
     dx = dh1 @ w1 + dh3 @ w3
     return dict(dh1=dh1, dh3=dh3, dx=dx if add is None else add + dx, dw1=dh1.T @ x, dw3=dh3.T @ x,
                 dw2=dy.T @ a)

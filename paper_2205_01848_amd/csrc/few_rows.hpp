@@ -239,26 +239,24 @@ __global__ __launch_bounds__(64 * W) void ffn_few_rows_kernel(const GroupParams 
             }
             constexpr int OS = ES == 4 ? 4 : 2;   // bytes of the dense block's values
             if constexpr (MODE == M_GATED_FWD) {
-              if (p.H1) {
+              float g, dg;
+              gate_f(v, p.act, g, dg);
+              if (p.H1) {   // the backward's factors
                 char *h1 = p.H1 + row * p.ldh + static_cast<int64_t>(col) * OS,
                      *h3 = p.H3 + row * p.ldh + static_cast<int64_t>(col) * OS;
                 if constexpr (ES == 4) {
-                  *reinterpret_cast<float*>(h1) = v;
-                  *reinterpret_cast<float*>(h3) = v3;
+                  *reinterpret_cast<float*>(h1) = v3 * dg;
+                  *reinterpret_cast<float*>(h3) = g;
                 } else {
-                  // saved values are rounded once, and the activation is theirs
-                  const uint16_t r1 = f2bf(v), r3 = f2bf(v3);
-                  *reinterpret_cast<uint16_t*>(h1) = r1;
-                  *reinterpret_cast<uint16_t*>(h3) = r3;
-                  v = bf2f(r1);
-                  v3 = bf2f(r3);
+                  *reinterpret_cast<uint16_t*>(h1) = f2bf(v3 * dg);
+                  *reinterpret_cast<uint16_t*>(h3) = f2bf(g);
                 }
               }
-              v = gate_f(v, p.act) * v3;
+              v = g * v3;
             } else if constexpr (MODE == M_I8_FWD1_SWIGLU) {
               v = v * sigm(v) * v3;
             } else if constexpr (MODE == M_I8_FWD1) {
-              v = act_f(v, p.act);
+              v = act_i8(v, p.act);
             } else if constexpr (MODE == M_ADD_STORE) {
               if (p.add) {
                 const char* b = p.add + row * p.ldadd + static_cast<int64_t>(col) * OS;

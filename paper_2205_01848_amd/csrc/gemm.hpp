@@ -94,31 +94,36 @@ __device__ __forceinline__ float act_grad_f(float h, int act) {
   return 0.5f * (1.f + th) + 0.5f * h * (1.f - th * th) * du;
 }
 __device__ __forceinline__ float sigm(float h) { return rcp_fast(1.f + exp_fast(-h)); }
-// The gate half of the dense block: silu (act SWIGLU), GELU or ReLU, and its
-// part in the backward, dh1 = da h3 act'(h1), dh3 = da act(h1).
-__device__ __forceinline__ float gate_f(float h, int act) {
-  return act == ACT_SWIGLU ? h * sigm(h) : act_f(h, act);
-}
-__device__ __forceinline__ void gate_bwd(float da, float h1, float h3, int act, float& dh1,
-                                         float& dh3) {
+// ReLU that keeps a NaN (a maximum with 0 would hide it).
+__device__ __forceinline__ float relu_nan(float h) { return h <= 0.f ? 0.f : h; }
+
+// The gate half of the dense block: g = act(h), silu (act SWIGLU), GELU or ReLU,
+// and its derivative dg.  The forward saves h3 dg and g, the factors of dA in
+// dH1 = dA (h3 dg) and dH3 = dA g, so the backward evaluates no activation.
+__device__ __forceinline__ void gate_f(float h, int act, float& g, float& dg) {
   if (act == ACT_SWIGLU) {
-    const float sg = sigm(h1), t = da * sg, u = t * h3;
-    dh1 = __builtin_fmaf(u, __builtin_fmaf(-h1, sg, h1), u);
-    dh3 = t * h1;
+    const float sg = sigm(h);
+    g = h * sg;
+    dg = __builtin_fmaf(g, 1.f - sg, sg);
   } else if (act == ACT_RELU) {
-    dh1 = h1 > 0.f ? da * h3 : 0.f;
-    dh3 = da * fmaxf(h1, 0.f);
+    g = relu_nan(h);
+    dg = h <= 0.f ? 0.f : h == h ? 1.f : h;
   } else {
-    // GELU = h s with s = sigmoid(2u): s + 2 h s (1 - s) u'.  Past |h| = 10 the
+    // GELU = h s with s = sigmoid(2u): s + h s (1 - s) 2u'.  Past |h| = 10 the
     // derivative is 1 or 0 to the last bit of a float; there u', whose h^2
     // grows without bound, is taken at 10
-    const float s = act_f(h1, ACT_GELU), hc = fminf(fmaxf(h1, -10.f), 10.f);
+    g = act_f(h, ACT_GELU);
+    const float hc = fminf(fmaxf(h, -10.f), 10.f);
     const float sg = rcp_fast(1.f + __builtin_amdgcn_exp2f(
                                         hc * __builtin_fmaf(kGelu3, hc * hc, kGelu1)));
     const float du = 1.5957691216057308f * __builtin_fmaf(3.f * 0.044715f, hc * hc, 1.f);
-    dh1 = da * h3 * __builtin_fmaf(hc * du, sg * (1.f - sg), sg);
-    dh3 = da * s;
+    dg = h == h ? __builtin_fmaf(hc * du, sg * (1.f - sg), sg) : h;
   }
+}
+// The activation of an int8 expert: a token that holds a NaN has scale NaN,
+// and its output has to show it.
+__device__ __forceinline__ float act_i8(float h, int act) {
+  return act == ACT_RELU ? relu_nan(h) : act_f(h, act);
 }
 
 // ---------------------------------------------------------------------------
@@ -227,8 +232,8 @@ enum Mode {
   M_I8_FWD1_SWIGLU = 8,    // A = silu(H1) H3
   // the dense gated block (gated.hip): no routing arrays, see Dense; the gate
   // half's activation at run time
-  M_GATED_FWD = 9,         // H1, H3 -> A = act(H1) H3 [, H1 H3 saved]
-  M_GATED_DA = 10,         // dA = dY W2 -> dH1 = dA H3 act'(H1), dH3 = dA act(H1)
+  M_GATED_FWD = 9,         // H1, H3 -> A = act(H1) H3 [, H3 act'(H1) and act(H1) saved]
+  M_GATED_DA = 10,         // dA = dY W2 -> dH1, dH3: dA times the saved factors
   M_ADD_STORE = 11,        // store with an addend (Y, dX), or partial sums
   M_DENSE_DW = 12          // weight gradient in fp32 or bf16, or partial sums
 };
@@ -970,14 +975,28 @@ __device__ __forceinline__ void epilogue16(const GemmParams& p,
             h1[e] = strip[r * kP + u8 + e];
             h3[e] = strip[r * kP + U + u8 + e];
           }
-          const uint4 b1 = pack8(h1), b3 = pack8(h3);
-          if (MODE == M_FWD1_SWIGLU || p.H1) {
+          uint4 b1, b3;
+          if constexpr (MODE == M_GATED_FWD) {
+            // A from the unrounded H; what is saved are the backward's factors
+            // (in the places of H1 and H3), rounded once
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              float g, dg;
+              gate_f(h1[e], ACT, g, dg);
+              a[e] = g * h3[e];
+              h1[e] = h3[e] * dg;
+              h3[e] = g;
+            }
+            b1 = pack8(h1);
+            b3 = pack8(h3);
+          } else {
+            b1 = pack8(h1);
+            b3 = pack8(h3);
             unpack8(b1, h1);
             unpack8(b3, h3);
-          }
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
-            a[e] = (ACT == ACT_SWIGLU ? h1[e] * sigm(h1[e]) : act_f(h1[e], ACT)) * h3[e];
+            for (int e = 0; e < 8; ++e) a[e] = h1[e] * sigm(h1[e]) * h3[e];
+          }
           const int64_t grow = row0 + lm;
           if (p.H1) {
             *reinterpret_cast<uint4*>(p.H1 + grow * p.ldh + static_cast<int64_t>(gc) * ES) = b1;
@@ -1031,8 +1050,9 @@ __device__ __forceinline__ void epilogue16(const GemmParams& p,
           for (int e = 0; e < 8; ++e) {
             // d silu(h1) h3 / dh1 = h3 sg (1 + h1 (1 - sg)), d / dh3 = h1 sg
             const float da = strip[r * kP + c8 + e];
-            if constexpr (ACT != ACT_SWIGLU) {
-              gate_bwd(da, h1[e], h3[e], ACT, g1[e], g3[e]);
+            if constexpr (MODE == M_GATED_DA) {
+              g1[e] = da * h1[e];
+              g3[e] = da * h3[e];
               continue;
             }
             const float sg = sigm(h1[e]);
@@ -1117,7 +1137,7 @@ __device__ __forceinline__ void epilogue16(const GemmParams& p,
   if constexpr (MODE == M_FWD1 || MODE == M_BWD_DA) {
     if (p.act == ACT_RELU) epilogue(std::integral_constant<int, ACT_RELU>{});
     else epilogue(std::integral_constant<int, ACT_GELU>{});
-  } else if constexpr (MODE == M_GATED_FWD || MODE == M_GATED_DA) {
+  } else if constexpr (MODE == M_GATED_FWD) {
     if (p.act == ACT_RELU) epilogue(std::integral_constant<int, ACT_RELU>{});
     else if (p.act == ACT_GELU) epilogue(std::integral_constant<int, ACT_GELU>{});
     else epilogue(std::integral_constant<int, ACT_SWIGLU>{});
@@ -1179,7 +1199,7 @@ __device__ __forceinline__ void epilogue_i8(const GemmParams& p, const floatx4 (
           for (int e = 0; e < 8; ++e) {
             v[e] = sp[e] * as * s1[e];
             if constexpr (GATED) v[e] = v[e] * sigm(v[e]) * (sp[U + e] * as * s3[e]);
-            else if constexpr (MODE == M_I8_FWD1) v[e] = act_f(v[e], ACT);
+            else if constexpr (MODE == M_I8_FWD1) v[e] = act_i8(v[e], ACT);
           }
           char* dst = p.C + static_cast<int64_t>(row0 + lm) * p.ldc;
           if (p.out_f32) {
@@ -1731,16 +1751,17 @@ __device__ __forceinline__ void epilogue_f32(const GemmParams& p, const MidTile&
           }
           *c = h1 * sigm(h1) * h3;
         } else if constexpr (MODE == M_GATED_FWD) {
-          const float h1 = acc[i][q], h3 = acc3[i][q];
+          const float h3 = acc3[i][q];
+          float g, dg;
+          gate_f(acc[i][q], p.act, g, dg);
           if (p.H1) {
-            reinterpret_cast<float*>(p.H1 + row * p.ldh)[col] = h1;
-            reinterpret_cast<float*>(p.H3 + row * p.ldh)[col] = h3;
+            reinterpret_cast<float*>(p.H1 + row * p.ldh)[col] = h3 * dg;
+            reinterpret_cast<float*>(p.H3 + row * p.ldh)[col] = g;
           }
-          *c = gate_f(h1, p.act) * h3;
+          *c = g * h3;
         } else if constexpr (MODE == M_GATED_DA) {
-          const float h1 = reinterpret_cast<const float*>(p.H1 + row * p.ldh)[col];
-          const float h3 = reinterpret_cast<const float*>(p.H3 + row * p.ldh)[col];
-          gate_bwd(acc[i][q], h1, h3, p.act, *c, c[p.f]);
+          *c = acc[i][q] * reinterpret_cast<const float*>(p.H1 + row * p.ldh)[col];
+          c[p.f] = acc[i][q] * reinterpret_cast<const float*>(p.H3 + row * p.ldh)[col];
         } else if constexpr (MODE == M_ADD_STORE) {
           if (t.slot >= 0) {
             p.partial[t.slot * p.slot_elems + row * p.N + col] = acc[i][q];

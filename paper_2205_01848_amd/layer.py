@@ -119,7 +119,7 @@ class MoELayer:
                 self.dlogits = e(T, E, t=f32)
                 self.dw_g = e(E, d, t=f32)
                 self.ws_gate_bwd = B.workspace(B.moe_gate_bwd_workspace_bytes(T, d, E), self.dev)
-        # the shared expert: its saved planes H1, H3, A and float32 gradients
+        # the shared expert: its saved planes and float32 gradients
         self.shared_f, self.shared_act = shared_f, B.ACTS[shared_act]
         if shared_f:
             sf = shared_f

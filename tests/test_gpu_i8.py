@@ -204,6 +204,26 @@ def test_ffn(tiles, rows, slack, d, f, dt, act):
     assert (got[~used] == 3).all()
 
 
+@pytest.mark.parametrize("act", ["swiglu", "gelu_tanh", "relu"])
+@pytest.mark.parametrize("R", [2, 40, 300])
+def test_ffn_shows_a_token_that_is_not_a_number(tiles, act, R):
+    """A NaN or an infinity in one token: its whole output is NaN, the others' are numbers."""
+    rng = np.random.default_rng(R)
+    d, f = 64, 136
+    x = rng.standard_normal((R, d)).astype(np.float32)
+    x[1, 5] = np.nan if R != 40 else np.inf
+    q, sc = torch.empty(R, 64, dtype=torch.int8, device=dev()), torch.empty(R, device=dev())
+    B.moe_quantize_rows(_d(x), q, sc)
+    (w1, s1), (w3, s3), (w2, s2) = _quantised(rng, d, 1, f), _quantised(rng, d, 1, f), _quantised(rng, f, 1, d)
+    y = torch.empty(R, d, device=dev())
+    g = act == "swiglu"
+    B.moe_expert_ffn_fwd_i8(B.ACTS[act], _d(np.array([0, R], np.int32)), _d(np.array([R], np.int32)), q, sc, _d(w1),
+                            _d(s1), _d(w3) if g else None, _d(s3) if g else None, _d(w2), _d(s2), y,
+                            B.workspace(B.moe_ffn_fwd_i8_workspace_bytes(B.MOE_F32, B.ACTS[act], 1, d, f, R), dev()))
+    bad = torch.isnan(y)
+    assert bad[1].all() and bad.sum() == d
+
+
 def test_empty_calls():
     i32 = lambda *v: torch.tensor(v, dtype=torch.int32, device=dev())
     q8 = lambda *s: torch.zeros(*s, dtype=torch.int8, device=dev())

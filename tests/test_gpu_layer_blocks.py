@@ -45,8 +45,8 @@ def test_shared_expert_in_training(dt, act, sact):
     assert torch.equal(dw1, L.dw1)              # the routed experts' part is the same
     s = [to_np(t) for t in dv["shared"]]
     x, dy = to_np(dv["x"]), to_np(dv["dy"])
-    h1, h3, a, ref = O.gated_fwd(x, *s, sact, to_np(routed))
-    b = O.gated_bwd(x, h1, h3, a, *s, dy, sact, to_np(droute))
+    f1, f3, a, ref = O.gated_fwd(x, *s, sact, to_np(routed))
+    b = O.gated_bwd(x, f1, f3, a, *s, dy, to_np(droute))
     # the layer's own tolerance: a few roundings to the layer dtype along the way
     assert_close(to_np(y), ref, RTOL[dt], "y")
     assert_close(to_np(dx), b["dx"], RTOL[dt], "dx")

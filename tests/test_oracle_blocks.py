@@ -55,9 +55,9 @@ def test_gated_block_is_autograd(act):
     g = {"swiglu": F.silu, "relu": F.relu, "gelu_tanh": lambda h: F.gelu(h, approximate="tanh")}[act]
     y = torch.tensor(add) + (g(t[0] @ t[1].T) * (t[0] @ t[2].T)) @ t[3].T
     y.backward(torch.tensor(dy))
-    h1, h3, a, got = O.gated_fwd(x, w1, w3, w2, act, add)
+    f1, f3, a, got = O.gated_fwd(x, w1, w3, w2, act, add)
     np.testing.assert_allclose(got, y.detach().numpy(), rtol=1e-12, atol=1e-12)
-    b = O.gated_bwd(x, h1, h3, a, w1, w3, w2, dy, act, add)
+    b = O.gated_bwd(x, f1, f3, a, w1, w3, w2, dy, add)
     for name, ref in zip(("dx", "dw1", "dw3", "dw2"), t):
         r = ref.grad.numpy() + (add if name == "dx" else 0)
         np.testing.assert_allclose(b[name], r, rtol=1e-11, atol=1e-12)
@@ -67,8 +67,8 @@ def test_gated_block_is_autograd(act):
 def test_gated_gradients_are_differences(act):
     x, w1, w3, w2, dy, _ = _block(3)
     ins = dict(x=x, w1=w1, w3=w3, w2=w2)
-    h1, h3, a, _ = O.gated_fwd(x, w1, w3, w2, act)
-    b = O.gated_bwd(x, h1, h3, a, w1, w3, w2, dy, act)
+    f1, f3, a, _ = O.gated_fwd(x, w1, w3, w2, act)
+    b = O.gated_bwd(x, f1, f3, a, w1, w3, w2, dy)
     rng, step = np.random.default_rng(4), 1e-5
     for name in ins:
         v = rng.standard_normal(ins[name].shape)
