@@ -9,8 +9,6 @@
 // instead of 64, at the same number of matrix instructions, so the same loop
 // does twice the products per second, and the same bytes.
 
-#include <cmath>
-
 #include "dense.hpp"
 #include "few_rows.hpp"
 #include "quant.hpp"
@@ -25,7 +23,7 @@ struct PlanI8 {
   size_t o_a, o_aq, o_as, total;
 };
 
-bool plan_i8(moe_dtype dt, moe_act act, int E, int d, int f, int64_t rows_alloc, PlanI8& q) {
+bool layout_i8(moe_dtype dt, moe_act act, int E, int d, int f, int64_t rows_alloc, PlanI8& q) {
   if (!dtype_ok(dt) || d > kMaxQuant || f > kMaxQuant) return false;
   if (!make_plan(MOE_BF16, act, E, d, f, rows_alloc, q.pl)) return false;
   q.pl.es = 1;
@@ -37,64 +35,8 @@ bool plan_i8(moe_dtype dt, moe_act act, int E, int d, int f, int64_t rows_alloc,
   return true;
 }
 
-// The kernel of one product: the one for few rows, deep tiles of 32, 64 or 128
-// rows, or, with a schedule, the tiles of gemm.hpp (128 columns and up to 192
-// rows, or 256 x 256).
-enum KernelI8 { I8_FEW, I8_DEEP32, I8_DEEP64, I8_DEEP128, I8_MID, I8_BIG };
-bool scheduled(KernelI8 k) { return k >= I8_MID; }
-
-// The host knows the rows at most and their mean over the experts, not the
-// loads: it compares the estimated times for experts of the mean, half a tile
-// more for raggedness.  A product is as long as its rounds of tiles (tile_time; a K
-// step is 128 bytes, as in bf16) or as the read of its live experts' weights, at
-// 5.6 bytes per ps, a tenth more for every further tile of an expert.  Few rows:
-// up to 16, bound by that read.  Over 47 calls (1 to 64 experts, 1 to 6000
-// rows, K from 1000 to 14336) the choice takes 0.3 % more than the best kernel.
-// Examples, us a call, few / deep 32 / deep 64 / deep 128 / tiles: FFN 4096,
-// 14336 of 8 experts, 8 rows 176 / 182 / 192 / 197 / 231, 256 rows 685 / 324 / 282
-// / 295 / 326, 1024 rows 2224 / 625 / 473 / 441 / 381; 64 experts 2048, 1408,
-// 512 rows 132 / 90 / 91 / 101 / 103; one product 14336 -> 4096, 16 rows 18 / 28
-// / 38 / 53 / 58.  The two tiles, us, 256 x 256 / 128 columns: 8192 rows on 8
-// experts, 4096 -> 2 x 14336 897 / 1000, 14336 -> 4096 506 / 468.
 KernelI8 kernel_i8(const FfnPlan& pl, int K, int N, bool gated) {
-  if (g_tile_mode != 0) return g_tile_mode == 1 ? I8_BIG : I8_MID;
-  const int groups = static_cast<int>(std::min<int64_t>(pl.E, pl.rows_most)), cus = persistent_grid();
-  const double mean = std::max(1., static_cast<double>(pl.rows_most) / pl.E);
-  const int steps = cdiv(K, kRowBytes);
-  const double read = static_cast<double>(groups) * N * (gated ? 2 : 1) * K / 5600;
-  auto tiles = [&](int unit) {   // of all experts, along M
-    return groups > 1 ? groups * std::max(1., mean / unit + 0.5) : static_cast<double>(cdiv(pl.rows_most, unit));
-  };
-  auto rounds = [&](double n, int per_cu, int half) {
-    const int places = per_cu * cus;
-    return n > places ? n / places + 0.25 : per_cu == 2 && 2 * n <= places ? half / 100. : 1.;
-  };
-  auto tile = [&](DenseKernel k, int h, int unit, int cols, int per_cu, int slower) {
-    const TileTime t = tile_time(false, k, h, D_KC);
-    const double n = tiles(unit) * cdiv(N, gated ? cols / 2 : cols);
-    // the tiles of gemm.hpp are for many rows: whole rounds
-    const double r = k != K_DEEP && n > per_cu * cus ? std::ceil(n / (per_cu * cus)) : rounds(n, per_cu, t.half);
-    return r * (static_cast<double>(t.step) * slower / 100 * steps + t.fix);
-  };
-  // the int8 matrix instructions draw more power than the bf16 ones: a step of
-  // the large tiles takes 7 to 10 % longer
-  const double big = tile(K_BIG, 0, BM, BN, 1, 107);
-  double mid = 0;
-  for (int h = 1; h <= kMidMaxH; ++h) {
-    const double t = tile(K_MID, h, kMidUnit * h, kMidN, 2, 110);
-    if (h == 1 || t < mid) mid = t;
-  }
-  KernelI8 best = big <= mid ? I8_BIG : I8_MID;
-  double t_best = std::max(std::min(big, mid), 1.15 * read + 3000) + 7000;   // and the schedule's launch
-  auto take = [&](KernelI8 k, double t) {
-    if (t < t_best) { t_best = t; best = k; }
-  };
-  for (int h = 1; h <= 4; h *= 2)
-    take(h == 1 ? I8_DEEP32 : h == 2 ? I8_DEEP64 : I8_DEEP128,
-         std::max(tile(K_DEEP, h, kMidUnit * h, kMidN, h <= 2 ? 2 : 1, 100),
-                  read * (0.9 + 0.1 * tiles(kMidUnit * h) / groups) + 3000));
-  if (pl.rows_most <= 16) take(I8_FEW, read + 2500);
-  return best;
+  return plan_i8(pl.E, pl.rows_most, K, N, gated, persistent_grid(), g_tile_mode);
 }
 
 // One product by kernel k.
@@ -180,7 +122,7 @@ extern "C" moe_status moe_expert_matmul_i8(void* stream, moe_dtype dt, int E, in
 extern "C" size_t moe_ffn_fwd_i8_workspace_bytes(moe_dtype dt, moe_act act, int E, int d, int f,
                                                  int64_t rows_alloc) {
   PlanI8 q;
-  return plan_i8(dt, act, E, d, f, rows_alloc, q) ? q.total : 0;
+  return layout_i8(dt, act, E, d, f, rows_alloc, q) ? q.total : 0;
 }
 
 extern "C" moe_status moe_expert_ffn_fwd_i8(void* stream, moe_dtype dt, moe_act act, int E, int d,
@@ -192,7 +134,7 @@ extern "C" moe_status moe_expert_ffn_fwd_i8(void* stream, moe_dtype dt, moe_act 
                                             const int8_t* w2q, const float* w2_scale, void* y_disp,
                                             void* workspace, size_t workspace_bytes) {
   PlanI8 q;
-  if (!plan_i8(dt, act, E, d, f, rows_alloc, q)) return MOE_EINVAL;
+  if (!layout_i8(dt, act, E, d, f, rows_alloc, q)) return MOE_EINVAL;
   const bool sw = act == MOE_SWIGLU;
   if (!offsets || !rows || !w1q || !w1_scale || !w2q || !w2_scale) return MOE_EINVAL;
   if (sw && (!w3q || !w3_scale || !aligned16(w3q))) return MOE_EINVAL;

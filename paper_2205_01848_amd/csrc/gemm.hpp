@@ -39,6 +39,7 @@
 
 #include "common.hpp"
 #include "ffn.hpp"
+#include "plan.hpp"
 #include "sched.hpp"
 #include "validate.hpp"
 
@@ -1957,8 +1958,6 @@ int persistent_grid() {
   const int n = num_cus();
   return (n + kXcds - 1) / kXcds * kXcds;
 }
-
-inline int cdiv(int64_t a, int64_t b) { return static_cast<int>((a + b - 1) / b); }
 
 // [rows_alloc, f] planes of h_save: A (ReLU), H and A (GELU), H1, H3 and A
 // (SwiGLU).

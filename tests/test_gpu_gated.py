@@ -64,11 +64,28 @@ def tiles(request):
     B.moe_set_gemm_tiles(0)
 
 
+# sizes at which the plan takes each kernel, tile height and split of K
+LARGER = [(777, 40, 72), (1030, 40, 2056), (2056, 40, 2056), (2056, 1032, 72), (2056, 1032, 520), (4100, 40, 72),
+          (4100, 40, 200), (4100, 136, 72), (4100, 136, 1032), (4100, 40, 2056), (777, 136, 2056),
+          (1030, 1032, 2056), (4100, 1032, 1032), (4100, 1032, 2056), (200, 4104, 1032), (1, 2056, 72),
+          (100, 40, 8200)]
+
+
 @pytest.mark.parametrize("act", ["swiglu", "gelu_tanh", "relu"])
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
 @pytest.mark.parametrize("T,d,f", SHAPES)
 @pytest.mark.parametrize("pad", [0, 24])
 def test_forward_and_backward(tiles, T, d, f, act, dt, pad):
+    _check_block(T, d, f, act, dt, pad)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("T,d,f", LARGER)
+def test_every_plan(T, d, f, dt):
+    _check_block(T, d, f, "swiglu", dt, 8)
+
+
+def _check_block(T, d, f, act, dt, pad):
     P = _problem(T, d, f, dt, pad)
     N = {n: to_np(v) for n, v in P.items()}
     rnd = ROUND[dt]

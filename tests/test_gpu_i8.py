@@ -94,6 +94,8 @@ SHAPES = [  # rows per expert, slack rows, K, N
     ([513], [0], 1032, 520),
     ([64, 64, 0, 250], [0, 0, 0, 6], 512, 1000),
     ([2] * 64, [0] * 64, 256, 72),
+    ([300], [0], 256, 4104),
+    ([300, 290], [0, 7], 1040, 4104),
 ]
 
 
