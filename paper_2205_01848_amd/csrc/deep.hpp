@@ -60,8 +60,8 @@ __device__ __forceinline__ void mma16(floatx4& c, const uint4& a, const uint4& b
 // of 128 elements (K-major A: RB = 4).
 // K-major k-rows r with r & 8 also have the two 16-element halves of every 32-element
 // segment swapped: a transpose read takes half a segment of k-rows r .. r + 3 and of
-// r + 8 .. r + 11 at X
-// -> 1384, the backward's dX: 43.4 -> 39.4 us; dW 31.6 -> 31.0.  In the tiles of 256,
+// r + 8 .. r + 11 at once, which would otherwise lie on the same banks (2048 tokens,
+// 1024 -> 2816: the backward's dX 43.4 -> 39.4 us, dW 31.6 -> 31.0.  In tiles of 256,
 // bound by other things, the swap gains nothing and is not made.)
 template <int RB, int NS, int ALAY, int BLAY, bool GATED, int ES>
 __device__ __forceinline__ void mainloop_deep(const TileOps& op, char* const (&sa)[NS],
