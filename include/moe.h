@@ -623,7 +623,8 @@ size_t moe_gated_ffn_bwd_workspace_bytes(moe_dtype dt, int T, int d, int f);
  *   x, y    [T,d] layer dtype, rows ldx, ldy elements apart
  *   w1, w3  [f,d], w2 [d,f] layer dtype
  *   add     NULL, or [T,d] layer dtype, rows ldadd apart (the routed experts'
- *           output, say); y itself is allowed
+ *           output, say).  y may be x or add itself (with the same row
+ *           distance)
  *   h_save  NULL for inference, else out [3,T,f]: H3 * act'(H1), act(H1) and
  *           A, what the backward reads, each rounded to the layer dtype once
  * Row distances are at least d and multiples of 8.
@@ -641,7 +642,8 @@ moe_status moe_gated_ffn_fwd(void* stream, moe_dtype dt, moe_act act, int T,
  *   dX = add + dH1 w1 + dH3 w3, dW1 = dH1^T X, dW3 = dH3^T X, dW2 = dY^T A
  *   act     the forward's
  *   dy, dx  [T,d] layer dtype, rows lddy, lddx elements apart; add NULL, or
- *           [T,d], rows ldadd apart (dx itself is allowed)
+ *           [T,d], rows ldadd apart.  dX is the last product, so dx may be dy,
+ *           x or add itself (with the same row distance)
  *   dw_dt   type of the weight gradients: MOE_F32, or the layer dtype
  *   dw1, dw3 [f,d], dw2 [d,f] out, overwritten (zeros for T = 0)
  */
@@ -673,7 +675,9 @@ int moe_timing_report(char* buf, size_t len);
  * and tiles of 32 to 192 rows and 128 columns (two workgroups per CU; the
  * heights chosen on the device from the rows per expert) -- the latter for
  * products with few tiles per CU; both kernels add every output's products in the same
- * order, so results are identical bit for bit in every mode.  1:
+ * order, so results are identical bit for bit in every mode.  (Also of the
+ * int8 products, whose sums are exact; a dense gated block may split a sum
+ * over K in a different number of ranges in another mode.)  1:
  * 256x256 only; 2: 128-column tiles only.  float32 layers run every product
  * on 128-column tiles in every mode.  Process-wide; read when a product is
  * launched.  Returns MOE_EINVAL for other modes. [host]

@@ -202,8 +202,6 @@ extern "C" moe_status moe_gated_ffn_bwd(void* stream, moe_dtype dt, moe_act act,
     for (void* w : {dw1, dw3, dw2}) MOE_TRY(launch_zero(s, w, bytes));
     return MOE_OK;
   }
-  if (g.wt) MOE_TRY(launch_transpose_w(s, 1, w1, w3, f, f, d, wt13));
-
   // dH from dA = dY W2 (W2 read K-major)
   GemmParams p{};
   p.A = static_cast<const char*>(dy);
@@ -220,29 +218,6 @@ extern "C" moe_status moe_gated_ffn_bwd(void* stream, moe_dtype dt, moe_act act,
   p.ldh = f * es;
   p.f = f;
   MOE_TRY(launch_dense<M_GATED_DA, P_BWD_DA>(s, dt, g.da, T, T, p));
-
-  // dX = add + [dH1 | dH3] [W1; W3]
-  GemmParams q{};
-  q.A = dh;
-  q.lda = F * es;
-  q.K = F;
-  q.N = d;
-  q.C = static_cast<char*>(dx);
-  q.ldc = lddx * es;
-  q.add = static_cast<const char*>(add);
-  q.ldadd = ldadd * es;
-  q.partial = partial;
-  if (g.wt) {
-    q.B = wt13;
-    q.ldb = F * es;
-    MOE_TRY(launch_dense<M_ADD_STORE, P_BWD_DX_T>(s, dt, g.dx, T, T, q));
-  } else {
-    q.B = static_cast<const char*>(w1);
-    q.B2 = static_cast<const char*>(w3);
-    q.kmsplit = f;
-    q.ldb = d * es;
-    MOE_TRY(launch_dense<M_ADD_STORE, P_BWD_DX>(s, dt, g.dx, T, T, q));
-  }
 
   // dW2 [d, f] = dY^T A, then [dW1; dW3] [2f, d] = [dH1 dH3]^T X
   auto weights = [&](const void* l, int64_t ldl, const void* r, int64_t ldr, int m, int n, void* to1,
@@ -263,6 +238,29 @@ extern "C" moe_status moe_gated_ffn_bwd(void* stream, moe_dtype dt, moe_act act,
   };
   MOE_TRY(launch_dense<M_DENSE_DW, P_BWD_DW2>(s, dt, g.dw2, T, d,
                                               weights(dy, lddy, a, f, d, f, dw2, dw2, d)));
-  return launch_dense<M_DENSE_DW, P_BWD_DW13>(s, dt, g.dw13, T, F,
-                                              weights(dh, F, x, ldx, F, d, dw1, dw3, f));
+  MOE_TRY(launch_dense<M_DENSE_DW, P_BWD_DW13>(s, dt, g.dw13, T, F,
+                                               weights(dh, F, x, ldx, F, d, dw1, dw3, f)));
+
+  // dX = add + [dH1 | dH3] [W1; W3], last: it may be written over dY or X
+  GemmParams q{};
+  q.A = dh;
+  q.lda = F * es;
+  q.K = F;
+  q.N = d;
+  q.C = static_cast<char*>(dx);
+  q.ldc = lddx * es;
+  q.add = static_cast<const char*>(add);
+  q.ldadd = ldadd * es;
+  q.partial = partial;
+  if (g.wt) {
+    MOE_TRY(launch_transpose_w(s, 1, w1, w3, f, f, d, wt13));
+    q.B = wt13;
+    q.ldb = F * es;
+    return launch_dense<M_ADD_STORE, P_BWD_DX_T>(s, dt, g.dx, T, T, q);
+  }
+  q.B = static_cast<const char*>(w1);
+  q.B2 = static_cast<const char*>(w3);
+  q.kmsplit = f;
+  q.ldb = d * es;
+  return launch_dense<M_ADD_STORE, P_BWD_DX>(s, dt, g.dx, T, T, q);
 }

@@ -214,3 +214,29 @@ def test_addend_may_be_the_output():
     B.moe_gated_ffn_fwd(B.MOE_SWIGLU, P["x"], P["w1"], P["w3"], P["w2"], z,
                         B.workspace(B.moe_gated_ffn_fwd_workspace_bytes(B.MOE_BF16, 40, 64, 72), dev()), add=z)
     assert torch.equal(y.contiguous(), z)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("T,d,f", [(40, 64, 72), (777, 520, 264), (777, 40, 2056), (2056, 1032, 520)])
+def test_outputs_over_inputs(T, d, f, dt):
+    """y over x, and dx over dy, x or the addend, with the bits of separate outputs (products
+    whole and with K split)."""
+    P = _problem(T, d, f, dt, pad=8)
+    w, act = (P["w1"], P["w3"], P["w2"]), B.MOE_GELU_TANH
+    y, h = _forward(P, "gelu_tanh", dt, add=False, pad=8)
+    wider = lambda t: torch.cat([t, torch.full_like(t[:, :8], 3)], 1)
+    x = wider(P["x"])
+    B.moe_gated_ffn_fwd(act, x[:, :d], *w, x[:, :d],
+                        B.workspace(B.moe_gated_ffn_fwd_workspace_bytes(CODE[dt], T, d, f), dev()))
+    assert torch.equal(x[:, :d], y) and (x[:, d:] == 3).all()
+    ws = B.workspace(B.moe_gated_ffn_bwd_workspace_bytes(CODE[dt], T, d, f), dev())
+
+    def backward(**over):
+        t = dict({n: wider(P[n])[:, :d] for n in ("x", "dy", "dx_add")})
+        dx = t[over["dx"]] if over else torch.empty_like(P["x"])
+        dw = [torch.empty_like(v) for v in w]
+        B.moe_gated_ffn_bwd(act, t["x"], h, *w, t["dy"], dx, *dw, ws, add=t["dx_add"])
+        return [dx] + dw
+    want = backward()
+    for n in ("dy", "x", "dx_add"):
+        assert all(torch.equal(a, b) for a, b in zip(backward(dx=n), want)), n
