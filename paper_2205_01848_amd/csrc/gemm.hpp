@@ -1073,6 +1073,23 @@ __device__ __forceinline__ void epilogue16(const GemmParams& p,
     }
   } else {
     constexpr int LR = WC / 8, RG = 64 / LR;   // lanes per row, rows per pass
+    // the addend's rows, kPf passes ahead of their use, as the factors above
+    constexpr int GB = 16 / RG, kIt = C::RB * GB, kPf = kIt < 4 ? kIt : 4, kRing = kPf + 1;
+    uint4 qa[kRing];
+    const bool adds = MODE == M_ADD_STORE && p.add && slot < 0;
+    auto issue = [&](int n) {
+      const int lm = wr0 + 16 * (n / GB) + RG * (n % GB) + el / LR, gc = n0 + wn * WC + (el % LR) * 8;
+      const bool ok = lm < m_valid && gc < p.N;
+      qa[n % kRing] = *reinterpret_cast<const uint4*>(
+          p.add + static_cast<int64_t>(row0 + (ok ? lm : 0)) * p.ldadd +
+          static_cast<int64_t>(ok ? gc : n0) * ES);
+    };
+    if constexpr (MODE == M_ADD_STORE) {
+      if (adds) {
+#pragma unroll
+        for (int n = 0; n < kPf; ++n) issue(n);
+      }
+    }
 #pragma unroll
     for (int i = 0; i < C::RB; ++i) {
       stage16<C>(strip, acc, i, el);
@@ -1081,6 +1098,9 @@ __device__ __forceinline__ void epilogue16(const GemmParams& p,
         const int r = RG * it + el / LR, c8 = (el % LR) * 8;
         const int lm = wr0 + 16 * i + r;
         const int gc = n0 + wn * WC + c8;
+        if constexpr (MODE == M_ADD_STORE) {
+          if (adds && GB * i + it + kPf < kIt) issue(GB * i + it + kPf);
+        }
         if (lm < m_valid && gc < p.N) {
           const float* sp = strip + r * kP + c8;
           if constexpr (is_dw(MODE)) {
@@ -1103,9 +1123,9 @@ __device__ __forceinline__ void epilogue16(const GemmParams& p,
                 *reinterpret_cast<float4*>(dst + 4) = make_float4(v[4], v[5], v[6], v[7]);
                 continue;
               }
-              if (p.add) {
+              if (adds) {
                 float b[8];
-                unpack8(*reinterpret_cast<const uint4*>(p.add + grow * p.ldadd + static_cast<int64_t>(gc) * ES), b);
+                unpack8(qa[(GB * i + it) % kRing], b);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] += b[e];
               }
@@ -1731,9 +1751,25 @@ __device__ __forceinline__ void epilogue_f32(const GemmParams& p, const MidTile&
   for (int i = 0; i < NB; ++i) {
     const int blk = GATED ? 2 * i + (wave >> 1) : i;
     if (GATED && blk >= RB) continue;
+    auto row_of = [&](int q) { return blk * 32 + 8 * (q >> 2) + 4 * (lane >> 5) + (q & 3); };
+    // what the dense block's epilogues read, the whole block's before its first store
+    // (rows behind the last one: the last one again)
+    float u1[16], u3[16];
+    if constexpr (MODE == M_GATED_DA || MODE == M_ADD_STORE) {
+#pragma unroll
+      for (int q = 0; q < 16; ++q) {
+        const int64_t row = t.row0 + min(row_of(q), t.m_valid - 1);
+        if constexpr (MODE == M_GATED_DA) {
+          u1[q] = reinterpret_cast<const float*>(p.H1 + row * p.ldh)[col];
+          u3[q] = reinterpret_cast<const float*>(p.H3 + row * p.ldh)[col];
+        } else {
+          u1[q] = p.add && t.slot < 0 ? reinterpret_cast<const float*>(p.add + row * p.ldadd)[col] : 0.f;
+        }
+      }
+    }
 #pragma unroll
     for (int q = 0; q < 16; ++q) {
-      const int lm = blk * 32 + 8 * (q >> 2) + 4 * (lane >> 5) + (q & 3);
+      const int lm = row_of(q);
       if (lm >= t.m_valid) continue;
       const int64_t row = t.row0 + lm;
       if constexpr (VARK) {
@@ -1761,15 +1797,14 @@ __device__ __forceinline__ void epilogue_f32(const GemmParams& p, const MidTile&
           }
           *c = g * h3;
         } else if constexpr (MODE == M_GATED_DA) {
-          *c = acc[i][q] * reinterpret_cast<const float*>(p.H1 + row * p.ldh)[col];
-          c[p.f] = acc[i][q] * reinterpret_cast<const float*>(p.H3 + row * p.ldh)[col];
+          *c = acc[i][q] * u1[q];
+          c[p.f] = acc[i][q] * u3[q];
         } else if constexpr (MODE == M_ADD_STORE) {
           if (t.slot >= 0) {
             p.partial[t.slot * p.slot_elems + row * p.N + col] = acc[i][q];
             continue;
           }
-          const float b = p.add ? reinterpret_cast<const float*>(p.add + row * p.ldadd)[col] : 0.f;
-          *c = acc[i][q] + b;
+          *c = acc[i][q] + u1[q];
         } else if constexpr (MODE == M_FWD1) {
           if (p.H1) reinterpret_cast<float*>(p.H1 + row * p.ldh)[col] = acc[i][q];
           *c = act_f(acc[i][q], p.act);
