@@ -224,6 +224,8 @@ __global__ __launch_bounds__(kThreads16, RB <= 2 ? 2 : 1) void ffn_gemm16_deep_k
       op.b = {p.B + o, GATED ? p.B2 + o : nullptr, p.ldb, min(GATED ? TN / 2 : TN, p.N - n0), 0};
       op.K = p.K;
     }
+    std::conditional_t<is_i8(MODE), ScalesI8<MODE, C>, int> sc;   // read beside the first stages
+    if constexpr (is_i8(MODE)) sc.load(p, lane, wm, wn, g, row0, m_valid, n0);
     floatx4 acc[RB][4];
     if constexpr (NS == 3) {
       char *const sa[3] = {a0, a1, a2}, *const sb[3] = {b0, b1, b2};
@@ -234,7 +236,7 @@ __global__ __launch_bounds__(kThreads16, RB <= 2 ? 2 : 1) void ffn_gemm16_deep_k
     }
     float* strip = reinterpret_cast<float*>((wave < 2 ? b0 : b1) + (wave & 1) * C::kStripBytes);
     if constexpr (is_i8(MODE))
-      epilogue_i8<MODE, C>(p, acc, strip, row_scales<C>(b0, b1, wave), lane, wm, wn, g, row0, m_valid, n0);
+      epilogue_i8<MODE, C>(p, acc, sc, strip, row_scales<C>(b0, b1, wave), lane, wm, wn, g, row0, m_valid, n0);
     else
       epilogue16<MODE, C>(p, acc, strip, lane, wm, wn, g, slot, row0, m_valid, n0, false);
     __syncthreads();   // strips are free before the next tile's loads
