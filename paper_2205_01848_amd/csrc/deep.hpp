@@ -61,8 +61,8 @@ __device__ __forceinline__ void mma16(floatx4& c, const uint4& a, const uint4& b
 // K-major k-rows r with r & 8 also have the two 16-element halves of every 32-element
 // segment swapped: a transpose read takes half a segment of k-rows r .. r + 3 and of
 // r + 8 .. r + 11 at once, which would otherwise lie on the same banks (2048 tokens,
-// 1024 -> 2816: the backward's dX 43.4 -> 39.4 us, dW 31.6 -> 31.0.  In tiles of 256,
-// bound by other things, the swap gains nothing and is not made.)
+// 1024 -> 2816: the backward's dX 43.4 -> 39.4 us.  The mid and the 256x256 kernels,
+// bound by other things, gain 0 to 1 % by it and do without.)
 template <int RB, int NS, int ALAY, int BLAY, bool GATED, int ES>
 __device__ __forceinline__ void mainloop_deep(const TileOps& op, char* const (&sa)[NS],
                                               char* const (&sb)[NS], floatx4 (&acc)[RB][4]) {
