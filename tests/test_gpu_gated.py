@@ -240,3 +240,48 @@ def test_outputs_over_inputs(T, d, f, dt):
     want = backward()
     for n in ("dy", "x", "dx_add"):
         assert all(torch.equal(a, b) for a, b in zip(backward(dx=n), want)), n
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [12, 530])
+def test_rows_as_far_apart_as_allowed(T, dt):
+    """Rows 8 MB apart, so that offsets pass 32 bits: the bits of contiguous rows."""
+    d, f, act = 72, 136, B.MOE_SWIGLU
+    P = _problem(T, d, f, dt)
+    w = (P["w1"], P["w3"], P["w2"])
+    y, h = _forward(P, "swiglu", dt)
+    ws = [B.workspace(q(CODE[dt], T, d, f), dev()) for q in (B.moe_gated_ffn_fwd_workspace_bytes,
+                                                             B.moe_gated_ffn_bwd_workspace_bytes)]
+    dx, dw = torch.empty_like(P["x"]), [torch.empty_like(v) for v in w]
+    B.moe_gated_ffn_bwd(act, P["x"], h, *w, P["dy"], dx, *dw, ws[1], add=P["dx_add"])
+    es = P["x"].element_size()
+    far = torch.empty(T * ((1 << 23) - 64) // es, dtype=DT[dt], device=dev()).view(T, -1)
+    V = {n: far[:, i * d:(i + 1) * d] for i, n in enumerate(("x", "dy", "add", "dx_add", "y", "dx"))}
+    for n in ("x", "dy", "add", "dx_add"):
+        V[n].copy_(P[n])
+    h2, dw2 = torch.empty_like(h), [torch.empty_like(v) for v in w]
+    B.moe_gated_ffn_fwd(act, V["x"], *w, V["y"], ws[0], add=V["add"], h_save=h2)
+    B.moe_gated_ffn_bwd(act, V["x"], h2, *w, V["dy"], V["dx"], *dw2, ws[1], add=V["dx_add"])
+    assert torch.equal(V["y"], y) and torch.equal(V["dx"], dx) and torch.equal(h2, h)
+    assert all(torch.equal(a, b) for a, b in zip(dw, dw2))
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("T,d,f", [(1, 2056, 72), (40, 64, 72), (100, 40, 8200), (777, 136, 2056), (2056, 1032, 520)])
+def test_workspace_is_all_that_is_written(T, d, f, dt):
+    """The bytes behind a workspace of the queried size stay as they were."""
+    P = _problem(T, d, f, dt)
+    w = (P["w1"], P["w3"], P["w2"])
+
+    def guarded(size):
+        buf = torch.full((size + (1 << 20),), 77, dtype=torch.uint8, device=dev())
+        return buf[:size], buf[size:]
+    y, dx = torch.empty_like(P["x"]), torch.empty_like(P["x"])
+    h, dw = torch.empty(3, T, f, dtype=DT[dt], device=dev()), [torch.empty_like(v) for v in w]
+    ws, behind = guarded(B.moe_gated_ffn_fwd_workspace_bytes(CODE[dt], T, d, f))
+    B.moe_gated_ffn_fwd(B.MOE_SWIGLU, P["x"], *w, y, ws)
+    B.moe_gated_ffn_fwd(B.MOE_SWIGLU, P["x"], *w, y, ws, h_save=h)
+    assert (behind == 77).all()
+    ws, behind = guarded(B.moe_gated_ffn_bwd_workspace_bytes(CODE[dt], T, d, f))
+    B.moe_gated_ffn_bwd(B.MOE_SWIGLU, P["x"], h, *w, P["dy"], dx, *dw, ws)
+    assert (behind == 77).all()

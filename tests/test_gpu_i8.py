@@ -275,3 +275,61 @@ def test_ffn_few_rows(T, k, rows, d, f, dt, act):
                                        None if s3 is None else s3[e], part(w2, f), s2[e], act, dt)
         assert (np.abs(got[r] - ref) <= slack_e * 1.001 + np.abs(ref) * (4 * U32 + ROUND[dt]) + 1e-30).all()
     assert (got[~used] == 3).all()
+
+
+def test_quantize_rows_far_apart():
+    """Rows 64 MB apart, past 2^31 elements: the bits of contiguous rows."""
+    x = torch.randn(140, 72, device=dev()).to(torch.bfloat16)
+    far = torch.empty(140 << 25, dtype=torch.bfloat16, device=dev()).view(140, -1)[:, 8:80]
+    far.copy_(x)
+    out = []
+    for t in (x, far):
+        q, s = torch.empty(140, 80, dtype=torch.int8, device=dev()), torch.empty(140, device=dev())
+        B.moe_quantize_rows(t, q, s)
+        out.append((q, s))
+    assert all(torch.equal(a, b) for a, b in zip(*out))
+
+
+@pytest.mark.parametrize("each", [2, 40])
+def test_weights_past_32_bits(tiles, each):
+    """Five experts of 1 GiB of weights: the bits of a call for each expert alone (the sums are exact)."""
+    E, K, N, R = 5, 16384, 65536, 5 * each
+    wq = torch.randint(-127, 128, (E, N, K), dtype=torch.int8, device=dev())
+    xq, xs = torch.randint(-127, 128, (R, K), dtype=torch.int8, device=dev()), torch.rand(R, device=dev())
+    ws, y = torch.rand(E, N, device=dev()), torch.empty(R, N, device=dev())
+    idx = lambda *v: torch.tensor(v, dtype=torch.int32, device=dev())
+    buf = B.workspace(B.moe_expert_matmul_i8_workspace_bytes(E, N, R), dev())
+    B.moe_expert_matmul_i8(idx(*range(0, R + 1, each)), idx(*[each] * E), xq, xs, wq, ws, y, buf)
+    one = torch.empty(each, N, device=dev())
+    for e in range(E):
+        r = slice(e * each, (e + 1) * each)
+        B.moe_expert_matmul_i8(idx(0, each), idx(each), xq[r], xs[r], wq[e:e + 1], ws[e:e + 1], one, buf)
+        assert torch.equal(y[r], one), e
+    # and a few columns of the last expert against whole numbers
+    c = [0, N // 2 + 1, N - 1]
+    exact = xq[-1].cpu().long() @ wq[-1, c].cpu().long().T
+    ref = exact.double() * xs[-1].item() * ws[-1, c].cpu().double()
+    assert ((y[-1, c].cpu().double() - ref).abs() <= 3.01 * U32 * ref.abs()).all()
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,d,f", [([3, 0, 5], 72, 200), ([70, 1, 300], 136, 1000), ([500, 900, 40], 264, 520)])
+def test_workspace_is_all_that_is_written(tiles, rows, d, f, dt):
+    """The bytes behind a workspace of the queried size stay as they were."""
+    rng = np.random.default_rng(d)
+    E, R = len(rows), sum(rows)
+    off = np.concatenate([[0], np.cumsum(rows)])
+    xq, xs = _quantised(rng, d, R)
+    w1, s1 = _quantised(rng, d, E, f)
+    w2, s2 = _quantised(rng, f, E, d)
+    code = B.MOE_BF16 if dt == "bf16" else B.MOE_F32
+    size = B.moe_ffn_fwd_i8_workspace_bytes(code, B.MOE_RELU, E, d, f, R)
+    buf = torch.full((size + (1 << 20),), 77, dtype=torch.uint8, device=dev())
+    i = [_d(np.asarray(a, np.int32)) for a in (off, rows)]
+    B.moe_expert_ffn_fwd_i8(B.MOE_RELU, *i, _d(xq), _d(xs), _d(w1), _d(s1), None, None, _d(w2), _d(s2),
+                            torch.empty(R, d, dtype=DT[dt], device=dev()), buf[:size])
+    assert (buf[size:] == 77).all()
+    size = B.moe_expert_matmul_i8_workspace_bytes(E, f, R)
+    buf = torch.full((size + (1 << 20),), 77, dtype=torch.uint8, device=dev())
+    B.moe_expert_matmul_i8(*i, _d(xq), _d(xs), _d(w1), _d(s1), torch.empty(R, f, dtype=DT[dt], device=dev()), buf[:size])
+    assert (buf[size:] == 77).all()
