@@ -55,7 +55,7 @@ __device__ __forceinline__ void mma16(floatx4& c, const uint4& a, const uint4& b
 }
 
 // acc += A_tile * B_tile^T: wave w owns tile rows 16 RB (w >> 1) .. and columns
-// 64 (w & 1) .. +63.  LDS tiles, swizzles, loads and fragments are those of the
+// 64 (w & 1) .. +63, over the nk K steps from k_first on.  LDS tiles, swizzles, loads and fragments are those of the
 // mid kernel (gemm.hpp): K-contiguous tiles as rows of 128 bytes, K-major ones as k-rows
 // of 128 elements (K-major A: RB = 4).
 // K-major k-rows r with r & 8 also have the two 16-element halves of every 32-element
@@ -64,19 +64,19 @@ __device__ __forceinline__ void mma16(floatx4& c, const uint4& a, const uint4& b
 // 1024 -> 2816: the backward's dX 43.4 -> 39.4 us.  The mid and the 256x256 kernels,
 // bound by other things, gain 0 to 1 % by it and do without.)
 template <int RB, int NS, int ALAY, int BLAY, bool GATED, int ES>
-__device__ __forceinline__ void mainloop_deep(const TileOps& op, char* const (&sa)[NS],
-                                              char* const (&sb)[NS], floatx4 (&acc)[RB][4]) {
+__device__ __forceinline__ void mainloop_deep(const TileOps& op, int wave, int k_first, int nk,
+                                              char* const (&sa)[NS], char* const (&sb)[NS],
+                                              floatx4 (&acc)[RB][4]) {
   static_assert(ALAY == L_KC || RB == 4, "K-major A tiles are 128 columns wide");
   static_assert(ES == 2 || (ALAY == L_KC && BLAY == L_KC), "int8 operands are K-contiguous");
   constexpr int KSTEP = kRowBytes / ES, KMROW = 256;
   const int lane = static_cast<int>(threadIdx.x) & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
   const int wm = wave >> 1, wn = wave & 1;
 #pragma unroll
   for (int i = 0; i < RB; ++i)
 #pragma unroll
     for (int j = 0; j < 4; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
-  const int K = op.K, nk = (K + KSTEP - 1) / KSTEP;
+  const int K = op.K;
 
   // ---- loads: of every stage, wave w loads the 1 KB blocks 4i + w of A
   // (i < RB) and of B (i < 4); a lane's offset has bit 31 set where it would
@@ -113,6 +113,7 @@ __device__ __forceinline__ void mainloop_deep(const TileOps& op, char* const (&s
     __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, MOE_LDS(dst), 16, off, soff, 0, 0);
   };
   auto load = [&](int kt, char* da, char* db) {
+    kt += k_first;
     const uint32_t kbad = bad(kt * kRowBytes + co >= K * ES);
     if constexpr (ALAY == L_KC) {
 #pragma unroll
@@ -178,19 +179,27 @@ __device__ __forceinline__ void mainloop_deep(const TileOps& op, char* const (&s
   ring_steps<NS, RB + 4>(nk, sa, sb, load, compute);
 }
 
-template <int MODE, int PASS, int RB, int NS>
-__global__ __launch_bounds__(kThreads16, RB <= 2 ? 2 : 1) void ffn_gemm16_deep_kernel(const GroupParams gp) {
+// KG = 2 (64 rows, dense): a second group of four wavefronts takes the second half of
+// the K steps into stages of its own, and its sums are added through LDS at the end.
+// A wavefront alone on its SIMD waits for its fragments between the matrix
+// instructions; two overlap.  For tiles that leave every CU one workgroup (2048
+// tokens, 2816 -> 1024: Y 25.8 -> 24.6, dX 39.3 -> 34.8 us; six stages for one group instead:
+// 25.3 and 42.2).
+template <int MODE, int PASS, int RB, int NS, int KG>
+__global__ __launch_bounds__(KG * kThreads16, RB <= 2 ? 2 : 1) void ffn_gemm16_deep_kernel(const GroupParams gp) {
   constexpr bool GATED = is_gated(MODE), DENSE = is_dense(MODE), VARK = is_dw(MODE);
   constexpr int ES = op_bytes(MODE), TM = 32 * RB, TN = kMidN;
   constexpr int kA = TM * kRowBytes, kB = TN * kRowBytes;
   using C = Tile16<RB, 4>;
   // one object per stage, so that the compiler can tell the loads into one
   // from the reads of another
-  __shared__ __attribute__((aligned(16))) char a0[kA], b0[kB], a1[kA], b1[kB], a2[kA], b2[kB];
+  __shared__ __attribute__((aligned(16))) char a0[KG * kA], b0[KG * kB], a1[KG * kA], b1[KG * kB],
+      a2[KG * kA], b2[KG * kB];
   __shared__ __attribute__((aligned(16))) char a3[NS > 3 ? kA : 16], b3[NS > 3 ? kB : 16];
   const GemmParams& p = gp.p;
   const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
+  const int wave8 = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
+  const int wave = wave8 & 3, kg = wave8 >> 2, ga = KG > 1 ? kg * kA : 0, gb = KG > 1 ? kg * kB : 0;
   const int wm = wave >> 1, wn = wave & 1;
   int my_first = 0, my_rows = 0, my_end = 0, n_mt = 0;
   if constexpr (!DENSE) {
@@ -227,18 +236,38 @@ __global__ __launch_bounds__(kThreads16, RB <= 2 ? 2 : 1) void ffn_gemm16_deep_k
     std::conditional_t<is_i8(MODE), ScalesI8<MODE, C>, int> sc;   // read beside the first stages
     if constexpr (is_i8(MODE)) sc.load(p, lane, wm, wn, g, row0, m_valid, n0);
     floatx4 acc[RB][4];
+    const int steps = ((op.K * ES + kRowBytes - 1) / kRowBytes + KG - 1) / KG;
     if constexpr (NS == 3) {
-      char *const sa[3] = {a0, a1, a2}, *const sb[3] = {b0, b1, b2};
-      mainloop_deep<RB, NS, a_layout(PASS), b_layout(PASS), GATED, ES>(op, sa, sb, acc);
+      char *const sa[3] = {a0 + ga, a1 + ga, a2 + ga}, *const sb[3] = {b0 + gb, b1 + gb, b2 + gb};
+      mainloop_deep<RB, NS, a_layout(PASS), b_layout(PASS), GATED, ES>(op, wave, kg * steps, steps, sa, sb, acc);
     } else {
       char *const sa[4] = {a0, a1, a2, a3}, *const sb[4] = {b0, b1, b2, b3};
-      mainloop_deep<RB, NS, a_layout(PASS), b_layout(PASS), GATED, ES>(op, sa, sb, acc);
+      mainloop_deep<RB, NS, a_layout(PASS), b_layout(PASS), GATED, ES>(op, wave, 0, steps, sa, sb, acc);
     }
-    float* strip = reinterpret_cast<float*>((wave < 2 ? b0 : b1) + (wave & 1) * C::kStripBytes);
-    if constexpr (is_i8(MODE))
-      epilogue_i8<MODE, C>(p, acc, sc, strip, row_scales<C>(b0, b1, wave), lane, wm, wn, g, row0, m_valid, n0);
-    else
-      epilogue16<MODE, C>(p, acc, strip, lane, wm, wn, g, slot, row0, m_valid, n0, false);
+    if constexpr (KG > 1) {
+      static_assert(DENSE && NS == 3 && RB * 4 * 16 * kThreads16 <= KG * kB, "the sums fit a stage of B");
+      floatx4* sums = reinterpret_cast<floatx4*>(b2) + (threadIdx.x & (kThreads16 - 1));
+      if (kg) {
+#pragma unroll
+        for (int i = 0; i < RB; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) sums[(i * 4 + j) * kThreads16] = acc[i][j];
+      }
+      __syncthreads();
+      if (!kg) {
+#pragma unroll
+        for (int i = 0; i < RB; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) acc[i][j] += sums[(i * 4 + j) * kThreads16];
+      }
+    }
+    if (KG == 1 || !kg) {
+      float* strip = reinterpret_cast<float*>((wave < 2 ? b0 : b1) + (wave & 1) * C::kStripBytes);
+      if constexpr (is_i8(MODE))
+        epilogue_i8<MODE, C>(p, acc, sc, strip, row_scales<C>(b0, b1, wave), lane, wm, wn, g, row0, m_valid, n0);
+      else
+        epilogue16<MODE, C>(p, acc, strip, lane, wm, wn, g, slot, row0, m_valid, n0, false);
+    }
     __syncthreads();   // strips are free before the next tile's loads
   }
 }
@@ -297,8 +326,15 @@ moe_status launch_deep(hipStream_t s, moe_dtype dt, const GroupParams& gp, int64
       return MOE_OK;
     }
   }
+  if constexpr (RB == 2 && is_dense(MODE) && !is_dw(MODE)) {
+    if (most_items <= persistent_grid()) {
+      ffn_gemm16_deep_kernel<MODE, PASS, RB, 3, 2><<<grid, 2 * kThreads16, 0, s>>>(gp);
+      MOE_LAUNCH_CHECK();
+      return MOE_OK;
+    }
+  }
   if constexpr (!is_dw(MODE) || RB == 4)
-    ffn_gemm16_deep_kernel<MODE, PASS, RB, kDeepStages<RB>><<<grid, kThreads16, 0, s>>>(gp);
+    ffn_gemm16_deep_kernel<MODE, PASS, RB, kDeepStages<RB>, 1><<<grid, kThreads16, 0, s>>>(gp);
   MOE_LAUNCH_CHECK();
   return MOE_OK;
 }
