@@ -81,7 +81,7 @@ class MoELayer:
         self.rows_alloc = int(rows_alloc)
         self.dev = torch.device(device)
         self.has_gate = gate
-        dt = B.MOE_BF16 if dtype == torch.bfloat16 else B.MOE_F32
+        self.dt = dt = B.MOE_BF16 if dtype == torch.bfloat16 else B.MOE_F32
         i32, f32 = torch.int32, torch.float32
         e = lambda *s, t=dtype: torch.empty(*s, dtype=t, device=self.dev)
         R = self.rows_alloc
@@ -185,10 +185,16 @@ class MoELayer:
 
     # ---- shared expert ------------------------------------------------------------
     def shared_fwd(self, x, shared):
-        """y += the shared expert's output, shared = (w1 [sf, d], w3 [sf, d], w2 [d, sf])."""
+        """y += the shared expert's output for the tokens of x (the layer's T, or fewer: then the
+        first rows of y), shared = (w1 [sf, d], w3 [sf, d], w2 [d, sf])."""
         self._need_shared(shared)
-        B.moe_gated_ffn_fwd(self.shared_act, x, *shared, self.y, self.ws_shared, add=self.y,
-                            h_save=self.sh_save)
+        n, y, ws = x.shape[0], self.y, self.ws_shared
+        if n < self.T:
+            y = y[:n]
+            need = B.moe_gated_ffn_fwd_workspace_bytes(self.dt, n, self.d, self.shared_f)
+            if need > ws.numel():     # fewer tokens may split K into more ranges
+                ws = B.workspace(need, self.dev)
+        B.moe_gated_ffn_fwd(self.shared_act, x, *shared, y, ws, add=y, h_save=self.sh_save)
 
     def shared_bwd(self, x, dy, shared):
         """dx += the shared expert's part; its weight gradients go to dsw1, dsw3, dsw2."""

@@ -1,0 +1,55 @@
+"""The shared expert and the int8 forward inside MoELayer, on the host (no GPU: the library
+calls are replaced by a record of their arguments): they work on the tokens of x, whatever
+the layer's buffers hold behind them."""
+import pytest
+import torch
+
+from paper_2205_01848_amd import MoELayer, rows_alloc_for
+from paper_2205_01848_amd import binding as B
+
+T, d, E, k, f = 8, 24, 4, 2, 32
+CALLS = ["moe_gate_topk", "moe_quantize_rows", "moe_count", "moe_update_capacity", "moe_dispatch", "moe_route",
+         "moe_expert_ffn_fwd", "moe_expert_ffn_fwd_i8", "moe_combine", "moe_gated_ffn_fwd"]
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    seen = []
+    for name in CALLS:
+        monkeypatch.setattr(B, name, lambda *a, _n=name, **kw: seen.append((_n, a, kw)))
+    return seen
+
+
+def _layer(cls=MoELayer, **kw):
+    return cls(T, d, E, k, f, "relu", torch.float32, rows_alloc_for("dynamic", T, k, E, 5, 4), device="cpu", **kw)
+
+
+def _args(calls, name):
+    found = [(a, kw) for n, a, kw in calls if n == name]
+    assert len(found) == 1, [n for n, _, _ in calls]
+    return found[0]
+
+
+SHARED = (torch.zeros(16, d), torch.zeros(16, d), torch.zeros(d, 16))
+
+
+@pytest.mark.parametrize("n", [0, 1, 5])
+@pytest.mark.parametrize("backward", [False, True])
+def test_a_forward_of_fewer_tokens_has_its_shared_expert(calls, n, backward):
+    L = _layer(shared_f=16, backward=backward)
+    L.forward(torch.zeros(n, d), torch.zeros(E, f, d), None, torch.zeros(E, d, f), w_g=torch.zeros(E, d), shared=SHARED)
+    a, kw = _args(calls, "moe_gated_ffn_fwd")
+    assert a[1].shape == a[5].shape == kw["add"].shape == (n, d)
+    assert a[5].data_ptr() == L.y.data_ptr() or n == 0
+    assert a[6].numel() >= B.moe_gated_ffn_fwd_workspace_bytes(B.MOE_F32, n, d, 16)
+
+
+def test_the_shared_workspace_of_fewer_tokens(calls):
+    """Fewer tokens may split K into more ranges and so need more workspace than all of them."""
+    most, wide, sf = 1500, 8192, 8192
+    need = {n: B.moe_gated_ffn_fwd_workspace_bytes(B.MOE_BF16, n, wide, sf) for n in (1, 100, 1024, most)}
+    assert need[1024] > need[most]
+    L = MoELayer(most, wide, E, k, f, "relu", torch.bfloat16, 1, device="cpu", shared_f=sf)
+    for n, least in need.items():
+        L.shared_fwd(torch.zeros(n, wide, dtype=torch.bfloat16), (torch.zeros(sf, 1).expand(sf, wide), None, None))
+        assert calls[-1][1][6].numel() >= least, n
