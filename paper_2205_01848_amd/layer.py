@@ -357,26 +357,38 @@ class MoELayer:
         gate (or cached ids) in the layer dtype -> quantise x, a scale per
         token -> count, capacity, dispatch of the quantised rows (half the
         bytes of bf16) -> int8 FFN -> combine [-> shared expert in the layer
-        dtype].  Arguments as for forward; no backward follows it."""
+        dtype].  x holds the layer's T tokens or fewer (with ids, weights
+        [tokens, k]), and only those are routed and returned.  Arguments as for
+        forward, whose padded rows, lagged counts and balance term it does not
+        take; no backward follows it."""
         T, d, E, k, R = self.T, self.d, self.E, self.k, self.rows_alloc
         if (experts.E, experts.f, experts.d) != (E, self.f, d):
             raise ValueError(f"quantised experts of sizes {(experts.E, experts.f, experts.d)}, the "
                              f"layer's are {(E, self.f, d)}")
+        if x.dim() != 2 or x.shape[1] != d or x.shape[0] > T:
+            raise ValueError(f"x has shape {tuple(x.shape)}, the layer takes up to {T} rows of {d}")
+        n = x.shape[0]
+        if ids is not None and tuple(ids.shape) != (n, k):
+            raise ValueError(f"ids have shape {tuple(ids.shape)}, expected {(n, k)}")
         if self.xq is None:
             width = B.quantized_width(d)
             new = lambda rows: torch.empty(rows, width, dtype=torch.int8, device=self.dev)
             self.xq, self.xq_disp = new(T), new(max(R, 1))
             self.xq_scale = torch.empty(T, dtype=torch.float32, device=self.dev)
-            dt = B.MOE_BF16 if self.dtype == torch.bfloat16 else B.MOE_F32
-            self.ws_i8 = B.workspace(B.moe_ffn_fwd_i8_workspace_bytes(dt, self.act, E, d, self.f, R),
+            self.ws_i8 = B.workspace(B.moe_ffn_fwd_i8_workspace_bytes(self.dt, self.act, E, d, self.f, R),
                                      self.dev)
         self._balance_on = False
         if ids is None:
             self.gate(x, w_g, bias, renorm)
             ids, weights = self.ids, self.weights
-        B.moe_quantize_rows(x, self.xq, self.xq_scale)
+        elif weights is None:
+            weights = self.weights
+        xq, scale = self.xq, self.xq_scale
+        if n < T:
+            xq, scale, ids = xq[:n], scale[:n], ids[:n]
+        B.moe_quantize_rows(x, xq, scale)
         # the dispatch moves rows of 16-byte vectors: two int8 values ride as one bf16
-        rows, disp = self.xq.view(torch.bfloat16), self.xq_disp.view(torch.bfloat16)
+        rows, disp = xq.view(torch.bfloat16), self.xq_disp.view(torch.bfloat16)
         kind, num, den = capacity
         if kind == "policy":
             B.moe_dispatch(rows, ids, E, self.capacity, self.offsets, R, self.counts, self.fill,
@@ -386,13 +398,18 @@ class MoELayer:
                         self.counts, self.fill, self.dest_row, self.src, disp, self.status,
                         self.ws_dispatch, row_align=self.row_align)
         q = experts
-        B.moe_expert_ffn_fwd_i8(self.act, self.offsets, self.fill, self.xq_disp[:R], self.xq_scale,
+        B.moe_expert_ffn_fwd_i8(self.act, self.offsets, self.fill, self.xq_disp[:R], scale,
                                 q.w1, q.s1, q.w3, q.s3, q.w2, q.s2, self.y_disp, self.ws_i8,
                                 src=self.src, k=k)
-        self.combine(weights)
+        y = self.y
+        if n < T:
+            y = y[:n]
+            B.moe_combine(self.y_disp, self.dest_row[:n], weights, y)
+        else:
+            self.combine(weights)
         if shared is not None:
             self.shared_fwd(x, shared)
-        return self.y
+        return y
 
     def forward_cached(self, x, w1, w3, w2, *, cached, cache_out, unchanged, w_g, bias=None,
                        renorm=0, capacity=("dynamic", 1, 1), gate_stream=None, rows="fill",

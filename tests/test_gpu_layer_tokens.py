@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from gpu_util import torch_dtype
-from paper_2205_01848_amd import MoELayer
+from paper_2205_01848_amd import MoELayer, QuantizedExperts
 from test_gpu_layer_blocks import CAP, _gate, _setup
 
 pytestmark = pytest.mark.gpu
@@ -24,3 +24,28 @@ def test_shared_expert_on_fewer_tokens(dt, n):
     x = dv["dy"][:n].contiguous()
     y = L.forward(x, *w, **_gate(dv, wl), shared=dv["shared"])[:n]
     assert torch.equal(y, _of(L, wl, n, dt).forward(x, *w, **_gate(dv, wl), shared=dv["shared"]))
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("act", ["swiglu", "relu"])
+@pytest.mark.parametrize("n", [0, 1, 7, 131, 300])
+@pytest.mark.parametrize("cap", [CAP, ("static", 1, 2)], ids=["dynamic", "static"])
+def test_int8_forward_of_fewer_tokens(dt, act, n, cap):
+    """The rows behind them stay out of the loads, the capacities, the status and y."""
+    wl, dv, L = _setup(dt, act, backward=False)
+    q, g = QuantizedExperts(dv["w1"], dv["w3"], dv["w2"]), dict(_gate(dv, wl), capacity=cap, shared=dv["shared"])
+    L.forward_i8(dv["x"], q, **g)
+    L.y.fill_(7)
+    L.status.zero_()
+    x = dv["dy"][:n].contiguous()
+    y = L.forward_i8(x, q, **g)
+    assert y.shape == (n, wl.d) and (L.y[n:] == 7).all() and L.status.item() == 0
+    small = _of(L, wl, n, dt)
+    assert torch.equal(y, small.forward_i8(x, q, **g))
+    for name in ("counts", "capacity", "offsets", "fill"):
+        assert torch.equal(getattr(L, name), getattr(small, name)), name
+    assert torch.equal(L.dest_row[:n], small.dest_row) and L.counts.sum().item() == n * wl.k
+    # the same picks from a cache
+    y = y.clone()
+    ids, weights = small.ids.clone(), small.weights.clone()
+    assert torch.equal(y, L.forward_i8(x, q, ids=ids, weights=weights, capacity=cap, shared=dv["shared"]))

@@ -53,3 +53,40 @@ def test_the_shared_workspace_of_fewer_tokens(calls):
     for n, least in need.items():
         L.shared_fwd(torch.zeros(n, wide, dtype=torch.bfloat16), (torch.zeros(sf, 1).expand(sf, wide), None, None))
         assert calls[-1][1][6].numel() >= least, n
+
+
+class Experts:
+    E, f, d = E, f, d
+    w1 = s1 = w3 = s3 = w2 = s2 = None
+
+
+@pytest.mark.parametrize("n", [0, 1, 5, T])
+@pytest.mark.parametrize("kind", ["static", "dynamic", "policy"])
+@pytest.mark.parametrize("cached", [False, True])
+def test_int8_forward_of_fewer_tokens(calls, n, kind, cached):
+    """None of the rows behind x's tokens is quantised, routed or combined."""
+    L = _layer(shared_f=16)
+    given = dict(ids=torch.zeros(n, k, dtype=torch.int32), weights=torch.zeros(n, k)) if cached else dict(w_g=torch.zeros(E, d))
+    y = L.forward_i8(torch.zeros(n, d), Experts, capacity=(kind, 5, 4), **given, shared=SHARED)
+    assert y.shape == (n, d) and (y.data_ptr() == L.y.data_ptr() or n == 0)
+    x, q, scale = _args(calls, "moe_quantize_rows")[0]
+    assert x.shape == (n, d) and q.shape == (n, 32) and scale.shape == (n,)
+    a = _args(calls, "moe_dispatch" if kind == "policy" else "moe_route")[0]
+    assert a[0].shape == (n, 16) and a[1].shape == (n, k)
+    a, kw = _args(calls, "moe_expert_ffn_fwd_i8")
+    assert a[4].shape == (n,) and kw["k"] == k
+    a = _args(calls, "moe_combine")[0]
+    assert a[1].shape == (n, k) and a[2].numel() >= n * k and a[3].shape == (n, d)
+    a, kw = _args(calls, "moe_gated_ffn_fwd")
+    assert a[1].shape == a[5].shape == kw["add"].shape == (n, d)
+
+
+def test_int8_forward_refuses_other_shapes(calls):
+    L, g = _layer(), dict(w_g=torch.zeros(E, d))
+    for x in (torch.zeros(T + 1, d), torch.zeros(T, d - 8), torch.zeros(T, d + 8), torch.zeros(T * d)):
+        with pytest.raises(ValueError, match="x has shape"):
+            L.forward_i8(x, Experts, **g)
+    for shape in ((T - 1, k), (T, k + 1), (T + 1, k), (T * k,)):
+        with pytest.raises(ValueError, match="ids"):
+            L.forward_i8(torch.zeros(T, d), Experts, ids=torch.zeros(*shape, dtype=torch.int32))
+    assert not calls
