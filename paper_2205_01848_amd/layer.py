@@ -165,7 +165,15 @@ class MoELayer:
         """count (dynamic), capacity and dispatch of this batch in one call."""
         B.moe_route(x, ids, self.E, dynamic, num, den, 0, self.rows_alloc, self.capacity,
                     self.offsets, self.counts, self.fill, self.dest_row, self.src, self.x_disp,
-                    self.status, self.ws_dispatch, row_align=self.row_align)
+                    self.status, self._ws_route(x.shape[0]), row_align=self.row_align)
+
+    def _ws_route(self, n: int):
+        """Workspace of moe_route on n tokens: fewer than T may take more of it (short batches
+        are routed by kernels of their own)."""
+        ws = self.ws_dispatch
+        if n < self.T and ws.numel() < B.moe_route_workspace_bytes(n, self.E, self.k):
+            ws = B.workspace(B.moe_route_workspace_bytes(n, self.E, self.k), self.dev)
+        return ws
 
     def ffn_fwd(self, w1, w3, w2, rows: str = "fill"):
         """rows="fill": the method, each expert over its kept rows.
@@ -396,7 +404,7 @@ class MoELayer:
         else:
             B.moe_route(rows, ids, E, kind != "static", num, den, 0, R, self.capacity, self.offsets,
                         self.counts, self.fill, self.dest_row, self.src, disp, self.status,
-                        self.ws_dispatch, row_align=self.row_align)
+                        self._ws_route(n), row_align=self.row_align)
         q = experts
         B.moe_expert_ffn_fwd_i8(self.act, self.offsets, self.fill, self.xq_disp[:R], scale,
                                 q.w1, q.s1, q.w3, q.s3, q.w2, q.s2, self.y_disp, self.ws_i8,

@@ -49,3 +49,17 @@ def test_int8_forward_of_fewer_tokens(dt, act, n, cap):
     y = y.clone()
     ids, weights = small.ids.clone(), small.weights.clone()
     assert torch.equal(y, L.forward_i8(x, q, ids=ids, weights=weights, capacity=cap, shared=dv["shared"]))
+
+
+@pytest.mark.parametrize("n", [9, 2048])
+def test_a_short_batch_of_a_long_layer(n):
+    """Routed by the kernels for short batches, whose workspace is larger."""
+    wl, dv, L = _setup("bf16", "relu", T=3000, d=64, E=64, f=72, backward=False)
+    L = MoELayer(wl.T, wl.d, wl.E, 8, wl.f, "relu", torch.bfloat16, 8 * L.rows_alloc)
+    small = lambda: MoELayer(n, wl.d, wl.E, 8, wl.f, "relu", torch.bfloat16, L.rows_alloc)
+    q, g = QuantizedExperts(dv["w1"], None, dv["w2"]), _gate(dv, wl)
+    L.forward_i8(dv["x"], q, **g)
+    x = dv["dy"][:n].contiguous()
+    assert torch.equal(L.forward_i8(x, q, **g), small().forward_i8(x, q, **g))
+    y = L.forward(x, dv["w1"], None, dv["w2"], **g)[:n]
+    assert torch.equal(y, small().forward(x, dv["w1"], None, dv["w2"], **g))

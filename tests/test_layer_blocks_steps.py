@@ -90,3 +90,20 @@ def test_int8_forward_refuses_other_shapes(calls):
         with pytest.raises(ValueError, match="ids"):
             L.forward_i8(torch.zeros(T, d), Experts, ids=torch.zeros(*shape, dtype=torch.int32))
     assert not calls
+
+
+@pytest.mark.parametrize("serve", [False, True])
+def test_the_routing_workspace_of_fewer_tokens(calls, serve):
+    """A short batch is routed by kernels of its own, which take more workspace than a longer one."""
+    most, E, k = 3000, 64, 8
+    need = {n: B.moe_route_workspace_bytes(n, E, k) for n in (1, 2048, most)}
+    assert need[2048] > need[most]
+    L = MoELayer(most, d, E, k, f, "relu", torch.float32, 64, device="cpu")
+    experts = type("", (Experts,), dict(E=E))
+    for n, least in need.items():
+        x, calls[:] = torch.zeros(n, d), []
+        if serve:
+            L.forward_i8(x, experts, w_g=torch.zeros(E, d))
+        else:
+            L.route(x, L.ids, True, 1, 1)
+        assert _args(calls, "moe_route")[0][16].numel() >= least, n
