@@ -286,6 +286,9 @@ class MoELayer:
         return ((c.gate, c.count, c.capacity_static, c.capacity_dynamic, c.dispatch, c.ffn_fwd,
                  c.combine) == _OWN_STEPS and self.__dict__.keys().isdisjoint(_STEPS))
 
+    def _is_overridden(self, step):
+        return getattr(type(self), step) is not _OWN_STEPS[_STEPS.index(step)] or step in self.__dict__
+
     def _fusable(self, x, w1, capacity, rows, counts_from_batch=True, ids=None, w_g=None):
         """Whether the forward is one library call: the class's own steps,
         capacities from this batch, kept rows, and tensors of the layer's own
@@ -368,14 +371,23 @@ class MoELayer:
         dtype].  x holds the layer's T tokens or fewer (with ids, weights
         [tokens, k]), and only those are routed and returned.  Arguments as for
         forward, whose padded rows, lagged counts and balance term it does not
-        take; no backward follows it."""
+        take; no backward follows it.  A layer with a gate, count, capacity or
+        combine of its own has them called, on batches of T tokens; one with a
+        dispatch or ffn_fwd of its own is refused, as those work on rows in the
+        layer dtype."""
         T, d, E, k, R = self.T, self.d, self.E, self.k, self.rows_alloc
         if (experts.E, experts.f, experts.d) != (E, self.f, d):
             raise ValueError(f"quantised experts of sizes {(experts.E, experts.f, experts.d)}, the "
                              f"layer's are {(E, self.f, d)}")
         if x.dim() != 2 or x.shape[1] != d or x.shape[0] > T:
             raise ValueError(f"x has shape {tuple(x.shape)}, the layer takes up to {T} rows of {d}")
-        n = x.shape[0]
+        n, own = x.shape[0], self._own_steps()
+        if not own:
+            for name in ("dispatch", "ffn_fwd"):
+                if self._is_overridden(name):
+                    raise ValueError(f"this layer has a {name} of its own, which the int8 forward cannot call")
+            if n != T:
+                raise ValueError(f"x has shape {tuple(x.shape)}, a layer with steps of its own takes all {T} tokens")
         if ids is not None and tuple(ids.shape) != (n, k):
             raise ValueError(f"ids have shape {tuple(ids.shape)}, expected {(n, k)}")
         if self.xq is None:
@@ -398,7 +410,12 @@ class MoELayer:
         # the dispatch moves rows of 16-byte vectors: two int8 values ride as one bf16
         rows, disp = xq.view(torch.bfloat16), self.xq_disp.view(torch.bfloat16)
         kind, num, den = capacity
-        if kind == "policy":
+        if kind == "policy" or not own:
+            if kind == "static":
+                self.capacity_static(num, den)
+            elif kind != "policy":
+                self.count(ids)
+                self.capacity_dynamic(num, den)
             B.moe_dispatch(rows, ids, E, self.capacity, self.offsets, R, self.counts, self.fill,
                            self.dest_row, self.src, disp, self.status, self.ws_dispatch)
         else:

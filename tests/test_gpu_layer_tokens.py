@@ -63,3 +63,13 @@ def test_a_short_batch_of_a_long_layer(n):
     assert torch.equal(L.forward_i8(x, q, **g), small().forward_i8(x, q, **g))
     y = L.forward(x, dv["w1"], None, dv["w2"], **g)[:n]
     assert torch.equal(y, small().forward(x, dv["w1"], None, dv["w2"], **g))
+
+
+@pytest.mark.parametrize("cap", [CAP, ("static", 1, 2)], ids=["dynamic", "static"])
+def test_int8_forward_with_a_step_of_its_own(cap):
+    """The steps called one by one: the same bits."""
+    wl, dv, L = _setup("bf16", "swiglu", backward=False)
+    q, g = QuantizedExperts(dv["w1"], dv["w3"], dv["w2"]), dict(_gate(dv, wl), capacity=cap)
+    y, fill = L.forward_i8(dv["x"], q, **g).clone(), L.fill.clone()
+    L.count = type(L).count.__get__(L)
+    assert torch.equal(y, L.forward_i8(dv["x"], q, **g)) and torch.equal(fill, L.fill)

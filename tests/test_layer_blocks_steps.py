@@ -107,3 +107,37 @@ def test_the_routing_workspace_of_fewer_tokens(calls, serve):
         else:
             L.route(x, L.ids, True, 1, 1)
         assert _args(calls, "moe_route")[0][16].numel() >= least, n
+
+
+HOOKS = {"gate": "moe_gate_topk", "count": "moe_count", "capacity_dynamic": "moe_update_capacity",
+         "combine": "moe_combine"}
+
+
+@pytest.mark.parametrize("step", sorted(HOOKS))
+@pytest.mark.parametrize("how", ["subclass", "instance"])
+def test_overridden_steps_are_called(calls, step, how):
+    own, hits = getattr(MoELayer, step), []
+
+    def hook(self, *a, **kw):
+        hits.append(step)
+        return own(self, *a, **kw)
+
+    L = _layer(type("Hooked", (MoELayer,), {step: hook}) if how == "subclass" else MoELayer)
+    if how == "instance":
+        setattr(L, step, hook.__get__(L))
+    L.forward_i8(torch.zeros(T, d), Experts, w_g=torch.zeros(E, d))
+    assert hits == [step]
+    assert [n for n, _, _ in calls] == ["moe_gate_topk", "moe_quantize_rows", "moe_count", "moe_update_capacity",
+                                        "moe_dispatch", "moe_expert_ffn_fwd_i8", "moe_combine"]
+    # such a step knows the layer's T tokens only
+    with pytest.raises(ValueError, match="x has shape"):
+        L.forward_i8(torch.zeros(T - 1, d), Experts, w_g=torch.zeros(E, d))
+
+
+@pytest.mark.parametrize("step", ["dispatch", "ffn_fwd"])
+def test_steps_in_the_layer_type_are_refused(calls, step):
+    """The int8 forward moves and multiplies int8 rows: it cannot call these."""
+    L = _layer(type("Hooked", (MoELayer,), {step: lambda self, *a, **kw: None}))
+    with pytest.raises(ValueError, match=step):
+        L.forward_i8(torch.zeros(T, d), Experts, w_g=torch.zeros(E, d))
+    assert not calls
