@@ -6,6 +6,7 @@ the library is missing it raises - there is no fallback path.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Optional
 
@@ -158,8 +159,62 @@ def _ptr(t: Optional[torch.Tensor]):
     return ctypes.c_void_p(t.data_ptr())
 
 
+# Every call runs on the device of its tensors, on that device's current stream,
+# whichever device is current.
 def _stream():
     return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+
+
+def _on_its_device(fn):
+    """fn with the device of its first tensor made current (the others are to live there too).
+    Where it is current already (the usual case) torch's guard, which costs as much as a
+    small launch, is left out."""
+    @functools.wraps(fn)
+    def call(*args, **kw):
+        for t in (*args, *kw.values()):
+            if isinstance(t, torch.Tensor):
+                i = t.get_device()          # -1: not in device memory, which fn refuses
+                if i >= 0 and i != torch.cuda.current_device():
+                    with torch.cuda.device(i):
+                        return fn(*args, **kw)
+                break
+        return fn(*args, **kw)
+    return call
+
+
+def _device_of(*tensors) -> int:
+    """Index of the one device all the call's tensors live on."""
+    first = -1
+    for t in tensors:
+        if t is None:
+            continue
+        i = t.get_device()          # -1: not in device memory
+        if i < 0:
+            raise MoEError("tensor must live in device memory")
+        if first < 0:
+            first = i
+        elif i != first:
+            raise MoEError(f"tensors on devices {first} and {i}: one device is needed")
+    return first
+
+
+class _Here:
+    """`with _Here(index) as stream`: on that device, with its current stream."""
+
+    __slots__ = ("index", "guard")
+
+    def __init__(self, index):
+        self.index = index
+        self.guard = None if index == torch.cuda.current_device() else torch.cuda.device(index)
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+        return torch.cuda.current_stream(self.index).cuda_stream
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
 
 
 def _dt(t: torch.Tensor) -> int:
@@ -202,6 +257,7 @@ def workspace(nbytes: int, device) -> torch.Tensor:
 
 
 # ---- entry points -----------------------------------------------------------
+@_on_its_device
 def moe_gate_topk(x, w_g, bias, k, renorm, logits, ids, weights):
     T, d = x.shape
     E = w_g.shape[0]
@@ -215,6 +271,7 @@ def moe_gate_topk(x, w_g, bias, k, renorm, logits, ids, weights):
            "moe_gate_topk")
 
 
+@_on_its_device
 def moe_count(ids, E, counts, status):
     T, k = ids.shape
     _need(ids, T * k, "ids", _I32)
@@ -224,6 +281,7 @@ def moe_count(ids, E, counts, status):
            "moe_count")
 
 
+@_on_its_device
 def moe_update_capacity(T, k, E, counts, num, den, cap_min, capacity, offsets, row_align=1):
     _need(counts, E, "counts", _I32, optional=True)
     _need(capacity, E, "capacity", _I32)
@@ -237,6 +295,7 @@ def moe_dispatch_workspace_bytes(T, E, k) -> int:
     return lib().moe_dispatch_workspace_bytes(T, E, k)
 
 
+@_on_its_device
 def moe_dispatch(x, ids, E, capacity, offsets, rows_alloc, counts, fill, dest_row, src, x_disp,
                  status, ws):
     T, d = x.shape
@@ -257,6 +316,7 @@ def moe_route_workspace_bytes(T, E, k) -> int:
     return lib().moe_route_workspace_bytes(T, E, k)
 
 
+@_on_its_device
 def moe_route(x, ids, E, dynamic, num, den, cap_min, rows_alloc, capacity, offsets, counts, fill,
               dest_row, src, x_disp, status, ws, row_align=1):
     """moe_count (dynamic), moe_update_capacity and moe_dispatch in one call."""
@@ -274,6 +334,7 @@ def moe_route(x, ids, E, dynamic, num, den, cap_min, rows_alloc, capacity, offse
                            _ptr(status), _ptr(ws), _nbytes(ws)), "moe_route")
 
 
+@_on_its_device
 def moe_layer_fwd(x, w_g, bias, w1, w3, w2, cached_ids, weights, *, act, k, renorm, dynamic, num,
                   den, rows_alloc, logits, ids, capacity, offsets, counts, fill, dest_row, src,
                   status, x_disp, h_save, y_disp, y, route_ws, ffn_ws, cap_min=0, row_align=1):
@@ -321,6 +382,7 @@ def moe_dispatch_noalloc_max_assignments() -> int:
     return lib().moe_dispatch_noalloc_max_assignments()
 
 
+@_on_its_device
 def moe_dispatch_noalloc(x, ids, E, capacity, offsets, rows_alloc, counts, fill, dest_row, src,
                          x_disp, status):
     """moe_dispatch without a workspace (the library's fixed device scratch)."""
@@ -346,6 +408,7 @@ def moe_ffn_bwd_workspace_bytes(dt, act, E, d, f, rows_alloc) -> int:
     return lib().moe_ffn_bwd_workspace_bytes(dt, act, E, d, f, rows_alloc)
 
 
+@_on_its_device
 def moe_expert_ffn_fwd(act, offsets, rows, x_disp, w1, w3, w2, h_save, y_disp, ws):
     E, f, d = w1.shape
     R, dt = x_disp.shape[0], w1.dtype
@@ -362,6 +425,7 @@ def moe_expert_ffn_fwd(act, offsets, rows, x_disp, w1, w3, w2, h_save, y_disp, w
            "moe_expert_ffn_fwd")
 
 
+@_on_its_device
 def moe_zero_pad_rows(offsets, fill, rows, buf):
     E = fill.shape[0]
     R, d = buf.shape
@@ -372,6 +436,7 @@ def moe_zero_pad_rows(offsets, fill, rows, buf):
                                    _ptr(rows), R, _ptr(buf)), "moe_zero_pad_rows")
 
 
+@_on_its_device
 def moe_combine(y_disp, dest_row, weights, y):
     T, k = dest_row.shape
     d = y.shape[1]
@@ -383,6 +448,7 @@ def moe_combine(y_disp, dest_row, weights, y):
                              _ptr(dest_row), _ptr(weights), _ptr(y)), "moe_combine")
 
 
+@_on_its_device
 def moe_combine_bwd(dy, y_disp, dest_row, weights, dy_disp, dweights):
     T, k = dest_row.shape
     d = dy.shape[1]
@@ -398,6 +464,7 @@ def moe_combine_bwd(dy, y_disp, dest_row, weights, dy_disp, dweights):
                                  _ptr(dweights)), "moe_combine_bwd")
 
 
+@_on_its_device
 def moe_expert_ffn_bwd(act, offsets, rows, x_disp, h_save, w1, w3, w2, dy_disp, dx_disp, dw1,
                        dw3, dw2, ws):
     E, f, d = w1.shape
@@ -421,45 +488,6 @@ def moe_expert_ffn_bwd(act, offsets, rows, x_disp, h_save, w1, w3, w2, dy_disp, 
 
 
 # ---- 8-bit integer products and the dense gated block ------------------------
-# These check that their tensors share one device and run on that device's
-# current stream, whichever device is current.
-def _device_of(*tensors) -> int:
-    """Index of the one device all the call's tensors live on."""
-    first = -1
-    for t in tensors:
-        if t is None:
-            continue
-        i = t.get_device()          # -1: not in device memory
-        if i < 0:
-            raise MoEError("tensor must live in device memory")
-        if first < 0:
-            first = i
-        elif i != first:
-            raise MoEError(f"tensors on devices {first} and {i}: one device is needed")
-    return first
-
-
-class _Here:
-    """`with _Here(index) as stream`: on that device, with its current stream.
-    Where it is the current device (the usual case) torch's guard, which costs
-    as much as a small launch, is left out."""
-
-    __slots__ = ("index", "guard")
-
-    def __init__(self, index):
-        self.index = index
-        self.guard = None if index == torch.cuda.current_device() else torch.cuda.device(index)
-
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-        return torch.cuda.current_stream(self.index).cuda_stream
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
-
-
 def _rows(t: Optional[torch.Tensor], name, T, d, dtype, optional=False):
     """Row distance in elements of a [T, d] tensor whose rows are contiguous."""
     if t is None:
@@ -619,6 +647,7 @@ def moe_gate_bwd_workspace_bytes(T, d, E) -> int:
     return lib().moe_gate_bwd_workspace_bytes(T, d, E)
 
 
+@_on_its_device
 def moe_gate_bwd(x, logits, ids, dweights, renorm, dlogits, dw_g, ws, dprob_coef=None):
     T, d = x.shape
     E = logits.shape[1]
@@ -634,6 +663,7 @@ def moe_gate_bwd(x, logits, ids, dweights, renorm, dlogits, dw_g, ws, dprob_coef
                               _ptr(dw_g), _ptr(ws), _nbytes(ws)), "moe_gate_bwd")
 
 
+@_on_its_device
 def moe_dispatch_bwd(dx_disp, dest_row, E, dlogits, w_g, dx):
     T, k = dest_row.shape
     d = dx.shape[1]
@@ -652,6 +682,7 @@ def moe_balance_workspace_bytes(T, E) -> int:
     return lib().moe_balance_workspace_bytes(T, E)
 
 
+@_on_its_device
 def moe_balance_fwd(logits, counts, k, lam, loss, dprob_coef, ws):
     T, E = logits.shape
     _need(logits, T * E, "logits", _F32)
@@ -663,6 +694,7 @@ def moe_balance_fwd(logits, counts, k, lam, loss, dprob_coef, ws):
            "moe_balance_fwd")
 
 
+@_on_its_device
 def moe_aggregate_spec(y_disp, dest_row, out):
     T, k = dest_row.shape
     d = out.shape[1]
@@ -677,6 +709,7 @@ def moe_spec_loss_workspace_bytes(T) -> int:
     return lib().moe_spec_loss_workspace_bytes(T)
 
 
+@_on_its_device
 def moe_spec_loss(y_disp, dest_row, weights, target, dy_disp, dweights, loss, ws):
     T, k = dest_row.shape
     d = target.shape[1]
@@ -695,6 +728,7 @@ def moe_spec_loss(y_disp, dest_row, weights, target, dy_disp, dweights, loss, ws
 
 
 # ---- sample assignment caching ------------------------------------------------
+@_on_its_device
 def moe_cache_update(fresh_ids, cached, cache_out, unchanged):
     T, k = fresh_ids.shape
     for t, name in ((fresh_ids, "fresh_ids"), (cached, "cached"), (cache_out, "cache_out")):
@@ -704,6 +738,7 @@ def moe_cache_update(fresh_ids, cached, cache_out, unchanged):
                                   _ptr(unchanged)), "moe_cache_update")
 
 
+@_on_its_device
 def moe_cached_weights(logits, ids, renorm, weights):
     T, E = logits.shape
     k = ids.shape[1]
@@ -736,15 +771,24 @@ def moe_capacity_trigger(T, counts, cap, grow, shrink, cap_min=0):
 
 
 class CapacityPolicy:
-    """Owner of one moe_capacity_policy object (see include/moe.h)."""
+    """Owner of one moe_capacity_policy object (see include/moe.h), for tensors of one device
+    (device: its index; None: the current one)."""
 
-    def __init__(self, T, k, E, delta_launch, grow, shrink, init_cap, cap_min=0, row_align=1):
+    def __init__(self, T, k, E, delta_launch, grow, shrink, init_cap, cap_min=0, row_align=1,
+                 device: Optional[int] = None):
         init = (ctypes.c_int32 * E)(*[int(c) for c in init_cap])
-        h = ctypes.c_void_p()
-        _check(lib().moe_policy_create(T, k, E, delta_launch, grow[0], grow[1], shrink[0],
-                                       shrink[1], cap_min, row_align, init, ctypes.byref(h)),
-               "moe_policy_create")
-        self._h, self.E = h, E
+        self._h = h = ctypes.c_void_p()
+        self.E = E
+        self.device = torch.cuda.current_device() if device is None else device
+        with _Here(self.device):
+            _check(lib().moe_policy_create(T, k, E, delta_launch, grow[0], grow[1], shrink[0],
+                                           shrink[1], cap_min, row_align, init, ctypes.byref(h)),
+                   "moe_policy_create")
+
+    def _here(self, *tensors):
+        if _device_of(*tensors) != self.device:
+            raise MoEError(f"tensors on device {_device_of(*tensors)}, the policy was made for {self.device}")
+        return _Here(self.device)
 
     def begin(self, capacity, offsets):
         """Enqueue the capacities for the next launch; returns (rows needed,
@@ -753,13 +797,15 @@ class CapacityPolicy:
         _need(offsets, self.E + 1, "offsets", _I32)
         rows = ctypes.c_int64()
         rec = ctypes.c_int()
-        _check(lib().moe_policy_begin(self._h, _stream(), _ptr(capacity), _ptr(offsets),
-                                      ctypes.byref(rows), ctypes.byref(rec)), "moe_policy_begin")
+        with self._here(capacity, offsets) as stream:
+            _check(lib().moe_policy_begin(self._h, stream, _ptr(capacity), _ptr(offsets),
+                                          ctypes.byref(rows), ctypes.byref(rec)), "moe_policy_begin")
         return rows.value, bool(rec.value)
 
     def end(self, counts):
         _need(counts, self.E, "counts", _I32)
-        _check(lib().moe_policy_end(self._h, _stream(), _ptr(counts)), "moe_policy_end")
+        with self._here(counts) as stream:
+            _check(lib().moe_policy_end(self._h, stream, _ptr(counts)), "moe_policy_end")
 
     def state(self):
         cap = (ctypes.c_int32 * self.E)()
