@@ -677,9 +677,12 @@ int moe_timing_report(char* buf, size_t len);
  * products with few tiles per CU; both kernels add every output's products in the same
  * order, so results are identical bit for bit in every mode.  (Also of the
  * int8 products, whose sums are exact; a dense gated block may split a sum
- * over K in a different number of ranges in another mode.)  1:
+ * over K in a different number of ranges in another mode.)  The int8 products
+ * and the dense gated block may then also take tiles with more stages in flight
+ * (32 to 128 rows and 128 columns) and, for few rows, a kernel without tiles.  1:
  * 256x256 only; 2: 128-column tiles only.  float32 layers run every product
- * on 128-column tiles in every mode.  Process-wide; read when a product is
+ * of the experts on 128-column tiles in every mode, and the dense block's in
+ * modes 1 and 2.  Process-wide; read when a product is
  * launched.  Returns MOE_EINVAL for other modes. [host]
  */
 moe_status moe_set_gemm_tiles(int mode);

@@ -35,7 +35,8 @@ struct GatedPlan {
   size_t o_part, o_wt, total_bwd;
 };
 
-// Rows up to which the forward streams its weights through the kernel for few rows.
+// Rows up to which the forward streams its weights through the kernel for few rows
+// (a forced tile mode, moe_set_gemm_tiles, has its tiles run instead).
 constexpr int kFewDense = 16;
 
 bool plan_gated(moe_dtype dt, int T, int d, int f, GatedPlan& g) {
@@ -46,7 +47,7 @@ bool plan_gated(moe_dtype dt, int T, int d, int f, GatedPlan& g) {
   g = {};
   g.total_fwd = g.total_bwd = 256;
   if (T == 0) return true;
-  g.few = T <= (dt == MOE_F32 ? 2 : 1) * kFewDense;
+  g.few = g_tile_mode == 0 && T <= (dt == MOE_F32 ? 2 : 1) * kFewDense;
   g.wt = use_wt13(pl, dt);
   g.h = dense_plan<M_GATED_FWD, P_FWD_H>(dt, T, f, d, rd, rd);
   g.y = dense_plan<M_ADD_STORE, P_FWD_Y>(dt, T, d, f, rf, rf);

@@ -186,3 +186,20 @@ def test_workspace_queries():
     assert B.quantized_width(24) == q.moe_quantized_width(24) == 32
     assert all(B.quantized_width(n) == q.moe_quantized_width(n) for n in range(0, 300))
     assert q.moe_quantized_width(-1) == 0
+
+
+@pytest.mark.parametrize("dt,rows", [(B.MOE_BF16, 16), (B.MOE_F32, 32)])
+def test_a_forced_tile_mode_holds_for_few_tokens_too(dt, rows):
+    """The automatic mode streams the weights of a few tokens' forward and needs room for A
+    alone; a forced mode runs its tiles, which split K and need room for partial sums."""
+    d, f = 4096, 14336
+    size = lambda T: B.moe_gated_ffn_fwd_workspace_bytes(dt, T, d, f)
+    a = lambda T: -(-T * f * (2 if dt == B.MOE_BF16 else 4) // 256) * 256
+    try:
+        for mode in (0, 1, 2):
+            B.moe_set_gemm_tiles(mode)
+            for T in (1, rows):
+                assert (size(T) > a(T) + 256) == (mode != 0), (mode, T)
+            assert size(rows + 1) > a(rows + 1) + 256, mode
+    finally:
+        B.moe_set_gemm_tiles(0)
