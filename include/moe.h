@@ -669,21 +669,23 @@ moe_status moe_timing_enable(int on);
 int moe_timing_report(char* buf, size_t len);
 
 /*
- * Tile shape of the expert products (a tuning and testing aid; not part of
- * the method).  mode 0 (default): the library picks per product.  bf16: from
- * N, K, the row budget and E, between 256x256 tiles (one workgroup per CU)
- * and tiles of 32 to 192 rows and 128 columns (two workgroups per CU; the
- * heights chosen on the device from the rows per expert) -- the latter for
- * products with few tiles per CU; both kernels add every output's products in the same
- * order, so results are identical bit for bit in every mode.  (Also of the
- * int8 products, whose sums are exact; a dense gated block may split a sum
- * over K in a different number of ranges in another mode.)  The int8 products
- * and the dense gated block may then also take tiles with more stages in flight
- * (32 to 128 rows and 128 columns) and, for few rows, a kernel without tiles.  1:
- * 256x256 only; 2: 128-column tiles only.  float32 layers run every product
- * of the experts on 128-column tiles in every mode, and the dense block's in
- * modes 1 and 2.  Process-wide; read when a product is
- * launched.  Returns MOE_EINVAL for other modes. [host]
+ * Tile shape of the products (a tuning and testing aid; not part of the
+ * method).  mode 0 (default): the library picks per product.  bf16: from N,
+ * K, the row budget and E, between 256x256 tiles (one workgroup per CU) and
+ * tiles of 32 to 192 rows and 128 columns (two workgroups per CU; the heights
+ * chosen on the device from the rows per expert) -- the latter for products
+ * with few tiles per CU.  The int8 products and the dense gated block also
+ * take tiles with more stages in flight (32 to 128 rows and 128 columns) and,
+ * for few rows, a kernel without tiles.  1: 256x256 only; 2: 128-column tiles
+ * only.  float32 experts run on 128-column tiles in every mode, a float32
+ * dense block in modes 1 and 2.
+ * The experts' results are identical bit for bit in every mode: their bf16
+ * and float32 kernels add every output's products in the same order, and
+ * int8 sums are exact.  A dense gated block's (and with it those of a layer
+ * with a shared expert) agree up to the order of float32 sums: another mode
+ * may split a sum over K into other ranges, or between more wavefronts.
+ * Process-wide; read when a product is launched.  Returns MOE_EINVAL for
+ * other modes. [host]
  */
 moe_status moe_set_gemm_tiles(int mode);
 
@@ -694,15 +696,15 @@ moe_status moe_set_gemm_tiles(int mode);
  * that the call makes first in its workspace ([E, d, F] with F = 2f under
  * SwiGLU, bf16).  mode 0 (default): the copy when the row budget holds at
  * least 8192 rows per expert (rows_alloc >= 8192 E), where the faster
- * product outweighs the copy; 1: never; 2: always.  The products are
+ * product outweighs the copy; 1: never; 2: always.  The experts' products are
  * identical bit for bit either way.  moe_ffn_bwd_workspace_bytes includes
  * the copy's E*d*F*2 bytes when the current mode would make it; a call
  * whose workspace lacks them reads the weights K-major.  moe_gated_ffn_bwd
  * follows the same rule for its one expert of T rows; its query and its call
  * are to see the same mode (a smaller workspace is MOE_EWORKSPACE there, as it
- * is after a change of moe_set_gemm_tiles).  Process-wide; read when a
- * backward (or its workspace query) is called.  Returns MOE_EINVAL for other
- * modes. [host]
+ * is after a change of moe_set_gemm_tiles), and its dX agrees between the modes
+ * up to the order of float32 sums.  Process-wide; read when a backward (or its
+ * workspace query) is called.  Returns MOE_EINVAL for other modes. [host]
  */
 moe_status moe_set_dx_weight_copy(int mode);
 
