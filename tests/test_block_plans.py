@@ -125,3 +125,13 @@ def test_the_gpu_tests_reach_every_kernel(lib):
     # (256x256 tiles by the tests' forced mode; the mid tiles of the weight gradients in fp32 likewise)
     took = {lib.i8(len(rows), sum(rows) + sum(slack) + 3, -(-K // 16) * 16, N, 0, 0) for rows, slack, K, N in Q.SHAPES}
     assert took >= {I8_FEW, I8_DEEP32, I8_DEEP64, I8_DEEP128}, took
+
+
+def test_the_gpu_tests_reach_every_kernel_of_the_transposed_weights(lib):
+    """dX from the transposed copy of [W1; W3]: both operands K-contiguous."""
+    import test_gpu_gated_copy as C
+    seen = set()
+    for T, d, f in C.SHAPES + C.LONG:
+        kernel, h, _, _, splits, _ = plan(lib, (0, 0, 0, 0, T, d, 2 * f, 4 * f, 4 * f), False)
+        seen |= {(kernel, h if kernel == DEEP else 0), ("split", splits > 1)}
+    assert seen == {(BIG, 0), (MID, 0), (DEEP, 1), (DEEP, 2), (DEEP, 4), ("split", True), ("split", False)}
