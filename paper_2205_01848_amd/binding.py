@@ -156,13 +156,21 @@ def _ptr(t: Optional[torch.Tensor]):
         raise MoEError("tensor must live in device memory")
     if not t.is_contiguous():
         raise MoEError("tensor must be contiguous")
-    return ctypes.c_void_p(t.data_ptr())
+    return t.data_ptr()
 
 
 # Every call runs on the device of its tensors, on that device's current stream,
 # whichever device is current.
 def _stream():
-    return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+    # (by index: without one, torch takes more than twice as long to find it)
+    return torch.cuda.current_stream(torch.cuda.current_device()).cuda_stream
+
+
+def _first_device(values) -> Optional[int]:
+    for t in values:
+        if isinstance(t, torch.Tensor):
+            return t.get_device()           # -1: not in device memory, which the call refuses
+    return None
 
 
 def _on_its_device(fn):
@@ -171,14 +179,13 @@ def _on_its_device(fn):
     small launch, is left out."""
     @functools.wraps(fn)
     def call(*args, **kw):
-        for t in (*args, *kw.values()):
-            if isinstance(t, torch.Tensor):
-                i = t.get_device()          # -1: not in device memory, which fn refuses
-                if i >= 0 and i != torch.cuda.current_device():
-                    with torch.cuda.device(i):
-                        return fn(*args, **kw)
-                break
-        return fn(*args, **kw)
+        i = _first_device(args)
+        if i is None:
+            i = _first_device(kw.values())
+        if i is None or i < 0 or i == torch.cuda.current_device():
+            return fn(*args, **kw)
+        with torch.cuda.device(i):
+            return fn(*args, **kw)
     return call
 
 

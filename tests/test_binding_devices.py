@@ -77,6 +77,7 @@ def _everything():
     B.moe_expert_matmul_i8(L.offsets, L.fill, z(R, 16, dtype=torch.int8), z(R), z(E, f, 16, dtype=torch.int8),
                            z(E, f), z(R, f), z(4096, dtype=torch.uint8))
     B.moe_cached_weights(L.logits, L.ids, 0, z(T, k))
+    B.moe_update_capacity(T, k, E, None, 5, 4, 0, capacity=L.capacity, offsets=L.offsets)   # tensors by name alone
     B.moe_cache_update(L.ids, L.ids, z(T, k, dtype=i32), z(1, dtype=i32))
     B.moe_dispatch_noalloc(x, L.ids, E, L.capacity, L.offsets, R, L.counts, L.fill, L.dest_row, L.src, L.x_disp,
                            L.status)
