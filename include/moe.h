@@ -540,7 +540,8 @@ int moe_quantized_width(int n);
  * each, the form the int8 products below read: tokens, and weights (a row of
  * a weight matrix is an output channel).
  *   scale = max_j |x_j| * (1/127), a float32 product with the float32 nearest
- *           to 1/127
+ *           to 1/127 (which is how a tensor is divided by 127 on the device;
+ *           within one unit in the last place of max_j |x_j| / 127)
  *   q_j   = the integer nearest to x_j / scale (ties to even), in [-127, 127]
  * decided exactly, not from a rounded quotient.  A row whose scale rounds to
  * 0 gets q = 0; a row with a NaN or an infinity gets scale NaN and q = 0 (so

@@ -94,3 +94,23 @@ def test_int8_ffn_is_near_the_real_one(act):
     bound = (np.abs(a).max(axis=1)[:, None] / 127 * 0.51 + np.abs(a) * 2.0 ** -8) @ np.abs(val(w2, s2)).T
     assert (np.abs(y - ref) <= bound).all()
     assert np.median(slack) < 0.05 * np.median(bound)
+
+
+# largest bf16 values of a row, up to a power of two, whose product with the float32 nearest
+# to 1/127 is not the rounded quotient
+OTHER_MAXIMA = (143, 144, 175, 207, 208, 239)
+
+
+def test_the_scale_is_the_product():
+    """The header's scale, max|x| times float32(1/127), and not max|x| / 127 rounded; half the
+    largest value lies next to 63.5 scales and shows which of the two is meant."""
+    m = np.arange(128, 256).astype(np.float32)
+    x = np.zeros((128, 8))
+    x[:, 0], x[:, 1], x[:, 2] = m, m / 2, -m / 2
+    q, s = O.quantize_rows(x)
+    assert (s == m * (np.float32(1) / np.float32(127))).all()
+    assert tuple(m[s != m / np.float32(127)]) == OTHER_MAXIMA
+    by_product = np.rint(m / 2 / s.astype(np.float64))
+    by_quotient = np.rint(m / 2 / (m / np.float32(127)).astype(np.float64))
+    assert (q[:, 1] == by_product).all() and (q[:, 2] == -by_product).all()
+    assert set(m[by_product != by_quotient]) <= set(OTHER_MAXIMA) and (by_product != by_quotient).any()
