@@ -61,7 +61,7 @@ __device__ __forceinline__ void mma16(floatx4& c, const uint4& a, const uint4& b
 // K-major k-rows r with r & 8 also have the two 16-element halves of every 32-element
 // segment swapped: a transpose read takes half a segment of k-rows r .. r + 3 and of
 // r + 8 .. r + 11 at once, which would otherwise lie on the same banks (2048 tokens,
-// 1024 -> 2816: the backward's dX 43.4 -> 39.4 us.  The mid and the 256x256 kernels,
+// 1024 -> 2816: the backward's dX, then on one group of wavefronts, 9 % shorter.  The mid and the 256x256 kernels,
 // bound by other things, gain 0 to 1 % by it and do without.)
 template <int RB, int NS, int ALAY, int BLAY, bool GATED, int ES>
 __device__ __forceinline__ void mainloop_deep(const TileOps& op, int wave, int k_first, int nk,
@@ -183,8 +183,9 @@ __device__ __forceinline__ void mainloop_deep(const TileOps& op, int wave, int k
 // the K steps into stages of its own, and its sums are added through LDS at the end.
 // A wavefront alone on its SIMD waits for its fragments between the matrix
 // instructions; two overlap.  For tiles that leave every CU one workgroup (2048
-// tokens, 2816 -> 1024: Y 25.8 -> 24.6, dX 39.3 -> 34.8 us; six stages for one group instead:
-// 25.3 and 42.2).
+// tokens, 2816 -> 1024, operands in the last-level cache: Y 18.8 -> 17.2, dX 38.0 ->
+// 31.9 us; six stages for one group instead left Y as it was and made dX 7 %
+// longer).  The plan (plan.hpp) knows the time of one group only.
 template <int MODE, int PASS, int RB, int NS, int KG>
 __global__ __launch_bounds__(KG * kThreads16, RB <= 2 ? 2 : 1) void ffn_gemm16_deep_kernel(const GroupParams gp) {
   constexpr bool GATED = is_gated(MODE), DENSE = is_dense(MODE), VARK = is_dw(MODE);

@@ -10,8 +10,9 @@
 // The W partial sums meet in LDS at the end, added in wavefront order.
 //
 // Against tiles of 32 rows and 128 columns, which stage both operands through
-// LDS with a barrier per step, this keeps 64 to 256 KB of weights in flight per
-// CU instead of two 20 KB stages.
+// LDS with a barrier per step, a wavefront keeps 4 KB of weights in flight (8 in a
+// gated product) and waits for nobody: 16 KB a CU for 1024 columns, 32 for 4096, 110 for
+// the 2 x 14336 of a gated product.
 #pragma once
 
 #include "deep.hpp"
@@ -274,8 +275,8 @@ __global__ __launch_bounds__(64 * W) void ffn_few_rows_kernel(const GroupParams 
   }
 }
 
-// Wavefronts per workgroup: enough workgroups' worth to keep about 16
-// wavefronts on every CU, but no more than there are K steps.
+// Wavefronts per workgroup: 16, halved while they are more than 8 a CU or more
+// than there are K steps, but not below 4.
 inline int few_waves(int64_t items, int steps) {
   const int64_t want = 8 * static_cast<int64_t>(num_cus());
   int w = 16;

@@ -8,7 +8,8 @@
 // The forward saves the two factors of dA and A.  Against saving H1 and H3 the
 // backward evaluates no activation (dA of 8192 tokens, 4096 x 14336, 907 -> 880 us) and each
 // factor is rounded to bf16 once, from the unrounded H (relative error of
-// dW1 0.0035 -> 0.0029).
+// dW1 0.0035 -> 0.0029; factors of 32 bits would give 0.0024 and take 0.9 GB more
+// traffic in that step, about 3 % of it).
 //
 // Both projections, the activation and the product are one kernel, and the
 // addend (the routed experts' output, or their gradient) goes into the

@@ -24,13 +24,18 @@ struct DensePlan {
 // epilogue; a last round that leaves one of the two places of every CU empty takes
 // `half` percent of that.  Fitted on 10,388 bf16 and 6165 fp32 measurements of
 // the block's six products (32 to 4096 tokens, d from 512 to 4096, f from 1384 to
-// 14336, every kernel, height and 1 to 8 K ranges): residual 3 to 19 % a product;
-// the plan's choice takes 1.6 % (bf16) and 2.1 % (fp32) more than the best
-// measured one on average (of 168 bf16 products, 79 on the mid kernel, 69 deep,
-// 20 on 256x256 tiles).
-// Examples, us: 1021 tokens, 5632 -> 2048, 64-row tiles two-stage / deep 58 /
-// 34; 2048 tokens, 2816 -> 1024 26 / 20; 32 tokens, 28672 -> 4096, whole K / six
-// ranges 173 / 50; 4096 tokens, 4096 -> 2 x 14336, 256x256 / mid 677 / 832.
+// 14336, every kernel, height and 1 to 8 K ranges): residual 3 to 19 % a product.
+// The fit is of the kernels before their epilogues read ahead and before 64-row
+// deep tiles, where a CU has at most one, shared K between two groups of
+// wavefronts (deep.hpp), so those are estimated up to a fifth too long.  With the
+// kernels as they are the choice takes 1.7 % (bf16, 168 products) and 2.8 % (fp32,
+// 90) more than the best measured one on average, 27 and 41 % at the worst (512
+// tokens, dX of 4096 x 14336; 100 tokens, dX of 1024 x 2816); of the bf16 ones 79
+// are on the mid kernel, 68 deep, 21 on 256x256 tiles.
+// Examples, us (operands in the last-level cache): 1021 tokens, 5632 -> 2048,
+// 64-row tiles two-stage / deep 45 / 31; 2048 tokens, 2816 -> 1024 24.4 / 17.2; 32
+// tokens, 28672 -> 4096 (weights K-major), whole K / six ranges 221 / 76 with their
+// join; 4096 tokens, 4096 -> 2 x 14336, 256x256 / mid 695 / 832.
 struct TileTime {
   int step, fix, half;
 };
