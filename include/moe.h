@@ -555,6 +555,56 @@ moe_status moe_quantize_rows(void* stream, moe_dtype dt, int64_t rows, int n,
                              const void* x, int64_t ldx, int8_t* q,
                              float* scale);
 
+/*
+ * moe_rms_norm_fwd - root-mean-square norm of rows, after the addition on a
+ * residual stream that precedes it:
+ *   s = x + add, rounded to the layer dtype (add NULL: s = x)
+ *   r = 1 / sqrt(mean_j s_j^2 + eps),  y_j = s_j r weight_j, rounded once
+ * and the same rows in 8 bits, as moe_quantize_rows forms them, from the
+ * unrounded values: with a = s weight (float32), q and c as that call's q and
+ * scale of a, scale = c r.  So x_scale and xq of the int8 experts come from
+ * the norm in front of them.  (A sum of squares beyond float32 gives r = 0.)
+ *   x, add  [rows,d] layer dtype, rows ldx, ldadd elements apart
+ *   weight  [d] layer dtype;  eps > 0, finite
+ *   sum     s out, rows ldsum apart (the stream's next value), or NULL; only
+ *           with add
+ *   y       out, rows ldy apart, or NULL
+ *   rstd    [rows] float32 out: r, what the backward reads; or NULL
+ *   q       [rows, moe_quantized_width(d)] int8 out and scale [rows] float32
+ *           out; both or neither; q or y is needed
+ * sum and y may each be x or add itself (with the same row distance), not one
+ * another.  d a multiple of 8, at most 32768; row distances at least d and
+ * multiples of 8.
+ */
+moe_status moe_rms_norm_fwd(void* stream, moe_dtype dt, int64_t rows, int d,
+                            const void* x, int64_t ldx, const void* add,
+                            int64_t ldadd, const void* weight, float eps,
+                            void* sum, int64_t ldsum, void* y, int64_t ldy,
+                            float* rstd, int8_t* q, float* scale);
+
+/* Workspace bytes of moe_rms_norm_bwd for these sizes. [host] */
+size_t moe_rms_norm_bwd_workspace_bytes(int64_t rows, int d);
+
+/*
+ * moe_rms_norm_bwd - its gradients.  With g = dy weight:
+ *   dx = r (g - s r^2 mean_j(g_j s_j)) + dsum, rounded once: the gradient of x
+ *        and of add alike
+ *   dw_j = sum_t dy_tj s_tj r_t  (float32 sums in a fixed order)
+ *   s       [rows,d] layer dtype: the forward's sum (x without add), rows lds
+ *           apart;  rstd [rows] the forward's
+ *   dy      [rows,d];  dsum [rows,d] or NULL: what reaches s beside the norm
+ *   dx      [rows,d] out; may be s, dy or dsum itself (with the same row
+ *           distance)
+ *   dw      [d] out in dw_dt (MOE_F32 or the layer dtype), zeros for rows = 0;
+ *           NULL: not computed, and no workspace needed
+ */
+moe_status moe_rms_norm_bwd(void* stream, moe_dtype dt, int64_t rows, int d,
+                            const void* s, int64_t lds, const void* weight,
+                            const float* rstd, const void* dy, int64_t lddy,
+                            const void* dsum, int64_t lddsum, void* dx,
+                            int64_t lddx, moe_dtype dw_dt, void* dw,
+                            void* workspace, size_t workspace_bytes);
+
 /* Workspace bytes of moe_expert_matmul_i8 for these sizes. [host] */
 size_t moe_expert_matmul_i8_workspace_bytes(int E, int N, int64_t rows_alloc);
 

@@ -11,7 +11,9 @@ from .moe_oracle import *  # noqa: F401,F403
 from .losses import *  # noqa: F401,F403
 from .policies import *  # noqa: F401,F403
 from .blocks import *  # noqa: F401,F403
-from . import blocks as _blocks, losses as _losses, moe_oracle as _core, policies as _policies
+from .step import *  # noqa: F401,F403
+from . import (blocks as _blocks, losses as _losses, moe_oracle as _core, policies as _policies,
+               step as _step)
 
 __all__ = (list(_core.__all__) + list(_losses.__all__) + list(_policies.__all__) +
-           list(_blocks.__all__))
+           list(_blocks.__all__) + list(_step.__all__))

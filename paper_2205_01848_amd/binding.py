@@ -23,6 +23,10 @@ STATUS_BAD_ID, STATUS_DUP_ID, STATUS_REGION = 1, 2, 4
 _c_int, _c_i64, _c_size, _p = ctypes.c_int, ctypes.c_int64, ctypes.c_size_t, ctypes.c_void_p
 
 
+class _stream_p(ctypes.c_void_p):
+    """The stream of the calls around the layer (norm, vocabulary loss, AdamW)."""
+
+
 class LayerFwdArgs(ctypes.Structure):
     """moe_layer_fwd_args."""
     _fields_ = ([(n, _c_int) for n in ("dtype", "act", "T", "d", "E", "k", "f", "renorm",
@@ -93,6 +97,11 @@ SIGNATURES = {
     "moe_policy_state": (_c_int, [_p, _p, _p, _p, _p]),
     "moe_quantized_width": (_c_int, [_c_int]),
     "moe_quantize_rows": (_c_int, [_p, _c_int, _c_i64, _c_int, _p, _c_i64, _p, _p]),
+    "moe_rms_norm_fwd": (_c_int, [_stream_p, _c_int, _c_i64, _c_int, _p, _c_i64, _p, _c_i64, _p,
+                                  ctypes.c_float, _p, _c_i64, _p, _c_i64, _p, _p, _p]),
+    "moe_rms_norm_bwd_workspace_bytes": (_c_size, [_c_i64, _c_int]),
+    "moe_rms_norm_bwd": (_c_int, [_stream_p, _c_int, _c_i64, _c_int, _p, _c_i64, _p, _p, _p, _c_i64, _p,
+                                  _c_i64, _p, _c_i64, _c_int, _p, _p, _c_size]),
     "moe_expert_matmul_i8_workspace_bytes": (_c_size, [_c_int, _c_int, _c_i64]),
     "moe_expert_matmul_i8": (_c_int, [_p, _c_int, _c_int, _c_int, _c_int, _p, _p, _c_i64, _p, _p,
                                       _p, _c_int, _c_int, _p, _p, _p, _p, _c_size]),
@@ -536,6 +545,46 @@ def moe_quantize_rows(x, q, scale):
     with _Here(_device_of(x, q, scale)) as stream:
         _check(lib().moe_quantize_rows(stream, dt, rows, n, _at(x), ld, _ptr(q), _ptr(scale)),
                "moe_quantize_rows")
+
+
+def moe_rms_norm_fwd(x, weight, eps, y=None, add=None, sum=None, rstd=None, q=None, scale=None):
+    """s = x + add -> sum, y = s rsqrt(mean s^2 + eps) weight, and the same rows in 8 bits -> q
+    [rows, quantized_width(d)], scale [rows]; x, add, sum, y [rows, d] may be rows of wider
+    tensors."""
+    (rows, d), dtype = x.shape, x.dtype
+    dt = _dt(x)
+    ldx, ldadd, ldsum, ldy = (_rows(t, n, rows, d, dtype, optional=n != "x") for t, n in
+                              ((x, "x"), (add, "add"), (sum, "sum"), (y, "y")))
+    _need(weight, d, "weight", dtype)
+    _need(rstd, rows, "rstd", _F32, optional=True)
+    _need(q, rows * quantized_width(d), "q", torch.int8, optional=True)
+    _need(scale, rows, "scale", _F32, optional=True)
+    with _Here(_device_of(x, weight, y, add, sum, rstd, q, scale)) as stream:
+        _check(lib().moe_rms_norm_fwd(stream, dt, rows, d, _at(x), ldx, _at(add), ldadd, _ptr(weight),
+                                      eps, _at(sum), ldsum, _at(y), ldy, _ptr(rstd), _ptr(q),
+                                      _ptr(scale)), "moe_rms_norm_fwd")
+
+
+def moe_rms_norm_bwd_workspace_bytes(rows, d) -> int:
+    return lib().moe_rms_norm_bwd_workspace_bytes(rows, d)
+
+
+def moe_rms_norm_bwd(s, weight, rstd, dy, dx, dw, ws, dsum=None):
+    """Gradients of moe_rms_norm_fwd; dw (float32 or the layer's type) and ws None: dx alone."""
+    (rows, d), dtype = s.shape, s.dtype
+    dt = _dt(s)
+    lds, lddy, lddx = (_rows(t, n, rows, d, dtype) for t, n in ((s, "s"), (dy, "dy"), (dx, "dx")))
+    lddsum = _rows(dsum, "dsum", rows, d, dtype, optional=True)
+    _need(weight, d, "weight", dtype)
+    _need(rstd, rows, "rstd", _F32)
+    if dw is not None and dw.dtype not in (dtype, _F32):
+        raise MoEError(f"dw: a tensor of {dtype} or float32 is needed")
+    _need(dw, d, "dw", optional=True)
+    with _Here(_device_of(s, weight, rstd, dy, dx, dw, ws, dsum)) as stream:
+        _check(lib().moe_rms_norm_bwd(stream, dt, rows, d, _at(s), lds, _ptr(weight), _ptr(rstd),
+                                      _at(dy), lddy, _at(dsum), lddsum, _at(dx), lddx,
+                                      dt if dw is None else _dt(dw), _ptr(dw), _ptr(ws),
+                                      0 if ws is None else _nbytes(ws)), "moe_rms_norm_bwd")
 
 
 def moe_expert_matmul_i8_workspace_bytes(E, N, rows_alloc) -> int:

@@ -27,6 +27,8 @@ template <> struct Unit<uint16_t> {
   uint4 v;
   __device__ __forceinline__ void load(const uint16_t* p) { v = *reinterpret_cast<const uint4*>(p); }
   __device__ __forceinline__ void get(float* f) const { unpack8(v, f); }
+  __device__ __forceinline__ void set(const float* f) { v = pack8(f); }   // rounds
+  __device__ __forceinline__ void store(uint16_t* p) const { *reinterpret_cast<uint4*>(p) = v; }
 };
 template <> struct Unit<float> {
   uint4 lo, hi;
@@ -38,17 +40,28 @@ template <> struct Unit<float> {
     Elem<float>::load(lo, f);
     Elem<float>::load(hi, f + 4);
   }
+  __device__ __forceinline__ void set(const float* f) {
+    lo = Elem<float>::store(f);
+    hi = Elem<float>::store(f + 4);
+  }
+  __device__ __forceinline__ void store(float* p) const {
+    reinterpret_cast<uint4*>(p)[0] = lo;
+    reinterpret_cast<uint4*>(p)[1] = hi;
+  }
 };
 
 // Largest |value| of a unit as bits: NaNs order above infinity and infinity
 // above every number, which a maximum of floats would lose.
+__device__ __forceinline__ uint32_t abs_bits_max(const float (&f)[8], uint32_t m) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) m = max(m, __float_as_uint(f[e]) & 0x7FFFFFFFu);
+  return m;
+}
 template <typename T>
 __device__ __forceinline__ uint32_t abs_bits_max(const Unit<T>& u, uint32_t m) {
   float f[8];
   u.get(f);
-#pragma unroll
-  for (int e = 0; e < 8; ++e) m = max(m, __float_as_uint(f[e]) & 0x7FFFFFFFu);
-  return m;
+  return abs_bits_max(f, m);
 }
 
 // How a row is divided: pre (1, or 2^64 where the row's values are so small
@@ -71,10 +84,8 @@ __device__ __forceinline__ RowScale row_scale(uint32_t amax, float& scale) {
 // quotient lies next to a half.  r = x - q s is exact in fp32 (it is a multiple of
 // half the last place of s and at most about s / 2), so comparing it with
 // s / 2 settles those cases; they are rare enough to branch on.
-template <typename T>
-__device__ __forceinline__ uint2 quantize8(const Unit<T>& u, const RowScale& rs) {
-  float f[8], q[8];
-  u.get(f);
+__device__ __forceinline__ uint2 quantize8(float (&f)[8], const RowScale& rs) {
+  float q[8];
   bool border = false;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
@@ -96,6 +107,12 @@ __device__ __forceinline__ uint2 quantize8(const Unit<T>& u, const RowScale& rs)
     b[e] = static_cast<uint32_t>(static_cast<int>(fminf(fmaxf(q[e], -127.f), 127.f))) & 255u;
   return make_uint2(b[0] | b[1] << 8 | b[2] << 16 | b[3] << 24,
                     b[4] | b[5] << 8 | b[6] << 16 | b[7] << 24);
+}
+template <typename T>
+__device__ __forceinline__ uint2 quantize8(const Unit<T>& u, const RowScale& rs) {
+  float f[8];
+  u.get(f);
+  return quantize8(f, rs);
 }
 
 }  // namespace

@@ -1,0 +1,97 @@
+"""What the operators around the layer refuse, on the CPU: the binding before any
+device access, the C entry points before any launch."""
+import ctypes
+import math
+
+import pytest
+import torch
+
+from paper_2205_01848_amd import binding as B
+
+bf16, f32, i32, i8, u8 = torch.bfloat16, torch.float32, torch.int32, torch.int8, torch.uint8
+EINVAL, EWORKSPACE = 1, 4
+
+
+def z(*s, dt=f32):
+    return torch.zeros(*s, dtype=dt)
+
+
+def passes_checks(fn, **kw):
+    """fn(**kw) gets past the size and type checks: it fails only for want of a device."""
+    with pytest.raises((B.MoEError, RuntimeError)) as e:
+        fn(**kw)
+    assert "device memory" in str(e.value) or "GPU" in str(e.value), e.value
+
+
+def refuses(match, fn, **kw):
+    with pytest.raises(B.MoEError, match=match):
+        fn(**kw)
+
+
+NORM = dict(x=z(5, 24), weight=z(24), eps=1e-5, y=z(5, 24), add=z(5, 24), sum=z(5, 24), rstd=z(5),
+            q=z(5, 32, dt=i8), scale=z(5))
+NORM_BWD = dict(s=z(5, 24), weight=z(24), rstd=z(5), dy=z(5, 24), dx=z(5, 24), dw=z(24), ws=z(4096, dt=u8),
+                dsum=z(5, 24))
+CALLS = [(B.moe_rms_norm_fwd, NORM, "x"), (B.moe_rms_norm_bwd, NORM_BWD, "s")]
+OPERANDS = [(fn, kw, n) for fn, kw, first in CALLS for n, t in kw.items()
+            if torch.is_tensor(t) and n not in ("ws", first)]
+
+
+@pytest.mark.parametrize("fn,kw", [c[:2] for c in CALLS], ids=lambda v: getattr(v, "__name__", ""))
+def test_sizes_that_fit_reach_the_device_check(fn, kw):
+    passes_checks(fn, **kw)
+
+
+@pytest.mark.parametrize("fn,kw,name", OPERANDS)
+def test_every_operand_too_small_or_of_another_type(fn, kw, name):
+    t = kw[name]
+    refuses(name, fn, **dict(kw, **{name: t[:-1].contiguous()}))
+    refuses(name, fn, **dict(kw, **{name: t.to(torch.float64)}))
+
+
+@pytest.mark.parametrize("fn,kw,name", [o for o in OPERANDS if o[1][o[2]].dim() == 2 and o[2] != "q"])
+def test_rows_with_gaps(fn, kw, name):
+    passes_checks(fn, **dict(kw, **{name: z(5, 32)[:, :24]}))
+    refuses(name, fn, **dict(kw, **{name: z(5, 28)[:, :24]}))          # 28 elements apart
+    refuses(name, fn, **dict(kw, **{name: z(24, 5).T}))
+
+
+P = ctypes.c_void_p(4096)       # an aligned address that is never read
+
+
+def _norm(lib, dt=1, rows=5, d=24, x=P, ldx=24, add=P, ldadd=24, w=P, eps=1e-5, sum=ctypes.c_void_p(8192), ldsum=24,
+          y=P, ldy=24, rstd=None, q=None, scale=None):
+    return lib.moe_rms_norm_fwd(None, dt, rows, d, x, ldx, add, ldadd, w, eps, sum, ldsum, y, ldy, rstd, q, scale)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(dt=2), dict(rows=-1), dict(d=0), dict(d=20), dict(d=32776, ldx=32776, ldadd=32776, ldsum=32776, ldy=32776),
+    dict(x=None), dict(w=None), dict(eps=0.0), dict(eps=-1.0), dict(eps=math.inf), dict(eps=math.nan),
+    dict(ldx=16), dict(ldx=28), dict(ldadd=20), dict(ldsum=16), dict(ldy=23), dict(y=None), dict(q=P), dict(scale=P),
+    dict(add=None), dict(sum=P), dict(x=ctypes.c_void_p(4100)), dict(y=ctypes.c_void_p(4104)),
+    dict(q=ctypes.c_void_p(4097), scale=P), dict(w=ctypes.c_void_p(4098))], ids=str)
+def test_norm_refuses(kw):
+    assert _norm(B.lib(), **kw) == EINVAL
+
+
+def _norm_bwd(lib, dt=1, rows=5, d=24, s=P, lds=24, w=P, rstd=P, dy=P, lddy=24, dsum=P, lddsum=24, dx=P, lddx=24,
+              dw_dt=1, dw=P, ws=P, nws=1 << 20):
+    return lib.moe_rms_norm_bwd(None, dt, rows, d, s, lds, w, rstd, dy, lddy, dsum, lddsum, dx, lddx, dw_dt, dw, ws, nws)
+
+
+@pytest.mark.parametrize("kw,st", [
+    (dict(dt=3), EINVAL), (dict(rows=-1), EINVAL), (dict(d=12), EINVAL), (dict(s=None), EINVAL), (dict(w=None), EINVAL),
+    (dict(rstd=None), EINVAL), (dict(dy=None), EINVAL), (dict(dx=None), EINVAL), (dict(lds=23), EINVAL),
+    (dict(lddy=16), EINVAL), (dict(lddsum=25), EINVAL), (dict(lddx=16), EINVAL), (dict(dw_dt=2), EINVAL),
+    (dict(dt=0, dw_dt=1), EINVAL), (dict(dx=ctypes.c_void_p(4104)), EINVAL), (dict(ws=None), EWORKSPACE),
+    (dict(nws=2 * 24 * 4 - 1), EWORKSPACE), (dict(ws=ctypes.c_void_p(4100)), EWORKSPACE)], ids=str)
+def test_norm_bwd_refuses(kw, st):
+    assert _norm_bwd(B.lib(), **kw) == st
+
+
+def test_norm_workspace():
+    """One partial sum a workgroup, 512 at most; nothing for sizes the call refuses."""
+    q = B.moe_rms_norm_bwd_workspace_bytes
+    assert q(0, 24) == q(1, 24) == q(4, 24) == 96 and q(5, 24) == 192 and q(1 << 40, 4096) == 512 * 4096 * 4
+    assert q(3, 4096) == 3 * 4096 * 4
+    assert q(-1, 24) == q(5, 20) == q(5, 32776) == 0
