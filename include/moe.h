@@ -707,6 +707,79 @@ moe_status moe_gated_ffn_bwd(void* stream, moe_dtype dt, moe_act act, int T,
                              void* dw3, void* dw2, void* workspace,
                              size_t workspace_bytes);
 
+/* ---- the weights' step ---------------------------------------------------- */
+
+/*
+ * A tensor of the step: n values, each array contiguous and 16-byte aligned (but
+ * for the exponents).
+ *   p       [n] weights in p_dtype, in/out;  g [n] gradients in g_dtype
+ *   master  NULL, or [n] float32: the weights' originals, in/out; p is then
+ *           their rounding (p_dtype MOE_BF16).  Without it p is itself updated:
+ *           a change below half its last place is lost
+ *   m, v    the moments, in/out, all zeros at first: float32 [n] where m_exp and
+ *           v_exp are NULL, else uint8 [n], with m_exp, v_exp uint8
+ *           [moe_adamw_blocks(n)]: a block of 128 values shares an exponent e, and
+ *           code c stands for the float with the bits
+ *             m: (c % 128 + 8 (e - 15)) << 20, negative where c > 128; 128 is NaN
+ *             v: (c + 16 (e - 15)) << 19
+ *           and 0 for c = 0: 16 octaves with 3 and with 4 bits of mantissa
+ *   weight_decay >= 0
+ * No array overlaps another (a weight listed twice is updated by two steps at once).
+ */
+typedef struct moe_adamw_tensor {
+  void* p;
+  const void* g;
+  float* master;
+  void *m, *v;
+  uint8_t *m_exp, *v_exp;
+  int64_t n;
+  double weight_decay;
+  moe_dtype p_dtype, g_dtype;
+} moe_adamw_tensor;
+
+/* What changes from step to step, in device memory, for a step captured in a
+ * graph: c1 = 1 / (1 - beta1^t), c2 = 1 / sqrt(1 - beta2^t). */
+typedef struct moe_adamw_schedule {
+  float lr, c1, c2;
+  uint32_t seed;
+} moe_adamw_schedule;
+
+/* Exponents of n 8-bit values: n / 128, rounded up (0 for n < 0). [host] */
+size_t moe_adamw_blocks(int64_t n);
+
+/*
+ * moe_adamw - one AdamW step over a list of tensors, 40 a launch:
+ *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2
+ *   p = p (1 - lr weight_decay)
+ *       - lr m / (1 - beta1^step) / (sqrt(v / (1 - beta2^step)) + eps)
+ * in float32; moments kept in 8 bits are formed in float64 (each product rounded
+ * by itself, g^2 before its factor), used for p before they are rounded, and rounded to the code above or below at random, with the probability that
+ * makes the code right on average (a v above 0 is kept above 0, an m 16 octaves
+ * below its block's largest becomes 0).  The random bits depend on seed, the
+ * tensor's place in the list and the element alone: give every step another seed.
+ * An m that is not a finite float32 is kept as NaN; a v that is not, as its block's
+ * largest value.
+ *   tensors    [host] [count] (read before the call returns)
+ *   lr, eps    lr >= 0, eps > 0, finite; 0 <= beta < 1; step >= 1
+ *   grad_scale NULL, or device [1]: every gradient is multiplied by it (a clipping
+ *              factor, the inverse of a loss scale)
+ *   schedule   NULL, or device: replaces lr, the corrections of `step`, and seed
+ */
+moe_status moe_adamw(void* stream, int count, const moe_adamw_tensor* tensors,
+                     double lr, double beta1, double beta2, double eps,
+                     int64_t step, uint32_t seed, const float* grad_scale,
+                     const moe_adamw_schedule* schedule);
+
+/*
+ * moe_adamw_unpack - the values 8-bit moments stand for (to save them, or to go on
+ * with 32-bit ones): m[i], v[i] [host arrays of count device pointers] float32 [n]
+ * out, 16-byte aligned, for every tensor of the list, all of them with exponents.
+ * p, g and master are not read.
+ */
+moe_status moe_adamw_unpack(void* stream, int count,
+                            const moe_adamw_tensor* tensors, float* const* m,
+                            float* const* v);
+
 /*
  * Kernel timing (instrumentation; not part of the method).  While enabled,
  * every kernel the library launches is bracketed by two HIP events recorded

@@ -10,7 +10,8 @@ import numpy as np
 from .blocks import quantize_rows
 from .moe_oracle import round_to
 
-__all__ = ["rms_norm_fwd", "rms_norm_bwd", "rms_norm_rows_i8"]
+__all__ = ["rms_norm_fwd", "rms_norm_bwd", "rms_norm_rows_i8", "adamw", "adamw_random", "adamw_encode",
+           "adamw_decode"]
 
 
 # ---- norm ------------------------------------------------------------------------
@@ -39,3 +40,66 @@ def rms_norm_bwd(s, r, weight, dy, dsum=None):
     g = dy * weight
     dx = r[:, None] * (g - s * (r * r * (g * s).mean(axis=1))[:, None])
     return dx if dsum is None else dx + dsum, (dy * s * r[:, None]).sum(axis=0)
+
+
+# ---- AdamW -----------------------------------------------------------------------
+def adamw(p, g, m, v, lr, beta1, beta2, eps, step, weight_decay=0.0):
+    """(p, m, v) after one step, unrounded."""
+    m = beta1 * m + (1 - beta1) * g
+    v = beta2 * v + (1 - beta2) * (g * g)
+    with np.errstate(invalid="ignore", over="ignore"):
+        p = p - lr * (weight_decay * p + m / (1 - beta1 ** step) / (np.sqrt(v / (1 - beta2 ** step)) + eps))
+    return p, m, v
+
+
+def adamw_random(n, seed, tensor, start=0):
+    """The 16 random bits for m and the 16 for v of elements start .. start + n - 1 of the list's
+    tensor number `tensor`."""
+    u = np.uint32
+    i = np.arange(start, start + n, dtype=np.uint64)
+    lo, hi = (i & 0xFFFFFFFF).astype(u), (i >> 32).astype(u)
+    with np.errstate(over="ignore"):
+        key = u(seed & 0xFFFFFFFF) ^ u((tensor + 1) * 0x9E3779B9 & 0xFFFFFFFF)
+        h = lo * u(0xBB67AE85) + hi * u(0x6A09E667) + key
+        h = (h ^ (h >> u(16))) * u(0x9E3779B1)
+        h = (h ^ (h >> u(15))) * u(0x85157AF5)
+        h ^= h >> u(16)
+    return (h & u(0xFFFF)).astype(np.int64), (h >> u(16)).astype(np.int64)
+
+
+def _blocks(a, fill):
+    out = np.full(-(-len(a) // 128) * 128, fill, dtype=a.dtype)
+    out[:len(a)] = a
+    return out.reshape(-1, 128)
+
+
+def adamw_encode(x, rnd, mant):
+    """(code, exponent per block) of values in float64: m (mant 3, with sign) or v (mant 4).  Counted
+    in steps of 2^-mant of the value's octave, the random 16 bits decide on the step begun."""
+    x = np.asarray(x, np.float64)
+    with np.errstate(invalid="ignore", divide="ignore"):
+        size = np.abs(x)
+        some = np.isfinite(size) & (size > 0)
+        frac, octave = np.frexp(np.where(some, size, 1.0))        # frac in [1/2, 1)
+        steps = np.floor(frac * 2 ** (mant + 1) + rnd / 65536).astype(np.int64)   # 2^mant .. 2^(mant+1)
+        octave = octave.astype(np.int64) - 1 + 127                # the float32 exponent
+    carry = steps == 2 ** (mant + 1)
+    octave, steps = octave + carry, np.where(carry, 2 ** mant, steps)
+    beyond = ~np.isfinite(size) | (some & (octave > 254))
+    e = np.maximum(_blocks(np.where(some & ~beyond, octave, 16), 16).max(axis=1), 16)
+    top = np.repeat(e, 128)[:len(x)]
+    code = (octave - (top - 15)) * 2 ** mant + steps - 2 ** mant
+    code = np.where(some & (code > 0), code, 0)
+    if mant == 3:
+        code = np.where(beyond, 128, np.where((code > 0) & (x < 0), code + 128, code))
+    else:
+        code = np.where(beyond, 255, np.where((code == 0) & some, 1, code))
+    return code.astype(np.uint8), e.astype(np.uint8)
+
+
+def adamw_decode(code, e, mant):
+    c = np.asarray(code, np.int64)
+    size = c & 127 if mant == 3 else c
+    octave = np.repeat(np.asarray(e, np.int64), 128)[:len(c)] - 15 + size // 2 ** mant
+    x = np.where(size > 0, (1 + size % 2 ** mant / 2 ** mant) * 2.0 ** (octave - 127.0), 0.0)
+    return np.where(c == 128, np.nan, np.where(c > 128, -x, x)) if mant == 3 else x

@@ -40,6 +40,12 @@ class LayerFwdArgs(ctypes.Structure):
                  ("ffn_ws_bytes", _c_size)])
 
 
+class AdamWTensorArgs(ctypes.Structure):
+    """moe_adamw_tensor."""
+    _fields_ = ([(n, _p) for n in ("p", "g", "master", "m", "v", "m_exp", "v_exp")] +
+                [("n", _c_i64), ("weight_decay", ctypes.c_double), ("p_dtype", _c_int), ("g_dtype", _c_int)])
+
+
 # name -> (restype, argtypes)
 SIGNATURES = {
     "moe_status_string": (ctypes.c_char_p, [_c_int]),
@@ -116,6 +122,10 @@ SIGNATURES = {
     "moe_gated_ffn_bwd": (_c_int, [_p, _c_int, _c_int, _c_int, _c_int, _c_int, _p, _c_i64, _p, _p,
                                    _p, _p, _p, _c_i64, _p, _c_i64, _p, _c_i64, _c_int, _p, _p, _p,
                                    _p, _c_size]),
+    "moe_adamw_blocks": (_c_size, [_c_i64]),
+    "moe_adamw": (_c_int, [_stream_p, _c_int, ctypes.POINTER(AdamWTensorArgs)] +
+                  [ctypes.c_double] * 4 + [_c_i64, ctypes.c_uint32, _p, _p]),
+    "moe_adamw_unpack": (_c_int, [_stream_p, _c_int, ctypes.POINTER(AdamWTensorArgs), _p, _p]),
     "moe_timing_enable": (_c_int, [_c_int]),
     "moe_set_gemm_tiles": (_c_int, [_c_int]),
     "moe_set_dx_weight_copy": (_c_int, [_c_int]),
@@ -880,6 +890,98 @@ class CapacityPolicy:
             self.close()
         except Exception:
             pass
+
+
+# ---- the weights' step ------------------------------------------------------------
+ADAMW_BLOCK = 128       # values of an 8-bit state that share an exponent
+
+
+def adamw_blocks(n: int) -> int:
+    """Exponents of n values in 8 bits."""
+    return -(-n // ADAMW_BLOCK)
+
+
+class AdamWTensor:
+    """One tensor of the step: weights p, gradients g (float32 or bf16), moments m and v (float32,
+    or uint8 with the exponents m_exp and v_exp, uint8 [adamw_blocks(n)]), and the float32 originals
+    of bf16 weights (master), all of n values."""
+
+    __slots__ = ("p", "g", "m", "v", "master", "m_exp", "v_exp", "weight_decay")
+
+    def __init__(self, p, g, m, v, master=None, m_exp=None, v_exp=None, weight_decay=0.0):
+        n, state = p.numel(), _F32 if m_exp is None else torch.uint8
+        if master is not None and p.dtype != torch.bfloat16:
+            raise MoEError("master: only bf16 weights have float32 originals")
+        if (m_exp is None) != (v_exp is None):
+            raise MoEError("m_exp and v_exp: both or neither")
+        _dt(p), _dt(g)
+        for t, count, name, dtype in ((g, n, "g", g.dtype), (m, n, "m", state), (v, n, "v", state),
+                                      (master, n, "master", _F32), (m_exp, adamw_blocks(n), "m_exp", state),
+                                      (v_exp, adamw_blocks(n), "v_exp", state)):
+            _need(t, count, name, dtype, optional=name in ("master", "m_exp", "v_exp"))
+            if t is not None and t.numel() != count:
+                raise MoEError(f"{name} holds {t.numel()} elements, expected {count}")
+        self.p, self.g, self.m, self.v, self.master = p, g, m, v, master
+        self.m_exp, self.v_exp, self.weight_decay = m_exp, v_exp, float(weight_decay)
+
+    def arrays(self):
+        return [t for t in (self.p, self.g, self.m, self.v, self.master, self.m_exp, self.v_exp) if t is not None]
+
+
+class AdamWList:
+    """Tensors of one device, checked and laid out once for moe_adamw; their memory has to stay where
+    it is (the list keeps the tensors)."""
+
+    def __init__(self, tensors):
+        self.tensors = list(tensors)
+        every = [a for t in self.tensors for a in t.arrays()]
+        self.device = _device_of(*every)
+        written = sorted((a.data_ptr(), a.data_ptr() + _nbytes(a)) for t in self.tensors for a in t.arrays()
+                         if a is not t.g and a.numel())
+        if any(a[1] > b[0] for a, b in zip(written, written[1:])):
+            raise MoEError("weights or moments overlap: a tensor is listed twice")
+        self.args = (AdamWTensorArgs * len(self.tensors))(*[
+            AdamWTensorArgs(*[_ptr(a) for a in (t.p, t.g, t.master, t.m, t.v, t.m_exp, t.v_exp)], t.p.numel(),
+                            t.weight_decay, _dt(t.p), _dt(t.g)) for t in self.tensors])
+
+
+def adamw_schedule(lr, beta1, beta2, step, seed=0) -> torch.Tensor:
+    """float32 [4] on the host with the bits of moe_adamw_schedule, to copy to the device tensor that a
+    captured step reads."""
+    t = torch.tensor([lr, 1 / (1 - beta1 ** step), (1 - beta2 ** step) ** -0.5, 0.0], dtype=_F32)
+    t.view(torch.int32)[3] = (int(seed) & 0xFFFFFFFF) - ((int(seed) & 0x80000000) << 1)
+    return t
+
+
+def moe_adamw(tensors: AdamWList, lr, beta1, beta2, eps, step, seed=0, grad_scale=None, schedule=None):
+    """One AdamW step over the list; grad_scale [1] and schedule [4] (adamw_schedule) on the device."""
+    _need(grad_scale, 1, "grad_scale", _F32, optional=True)
+    _need(schedule, 4, "schedule", _F32, optional=True)
+    if not tensors.tensors:
+        return
+    if _device_of(tensors.tensors[0].p, grad_scale, schedule) != tensors.device:
+        raise MoEError(f"grad_scale or schedule lies elsewhere than the tensors' device {tensors.device}")
+    with _Here(tensors.device) as stream:
+        _check(lib().moe_adamw(stream, len(tensors.args), tensors.args, lr, beta1, beta2, eps, step,
+                               int(seed) & 0xFFFFFFFF, _ptr(grad_scale), _ptr(schedule)), "moe_adamw")
+
+
+def moe_adamw_unpack(tensors: AdamWList, values):
+    """values: for every tensor of the list, float32 tensors [n] that take what its m and v stand for."""
+    if len(values) != len(tensors.tensors):
+        raise MoEError(f"{len(values)} pairs of values for {len(tensors.tensors)} tensors")
+    for t, pair in zip(tensors.tensors, values):
+        for a in pair:
+            _need(a, t.p.numel(), "values", _F32)
+        if t.m_exp is None:
+            raise MoEError("a tensor of the list has its moments in 32 bits")
+        if _device_of(*pair) != tensors.device:
+            raise MoEError(f"values lie elsewhere than the tensors' device {tensors.device}")
+    if not values:
+        return
+    m, v = ((_p * len(values))(*[_ptr(pair[k]) for pair in values]) for k in (0, 1))
+    with _Here(tensors.device) as stream:
+        _check(lib().moe_adamw_unpack(stream, len(values), tensors.args, m, v), "moe_adamw_unpack")
 
 
 # ---- kernel timing (instrumentation) ----------------------------------------

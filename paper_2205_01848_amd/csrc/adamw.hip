@@ -1,0 +1,394 @@
+// AdamW over many tensors in one launch (40 a launch), with states in 32 or in 8 bits:
+//     m = b1 m + (1 - b1) g,  v = b2 v + (1 - b2) g^2   (g times an optional device scale)
+//     p = p (1 - lr wd) - lr m / (1 - b1^t) / (sqrt(v / (1 - b2^t)) + eps)
+// p taken from, and kept in, a 32-bit original where the tensor has one.
+//
+// States in 8 bits.  A block of 128 values shares one exponent e, that of its largest,
+// kept in a byte; a value keeps the leading bits of its 32-bit number, counted down from
+// the block's top octave: code c stands for the float with the bits
+//     (c + ((e - 15) << k)) << (23 - k),     0 for c = 0,
+// k = 3 bits of mantissa for m beside its sign, k = 4 for v, so both span 16 octaves.
+// Encoding and decoding are integer additions and shifts, and a block whose values
+// all shrink alike keeps its codes and lowers e.
+//
+// The bits that are dropped round up with the probability that they are worth.  Rounded
+// to nearest, a step of b2 = 0.999 could not move v, whose codes lie 1/32 to 1/16 apart: its
+// change of at most a thousandth a step is lost unless g^2 is more than 30 v, so v
+// would climb with outliers and never come down.  Rounded at random the codes are right on
+// average.  A v above 0 never becomes 0, where the next step would divide m by eps.
+// The random bits are a function of (seed, tensor, element), so a step can be repeated.
+//
+// So that a value's code does not depend on how its sums were rounded, the moments of
+// 8-bit states are formed in float64, whose operations run at the rate of those of
+// float32 here, and the code is taken from its high word (20 of the 52 bits of
+// mantissa, 17 or 16 of them behind the code's, are all that the random bits reach).
+// Every product is rounded by itself: with decimal betas sums like (9 m + g) / 10 lie
+// exactly on the borders that the random bits draw often enough (2 of 40 million) for a
+// fused multiply-add to give other codes than the formula written out.
+//
+// Bound by memory: bf16 weights, fp32 gradients and 8-bit states take 12 bytes a value,
+// 32-bit states and originals beside them 32.  A thread takes 8 neighbouring values, so a
+// block of 128 is a row of 16 lanes, whose maximum four DPP steps find.
+
+#include <algorithm>
+#include <cmath>
+
+#include "common.hpp"
+#include "validate.hpp"
+
+namespace moe {
+namespace {
+
+constexpr int kList = 40;              // tensors of a launch (kernel arguments: at most 4 KB)
+constexpr int kAdamThreads = 256;
+constexpr int kTile = kAdamThreads * 8;
+constexpr int kBlock = 128;            // values that share an exponent
+
+struct AdamTensor {
+  void* p;
+  const void* g;
+  float* master;
+  void *m, *v;
+  uint8_t *m_exp, *v_exp;
+  int64_t n;
+  float decay;
+  uint32_t key;        // of its random bits, but for the seed
+  int first;           // its first chunk
+  int p16, g16;        // bf16
+};
+struct AdamArgs {
+  AdamTensor t[kList];
+  int count, chunks, tiles;   // tiles a chunk
+  float lr, c1, c2, eps;      // c1 = 1 / (1 - b1^t), c2 = 1 / sqrt(1 - b2^t)
+  double b1, b2, a1, a2;      // a = 1 - b
+  uint32_t seed;
+  const float* grad_scale;
+  const moe_adamw_schedule* schedule;
+};
+static_assert(sizeof(AdamArgs) <= 4096, "kernel arguments");
+
+// The tensor of a chunk: the last one that starts at or before it (empty tensors have no
+// chunk).  All on scalars.
+__device__ __forceinline__ int find_tensor(const AdamArgs& a, int chunk) {
+  int lo = 0, hi = a.count;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (a.t[mid].first <= chunk) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+
+// 8 values from p + i on, `left` of them there (8 or more: all).
+__device__ __forceinline__ void load8(const void* p, bool b16, int64_t i, int64_t left, float (&f)[8]) {
+  if (left >= 8) {
+    if (b16) {
+      unpack8(*reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + i), f);
+    } else {
+      const uint4* q = reinterpret_cast<const uint4*>(static_cast<const float*>(p) + i);
+      const uint4 a = q[0], b = q[1];
+      Elem<float>::load(a, f);
+      Elem<float>::load(b, f + 4);
+    }
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    f[e] = e >= left ? 0.f : b16 ? bf2f(static_cast<const uint16_t*>(p)[i + e]) : static_cast<const float*>(p)[i + e];
+}
+__device__ __forceinline__ void store8(void* p, bool b16, int64_t i, int64_t left, const float (&f)[8]) {
+  if (left >= 8) {
+    if (b16) {
+      *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p) + i) = pack8(f);
+    } else {
+      uint4* q = reinterpret_cast<uint4*>(static_cast<float*>(p) + i);
+      q[0] = Elem<float>::store(f);
+      q[1] = Elem<float>::store(f + 4);
+    }
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if (e < left) {
+      if (b16) static_cast<uint16_t*>(p)[i + e] = f2bf(f[e]);
+      else static_cast<float*>(p)[i + e] = f[e];
+    }
+}
+__device__ __forceinline__ uint2 load_codes(const void* p, int64_t i, int64_t left) {
+  const uint8_t* q = static_cast<const uint8_t*>(p) + i;
+  if (left >= 8) return *reinterpret_cast<const uint2*>(q);
+  uint32_t w[2] = {0, 0};
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if (e < left) w[e / 4] |= static_cast<uint32_t>(q[e]) << (e % 4 * 8);
+  return make_uint2(w[0], w[1]);
+}
+__device__ __forceinline__ void store_codes(void* p, int64_t i, int64_t left, const uint32_t (&c)[8]) {
+  uint8_t* q = static_cast<uint8_t*>(p) + i;
+  if (left >= 8) {
+    *reinterpret_cast<uint2*>(q) = make_uint2(c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24,
+                                              c[4] | c[5] << 8 | c[6] << 16 | c[7] << 24);
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if (e < left) q[e] = static_cast<uint8_t>(c[e]);
+}
+
+// What code c of a block with exponent e stands for.
+__device__ __forceinline__ float decode_m(uint32_t c, int base) {
+  const uint32_t size = c & 127;
+  const float x = __uint_as_float(((size + base) << 20) | (c & 128) << 24);
+  return size ? x : c ? NAN : 0.f;
+}
+__device__ __forceinline__ float decode_v(uint32_t c, int base) {
+  return c ? __uint_as_float((c + base) << 19) : 0.f;
+}
+
+// The largest of a row of 16 lanes, in all of them.
+template <int CTRL> __device__ __forceinline__ int dpp_max(int v) {
+  return max(v, __builtin_amdgcn_update_dpp(v, v, CTRL, 0xF, 0xF, false));
+}
+__device__ __forceinline__ int row16_max(int v) {
+  v = dpp_max<0xB1>(v);    // lanes 1 apart, then 2, then the other half of 8, of 16
+  v = dpp_max<0x4E>(v);
+  v = dpp_max<0x141>(v);
+  return dpp_max<0x140>(v);
+}
+
+// The element's random bits: 16 low ones for m, 16 high ones for v.
+__device__ __forceinline__ uint32_t random_bits(uint32_t x) {
+  x = (x ^ x >> 16) * 0x9E3779B1u;
+  x = (x ^ x >> 15) * 0x85157AF5u;
+  return x ^ x >> 16;
+}
+
+// b x + a y in float64, three roundings.
+__device__ __forceinline__ double mix(double b, double x, double a, double y) {
+#pragma clang fp contract(off)
+  const double p = b * x, q = a * y;
+  return p + q;
+}
+
+struct AdamStep {
+  float lr, c1, c2, scale;
+  uint32_t seed;
+};
+
+__device__ __forceinline__ void update(float (&p)[8], const float (&m)[8], const float (&v)[8],
+                                       const AdamStep& st, float keep, float eps) {
+  const float rate = st.lr * st.c1;
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    p[e] = p[e] * keep - rate * m[e] / (__builtin_sqrtf(v[e]) * st.c2 + eps);
+}
+
+__global__ __launch_bounds__(kAdamThreads) void adamw_kernel(const AdamArgs a) {
+  AdamStep st = {a.lr, a.c1, a.c2, a.grad_scale ? *a.grad_scale : 1.f, a.seed};
+  if (a.schedule) {
+    st.lr = a.schedule->lr;
+    st.c1 = a.schedule->c1;
+    st.c2 = a.schedule->c2;
+    st.seed = a.schedule->seed;
+  }
+  const int ti = find_tensor(a, blockIdx.x);
+  const AdamTensor& t = a.t[ti];
+  const int64_t i0 = static_cast<int64_t>(static_cast<int>(blockIdx.x) - t.first) * a.tiles * kTile;
+  const float keep = 1.f - st.lr * t.decay;
+  for (int k = 0; k < a.tiles; ++k) {
+    const int64_t i = i0 + k * kTile + threadIdx.x * 8, left = t.n - i;
+    if (i0 + k * kTile >= t.n) break;
+    float g[8], p[8], m[8], v[8];
+    load8(t.g, t.g16, i, left, g);
+    if (t.master) load8(t.master, false, i, left, p);
+    else load8(t.p, t.p16, i, left, p);
+    if (!t.m_exp) {
+      load8(t.m, false, i, left, m);
+      load8(t.v, false, i, left, v);
+      const float b1 = static_cast<float>(a.b1), b2 = static_cast<float>(a.b2);
+      const float a1 = static_cast<float>(a.a1), a2 = static_cast<float>(a.a2);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        g[e] *= st.scale;
+        m[e] = b1 * m[e] + a1 * g[e];
+        v[e] = b2 * v[e] + a2 * (g[e] * g[e]);
+      }
+      store8(t.m, false, i, left, m);
+      store8(t.v, false, i, left, v);
+    } else {
+      const uint2 mc = load_codes(t.m, i, left), vc = load_codes(t.v, i, left);
+      const int64_t blk = i / kBlock;
+      const bool here = left > 0;
+      const int me = here ? t.m_exp[blk] : 15, ve = here ? t.v_exp[blk] : 15;
+      const uint32_t x0 = static_cast<uint32_t>(i) * 0xBB67AE85u + static_cast<uint32_t>(i >> 32) * 0x6A09E667u +
+                          (st.seed ^ t.key);
+      uint32_t mq[8], vq[8];
+      int mt[8], vt[8], mtop = 16, vtop = 16;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t cm = (e < 4 ? mc.x : mc.y) >> (e % 4 * 8) & 255, cv = (e < 4 ? vc.x : vc.y) >> (e % 4 * 8) & 255;
+        const double gd = static_cast<double>(g[e]) * st.scale;
+        const double md = mix(a.b1, decode_m(cm, (me - 15) * 8), a.a1, gd);
+        const double vd = mix(a.b2, decode_v(cv, (ve - 15) * 16), a.a2, gd * gd);
+        m[e] = static_cast<float>(md);
+        v[e] = static_cast<float>(vd);
+        const uint32_t rnd = random_bits(x0 + e * 0xBB67AE85u);
+        const uint32_t mh = static_cast<uint32_t>(__double2hiint(md)), vh = static_cast<uint32_t>(__double2hiint(vd));
+        mt[e] = static_cast<int>(((mh & 0x7FFFFFFFu) + ((rnd & 0xFFFF) << 1)) >> 17) - ((1023 - 127) << 3);
+        vt[e] = static_cast<int>(((vh & 0x7FFFFFFFu) + (rnd >> 16)) >> 16) - ((1023 - 127) << 4);
+        mq[e] = mh >> 31 << 7;
+        vq[e] = vd > 0 ? 1 : 0;
+        // (beyond the 32-bit numbers, and NaN: not counted)
+        if (mt[e] < 255 << 3) mtop = max(mtop, mt[e] >> 3);
+        if (vt[e] < 255 << 4) vtop = max(vtop, vt[e] >> 4);
+      }
+      mtop = row16_max(mtop);
+      vtop = row16_max(vtop);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int c = mt[e] - (mtop - 15) * 8, d = vt[e] - (vtop - 15) * 16;
+        mq[e] = mt[e] >= 255 << 3 ? 128 : c > 0 ? mq[e] | c : 0;
+        vq[e] = vt[e] >= 255 << 4 ? 255 : max(d, static_cast<int>(vq[e]));
+      }
+      store_codes(t.m, i, left, mq);
+      store_codes(t.v, i, left, vq);
+      if (here && threadIdx.x % (kBlock / 8) == 0) {
+        t.m_exp[blk] = static_cast<uint8_t>(mtop);
+        t.v_exp[blk] = static_cast<uint8_t>(vtop);
+      }
+    }
+    update(p, m, v, st, keep, a.eps);
+    if (t.master) store8(t.master, false, i, left, p);
+    store8(t.p, t.p16, i, left, p);
+  }
+}
+
+// The values of 8-bit states: t.m, t.v to the 32-bit t.p and t.master.
+__global__ __launch_bounds__(kAdamThreads) void adamw_unpack_kernel(const AdamArgs a) {
+  const int ti = find_tensor(a, blockIdx.x);
+  const AdamTensor& t = a.t[ti];
+  const int64_t i0 = static_cast<int64_t>(static_cast<int>(blockIdx.x) - t.first) * a.tiles * kTile;
+  for (int k = 0; k < a.tiles; ++k) {
+    const int64_t i = i0 + k * kTile + threadIdx.x * 8, left = t.n - i;
+    if (left <= 0) break;
+    const uint2 mc = load_codes(t.m, i, left), vc = load_codes(t.v, i, left);
+    const int mb = (t.m_exp[i / kBlock] - 15) * 8, vb = (t.v_exp[i / kBlock] - 15) * 16;
+    float m[8], v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      m[e] = decode_m((e < 4 ? mc.x : mc.y) >> (e % 4 * 8) & 255, mb);
+      v[e] = decode_v((e < 4 ? vc.x : vc.y) >> (e % 4 * 8) & 255, vb);
+    }
+    store8(t.p, false, i, left, m);
+    store8(t.master, false, i, left, v);
+  }
+}
+
+bool tensor_ok(const moe_adamw_tensor& t) {
+  if (t.n < 0 || !dtype_ok(t.p_dtype) || !dtype_ok(t.g_dtype)) return false;
+  if (!(t.weight_decay >= 0) || !(t.weight_decay < INFINITY)) return false;
+  if (!t.m_exp != !t.v_exp || (t.master && t.p_dtype == MOE_F32)) return false;
+  if (t.n == 0) return true;
+  return t.p && t.g && t.m && t.v && aligned16(t.p) && aligned16(t.g) && aligned16(t.master) &&
+         aligned16(t.m) && aligned16(t.v);
+}
+
+// Launches kernel(args) over the tensors, kList a launch.  `each` fills in a tensor.
+template <typename F, typename K>
+moe_status for_lists(hipStream_t s, const char* name, int count, const moe_adamw_tensor* ts, AdamArgs a,
+                     F&& each, K kernel) {
+  // as many tiles a chunk as leave every CU sixteen workgroups, 4 at the most
+  int64_t all = 0;
+  for (int i = 0; i < count; ++i) all += (ts[i].n + kTile - 1) / kTile;
+  a.tiles = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(4, all / (16 * num_cus()))));
+  const int64_t chunk = static_cast<int64_t>(a.tiles) * kTile;
+  int at = 0;
+  while (at < count) {
+    a.count = 0;
+    int64_t chunks = 0;
+    for (; at < count && a.count < kList; ++at) {
+      if (ts[at].n == 0) continue;
+      const int64_t more = (ts[at].n + chunk - 1) / chunk;
+      if (chunks + more > 0x7FFFFFFF) break;   // the next launch's
+      AdamTensor& t = a.t[a.count++];
+      t = {};
+      t.n = ts[at].n;
+      t.m = ts[at].m;
+      t.v = ts[at].v;
+      t.m_exp = ts[at].m_exp;
+      t.v_exp = ts[at].v_exp;
+      t.first = static_cast<int>(chunks);
+      each(t, at);
+      chunks += more;
+    }
+    if (a.count == 0) break;
+    a.chunks = static_cast<int>(chunks);
+    MOE_TIMED(name, s);
+    kernel<<<a.chunks, kAdamThreads, 0, s>>>(a);
+    MOE_LAUNCH_CHECK();
+  }
+  return MOE_OK;
+}
+
+}  // namespace
+}  // namespace moe
+
+using namespace moe;
+
+extern "C" size_t moe_adamw_blocks(int64_t n) {
+  return n < 0 ? 0 : static_cast<size_t>((n + kBlock - 1) / kBlock);
+}
+
+extern "C" moe_status moe_adamw(void* stream, int count, const moe_adamw_tensor* tensors, double lr,
+                                double beta1, double beta2, double eps, int64_t step, uint32_t seed,
+                                const float* grad_scale, const moe_adamw_schedule* schedule) {
+  auto fine = [](double v) { return v >= 0 && v < INFINITY; };
+  if (count < 0 || (count > 0 && !tensors) || step < 1) return MOE_EINVAL;
+  if (!fine(lr) || !fine(beta1) || !fine(beta2) || beta1 >= 1 || beta2 >= 1 || !fine(eps) ||
+      !(static_cast<float>(eps) > 0.f))
+    return MOE_EINVAL;
+  if ((reinterpret_cast<uintptr_t>(schedule) | reinterpret_cast<uintptr_t>(grad_scale)) & 3) return MOE_EINVAL;
+  for (int i = 0; i < count; ++i)
+    if (!tensor_ok(tensors[i]) || tensors[i].n > int64_t(1) << 40) return MOE_EINVAL;
+  AdamArgs a{};
+  a.lr = static_cast<float>(lr);
+  a.c1 = static_cast<float>(1 / (1 - std::pow(beta1, static_cast<double>(step))));
+  a.c2 = static_cast<float>(1 / std::sqrt(1 - std::pow(beta2, static_cast<double>(step))));
+  a.eps = static_cast<float>(eps);
+  a.b1 = beta1;
+  a.b2 = beta2;
+  a.a1 = 1 - beta1;
+  a.a2 = 1 - beta2;
+  a.seed = seed;
+  a.grad_scale = grad_scale;
+  a.schedule = schedule;
+  return for_lists(static_cast<hipStream_t>(stream), "adamw", count, tensors, a,
+                   [&](AdamTensor& t, int i) {
+                     t.p = tensors[i].p;
+                     t.g = tensors[i].g;
+                     t.master = tensors[i].master;
+                     t.decay = static_cast<float>(tensors[i].weight_decay);
+                     t.key = static_cast<uint32_t>(i + 1) * 0x9E3779B9u;
+                     t.p16 = tensors[i].p_dtype == MOE_BF16;
+                     t.g16 = tensors[i].g_dtype == MOE_BF16;
+                   },
+                   adamw_kernel);
+}
+
+extern "C" moe_status moe_adamw_unpack(void* stream, int count, const moe_adamw_tensor* tensors,
+                                       float* const* m, float* const* v) {
+  if (count < 0 || (count > 0 && (!tensors || !m || !v))) return MOE_EINVAL;
+  for (int i = 0; i < count; ++i) {
+    const moe_adamw_tensor& t = tensors[i];
+    if (t.n < 0 || t.n > int64_t(1) << 40) return MOE_EINVAL;
+    if (t.n > 0 && (!t.m || !t.v || !t.m_exp || !t.v_exp || !m[i] || !v[i] || !aligned16(t.m) ||
+                    !aligned16(t.v) || !aligned16(m[i]) || !aligned16(v[i])))
+      return MOE_EINVAL;
+  }
+  return for_lists(static_cast<hipStream_t>(stream), "adamw_unpack", count, tensors, AdamArgs{},
+                   [&](AdamTensor& t, int i) {
+                     t.p = m[i];
+                     t.master = v[i];
+                   },
+                   adamw_unpack_kernel);
+}

@@ -38,3 +38,68 @@ def test_norm_rows_in_8_bits():
     q, scale = O.rms_norm_rows_i8(s, r, w)
     assert (np.abs(q * scale[:, None] - y) <= scale[:, None] * (0.5 + 1e-4)).all()
     assert (np.abs(q).max(axis=1) == 127).all()
+
+
+def test_adamw_is_torchs():
+    rng = np.random.default_rng(2)
+    p, g1, g2 = (rng.standard_normal(50) for _ in range(3))
+    t = torch.from_numpy(p.copy()).requires_grad_()
+    opt = torch.optim.AdamW([t], lr=0.01, betas=(0.9, 0.99), eps=1e-6, weight_decay=0.1)
+    m = v = np.zeros(50)
+    for step, g in enumerate((g1, g2), 1):
+        t.grad = torch.from_numpy(g.copy())
+        opt.step()
+        p, m, v = O.adamw(p, g, m, v, 0.01, 0.9, 0.99, 1e-6, step, 0.1)
+    np.testing.assert_allclose(p, t.detach().numpy(), rtol=1e-12)
+
+
+def test_adamw_codes_by_hand():
+    none = np.zeros(8, np.int64)
+    # 1 is the top octave (exponent 127): codes count from 2^-15 (1 + 2^-k)
+    c, e = O.adamw_encode([1.0, -1.0, 1.875, 1.124, 0.5, 2.0 ** -15 * 1.125, 2.0 ** -15, 0.0], none, 3)
+    assert e.tolist() == [127] and c.tolist() == [120, 248, 127, 120, 112, 1, 0, 0]
+    c, e = O.adamw_encode([1.0, 1.9375, 0.5, 2.0 ** -15, 1e-30, 0.0, 1.06, 0.75], none, 4)
+    assert e.tolist() == [127] and c.tolist() == [240, 255, 224, 1, 1, 0, 240, 232]
+    assert O.adamw_decode([1, 240, 0, 255], [127], 4).tolist() == [2.0 ** -15 * 1.0625, 1.0, 0.0, 1.9375]
+    # 65535 of 65536: everything that is not on a code goes up, the largest past its octave
+    c, e = O.adamw_encode([1.99, -1.01, 1.0, 0.0], np.full(4, 65535), 3)
+    assert e.tolist() == [128] and O.adamw_decode(c, e, 3).tolist() == [2.0, -1.125, 1.0, 0.0]
+    c, e = O.adamw_encode([np.nan, np.inf, 1e39, 1.0], none[:4], 3)
+    assert e.tolist() == [127] and c.tolist() == [128, 128, 128, 120]
+    c, e = O.adamw_encode([np.nan, np.inf, 1e39, 1.0], none[:4], 4)
+    assert e.tolist() == [127] and c.tolist() == [255, 255, 255, 240]
+
+
+@pytest.mark.parametrize("mant", [3, 4])
+def test_adamw_every_code_comes_back(mant):
+    for e in (16, 100, 254):
+        code = np.arange(256).astype(np.uint8)
+        if mant == 3:
+            code[128] = 0
+        # both blocks hold a value of the top octave
+        code[0], code[255] = 127 if mant == 3 else 250, 255
+        x = O.adamw_decode(code, [e, e], mant)
+        c, ee = O.adamw_encode(x, np.zeros(256, np.int64), mant)
+        assert ee.tolist() == [e, e] and (c == code).all()
+
+
+@pytest.mark.parametrize("mant", [3, 4])
+def test_adamw_rounding_is_right_on_average(mant):
+    """Every value's mean over 2000 seeds, within 5 standard deviations of a step's uniform error."""
+    rng = np.random.default_rng(4)
+    x = np.exp(rng.uniform(-6, 0, 256)) * (rng.choice([-1, 1], 256) if mant == 3 else 1)
+    tries = np.stack([O.adamw_decode(*O.adamw_encode(x, O.adamw_random(256, s, 3)[mant == 4], mant), mant)
+                      for s in range(2000)])
+    step = np.exp2(np.floor(np.log2(np.abs(x))) - mant)
+    assert (np.abs(tries - x) <= step * 2).all()
+    assert (np.abs(tries.mean(axis=0) - x) <= 5 * step / 2 / np.sqrt(2000)).all()
+
+
+def test_adamw_random_bits():
+    a, b = O.adamw_random(1 << 16, 7, 0)
+    for r in (a, b):
+        assert abs(r.mean() - 32767.5) < 5 * 65536 / np.sqrt(12 * 65536)
+    assert (O.adamw_random(1 << 16, 8, 0)[0] != a).mean() > 0.99 and (O.adamw_random(1 << 16, 7, 1)[0] != a).mean() > 0.99
+    np.testing.assert_array_equal(O.adamw_random(100, 7, 0, start=500)[1], b[500:600])
+    big = O.adamw_random(4, 7, 0, start=(1 << 32) - 2)
+    assert (big[0][2:] != a[:2]).any()

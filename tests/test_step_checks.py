@@ -95,3 +95,56 @@ def test_norm_workspace():
     assert q(0, 24) == q(1, 24) == q(4, 24) == 96 and q(5, 24) == 192 and q(1 << 40, 4096) == 512 * 4096 * 4
     assert q(3, 4096) == 3 * 4096 * 4
     assert q(-1, 24) == q(5, 20) == q(5, 32776) == 0
+
+
+def _list(n=200, bits=8, master=False, p=bf16, **kw):
+    t = dict(p=z(n, dt=p), g=z(n), m=z(n), v=z(n), weight_decay=0.1)
+    if bits == 8:
+        t.update(m=z(n, dt=u8), v=z(n, dt=u8), m_exp=z(2, dt=u8), v_exp=z(2, dt=u8))
+    if master:
+        t["master"] = z(n)
+    return dict(t, **kw)
+
+
+@pytest.mark.parametrize("match,kw", [
+    ("g holds", dict(g=z(199))), ("g holds", dict(g=z(201))), ("m holds", dict(m=z(199, dt=u8))),
+    ("v holds", dict(v=z(201, dt=u8))), ("m_exp holds", dict(m_exp=z(1, dt=u8))), ("v_exp holds", dict(v_exp=z(3, dt=u8))),
+    ("v_exp: both", dict(v_exp=None)), ("m: element type", dict(m=z(200))), ("v: element type", dict(v=z(200))),
+    ("m: element type", dict(m_exp=None, v_exp=None)), ("master: only", dict(p=z(200), master=z(200))),
+    ("master: element", dict(master=z(200, dt=bf16))), ("master holds", dict(master=z(100))),
+    ("unsupported", dict(p=z(200, dt=torch.float16))), ("unsupported", dict(g=z(200, dt=torch.float64)))], ids=str)
+def test_adamw_tensor_refuses(match, kw):
+    B.AdamWTensor(**_list())
+    refuses(match, B.AdamWTensor, **dict(_list(), **kw))
+
+
+def _adamw(lib, count=1, lr=0.1, b1=0.9, b2=0.99, eps=1e-8, step=1, scale=None, schedule=None, tensors=True, **kw):
+    a = ctypes.addressof(ctypes.create_string_buffer(16)) // 16 * 16 + 16
+    f = dict(p=a, g=a, master=None, m=a, v=a, m_exp=None, v_exp=None, n=0, weight_decay=0.0, p_dtype=1, g_dtype=0)
+    f.update(kw)
+    arr = (B.AdamWTensorArgs * 1)(B.AdamWTensorArgs(*f.values()))
+    return lib.moe_adamw(None, count, arr if tensors else None, lr, b1, b2, eps, step, 0, scale, schedule)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(count=-1), dict(tensors=False), dict(lr=-0.1), dict(lr=math.nan), dict(lr=math.inf), dict(b1=1.0), dict(b1=-0.1),
+    dict(b2=1.0), dict(b2=math.nan), dict(eps=0.0), dict(eps=1e-60), dict(eps=math.inf), dict(step=0), dict(n=-1),
+    dict(p_dtype=2), dict(g_dtype=-1), dict(weight_decay=-1.0), dict(weight_decay=math.nan), dict(m_exp=64), dict(v_exp=64),
+    dict(p_dtype=0, master=64), dict(n=5, p=None), dict(n=5, g=None), dict(n=5, m=None), dict(n=5, v=None),
+    dict(n=5, p=72), dict(n=5, g=66), dict(n=5, master=68), dict(n=5, m=65), dict(n=5, v=72), dict(n=(1 << 40) + 1),
+    dict(scale=66), dict(schedule=65)], ids=str)
+def test_adamw_refuses(kw):
+    assert _adamw(B.lib()) == 0 and _adamw(B.lib(), **kw) == EINVAL
+
+
+def test_adamw_of_nothing():
+    assert B.lib().moe_adamw(None, 0, None, 0.1, 0.9, 0.99, 1e-8, 1, 0, None, None) == 0
+    assert B.lib().moe_adamw_unpack(None, 0, None, None, None) == 0
+    assert [B.lib().moe_adamw_blocks(n) for n in (-1, 0, 1, 128, 129)] == [0, 0, 1, 1, 2] == \
+        [max(0, B.adamw_blocks(n)) for n in (-1, 0, 1, 128, 129)]
+
+
+def test_adamw_schedule():
+    t = B.adamw_schedule(0.5, 0.5, 0.75, 2, seed=0xFFFFFFFE)
+    assert t[:3].tolist() == [0.5, pytest.approx(4 / 3), pytest.approx((1 - 0.5625) ** -0.5)]
+    assert t.view(i32)[3] == -2 and B.adamw_schedule(0.5, 0.5, 0.75, 2, seed=5).view(i32)[3] == 5
