@@ -63,6 +63,7 @@ typedef enum { MOE_RELU = 0, MOE_GELU_TANH = 1, MOE_SWIGLU = 2 } moe_act;
 #define MOE_STATUS_BAD_ID 1 /* a cached expert id outside [0, E) */
 #define MOE_STATUS_DUP_ID 2 /* a token names the same expert twice */
 #define MOE_STATUS_REGION 4 /* an expert's capacity region does not fit */
+#define MOE_STATUS_BAD_TARGET 8 /* a target beyond the vocabulary */
 
 /* Human-readable name of a moe_status value. [host] */
 const char* moe_status_string(int status);
@@ -429,6 +430,43 @@ moe_status moe_spec_loss(void* stream, moe_dtype dt, int T, int d, int k,
                          const float* weights, const void* target,
                          int64_t rows_alloc, void* dy_disp, float* dweights,
                          float* loss, void* workspace, size_t workspace_bytes);
+
+/* Workspace bytes of moe_vocab_loss for these sizes; grad: with gradients, dW in
+ * dw_dt. [host] */
+size_t moe_vocab_loss_workspace_bytes(moe_dtype dt, int T, int d, int V,
+                                      int grad, moe_dtype dw_dt);
+
+/*
+ * moe_vocab_loss - softmax cross entropy of a projection onto a vocabulary of V
+ * words, and both of its gradients:
+ *   l = x w^T (float32),  lse_t = log sum_v exp l_tv,  loss_t = lse_t - l_t,target
+ *   of sum_t c_t loss_t, c_t = scale weights_t:
+ *   dl_tv = c_t (exp(l_tv - lse_t) - [v = target_t]) (bf16: rounded),
+ *   dx = dl w, dw = dl^T x, each rounded once
+ * The logits are never kept: without gradients none is written, with them the
+ * workspace holds those of one piece of rows (at most 2 GiB, 256 rows at least),
+ * as 16-bit (bf16) or float32 exponentials.
+ *   x        [T,d] layer dtype, rows ldx elements apart;  w [V,d] layer dtype
+ *   targets  [T] int32.  A negative one is ignored: its loss and lse are 0, its
+ *            row of dx is 0, and nothing of its row of x reaches dw.  One of V or
+ *            more is ignored likewise, and sets MOE_STATUS_BAD_TARGET
+ *   scale    finite (1 / T for a mean);  weights [T] float32 or NULL (ones)
+ *   loss     [T] float32 out;  lse [T] float32 out, or NULL
+ *   dx       [T,d] layer dtype out, rows lddx apart, and dw [V,d] out in dw_dt
+ *            (MOE_F32 or the layer dtype), both overwritten, or both NULL (scale,
+ *            weights, lddx and dw_dt are then not used).  dx may be x itself (with
+ *            the same row distance).  T = 0: dw is zeros
+ *   status   [1] int32 in/out
+ * d a multiple of 8, V any number; row distances at least d and multiples of 8.
+ * The query and the call are to see the same moe_set_gemm_tiles mode.
+ */
+moe_status moe_vocab_loss(void* stream, moe_dtype dt, int T, int d, int V,
+                          const void* x, int64_t ldx, const void* w,
+                          const int32_t* targets, float scale,
+                          const float* weights, float* loss, float* lse,
+                          void* dx, int64_t lddx, moe_dtype dw_dt, void* dw,
+                          int32_t* status, void* workspace,
+                          size_t workspace_bytes);
 
 /* ---- sample assignment caching (Section 4.2) ------------------------------ */
 

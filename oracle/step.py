@@ -10,7 +10,7 @@ import numpy as np
 from .blocks import quantize_rows
 from .moe_oracle import round_to
 
-__all__ = ["rms_norm_fwd", "rms_norm_bwd", "rms_norm_rows_i8", "adamw", "adamw_random", "adamw_encode",
+__all__ = ["rms_norm_fwd", "rms_norm_bwd", "rms_norm_rows_i8", "vocab_loss", "adamw", "adamw_random", "adamw_encode",
            "adamw_decode"]
 
 
@@ -40,6 +40,28 @@ def rms_norm_bwd(s, r, weight, dy, dsum=None):
     g = dy * weight
     dx = r[:, None] * (g - s * (r * r * (g * s).mean(axis=1))[:, None])
     return dx if dsum is None else dx + dsum, (dy * s * r[:, None]).sum(axis=0)
+
+
+# ---- loss of a vocabulary projection ---------------------------------------------
+def vocab_loss(x, w, targets, scale=1.0, weights=None):
+    """dict of loss, lse, p (probabilities), dl, dx, dw; rows of ignored tokens (targets outside the
+    vocabulary) are zeros in all but p."""
+    t = np.asarray(targets)
+    live = (t >= 0) & (t < len(w))
+    x = np.where(live[:, None], np.asarray(x, np.float64), 0.0)
+    l = x @ np.asarray(w, np.float64).T
+    top = l.max(axis=1)
+    z = np.exp(l - top[:, None])
+    logs = np.log(z.sum(axis=1))
+    p = z / z.sum(axis=1, keepdims=True)
+    at = np.where(live, t, 0)
+    rows = np.arange(len(t))
+    c = np.where(live, scale * (1.0 if weights is None else np.asarray(weights, np.float64)), 0.0)
+    loss = np.where(live, logs + (top - l[rows, at]), 0.0)
+    dl = p * c[:, None]
+    dl[rows, at] = c * np.expm1(-loss)
+    return dict(loss=loss, lse=np.where(live, top + logs, 0.0), p=p, c=c, dl=dl, dx=dl @ np.asarray(w, np.float64),
+                dw=dl.T @ x, x=x)
 
 
 # ---- AdamW -----------------------------------------------------------------------

@@ -18,7 +18,7 @@ LIB_PATH = os.path.join(HERE, "libmoe.so")
 MOE_F32, MOE_BF16 = 0, 1
 MOE_RELU, MOE_GELU_TANH, MOE_SWIGLU = 0, 1, 2
 ACTS = {"relu": MOE_RELU, "gelu_tanh": MOE_GELU_TANH, "swiglu": MOE_SWIGLU}
-STATUS_BAD_ID, STATUS_DUP_ID, STATUS_REGION = 1, 2, 4
+STATUS_BAD_ID, STATUS_DUP_ID, STATUS_REGION, STATUS_BAD_TARGET = 1, 2, 4, 8
 
 _c_int, _c_i64, _c_size, _p = ctypes.c_int, ctypes.c_int64, ctypes.c_size_t, ctypes.c_void_p
 
@@ -89,6 +89,9 @@ SIGNATURES = {
     "moe_spec_loss_workspace_bytes": (_c_size, [_c_int]),
     "moe_spec_loss": (_c_int, [_p, _c_int, _c_int, _c_int, _c_int, _p, _p, _p, _p, _c_i64, _p,
                                _p, _p, _p, _c_size]),
+    "moe_vocab_loss_workspace_bytes": (_c_size, [_c_int] * 6),
+    "moe_vocab_loss": (_c_int, [_stream_p, _c_int, _c_int, _c_int, _c_int, _p, _c_i64, _p, _p,
+                                ctypes.c_float, _p, _p, _p, _p, _c_i64, _c_int, _p, _p, _p, _c_size]),
     "moe_cache_update": (_c_int, [_p, _c_int, _c_int, _p, _p, _p, _p]),
     "moe_cached_weights": (_c_int, [_p, _c_int, _c_int, _c_int, _c_int, _p, _p, _p]),
     "moe_caching_decision": (_c_int, [_c_int, _c_i64, _c_i64, _c_int, _c_int, _c_int, _c_int,
@@ -791,6 +794,38 @@ def moe_spec_loss(y_disp, dest_row, weights, target, dy_disp, dweights, loss, ws
                                _ptr(weights), _ptr(target), y_disp.shape[0], _ptr(dy_disp),
                                _ptr(dweights), _ptr(loss), _ptr(ws), _nbytes(ws)),
            "moe_spec_loss")
+
+
+def moe_vocab_loss_workspace_bytes(dt, T, d, V, dw_dt=None) -> int:
+    """dw_dt: the type of dw, or None without gradients."""
+    return lib().moe_vocab_loss_workspace_bytes(dt, T, d, V, int(dw_dt is not None), dt if dw_dt is None else dw_dt)
+
+
+def moe_vocab_loss(x, w, targets, loss, lse, status, ws, scale=1.0, weights=None, dx=None, dw=None):
+    """Cross entropy of x w^T against targets [T] (negative: ignored) -> loss [T], lse [T] (or None);
+    with dx and dw (float32 or the layer's type) the gradients of sum_t scale weights_t loss_t.  x [T, d] and
+    dx may be rows of wider tensors; w [V, d]."""
+    (T, d), V, dtype = x.shape, w.shape[0], x.dtype
+    dt = _dt(x)
+    ldx, lddx = _rows(x, "x", T, d, dtype), _rows(dx, "dx", T, d, dtype, optional=True)
+    if tuple(w.shape) != (V, d):
+        raise MoEError(f"w has shape {tuple(w.shape)}, expected {(V, d)}")
+    _need(w, V * d, "w", dtype)
+    _need(targets, T, "targets", _I32)
+    _need(weights, T, "weights", _F32, optional=True)
+    _need(loss, T, "loss", _F32)
+    _need(lse, T, "lse", _F32, optional=True)
+    _need(status, 1, "status", _I32)
+    if (dx is None) != (dw is None):
+        raise MoEError("dx and dw: both or neither")
+    if dw is not None and dw.dtype not in (dtype, _F32):
+        raise MoEError(f"dw: a tensor of {dtype} or float32 is needed")
+    _need(dw, V * d, "dw", optional=True)
+    with _Here(_device_of(x, w, targets, loss, lse, status, ws, weights, dx, dw)) as stream:
+        _check(lib().moe_vocab_loss(stream, dt, T, d, V, _at(x), ldx, _ptr(w), _ptr(targets), scale,
+                                    _ptr(weights), _ptr(loss), _ptr(lse), _at(dx), lddx,
+                                    dt if dw is None else _dt(dw), _ptr(dw), _ptr(status), _ptr(ws),
+                                    _nbytes(ws)), "moe_vocab_loss")
 
 
 # ---- sample assignment caching ------------------------------------------------

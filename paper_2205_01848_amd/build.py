@@ -17,7 +17,7 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmoe.so")
-SOURCES = ["capi.hip", "gate.hip", "route.hip", "ffn.hip", "ffn_i8.hip", "gated.hip", "quant.hip", "norm.hip", "adamw.hip", "layer.hip",
+SOURCES = ["capi.hip", "gate.hip", "route.hip", "ffn.hip", "ffn_i8.hip", "gated.hip", "quant.hip", "norm.hip", "adamw.hip", "vocab.hip", "layer.hip",
            "losses.hip", "cache.hip", "policy.hip"]
 ARCH = "gfx950"
 

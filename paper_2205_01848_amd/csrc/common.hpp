@@ -93,6 +93,28 @@ __device__ __forceinline__ float wave_sum(float v) {
   return v;
 }
 
+// The same over a group of N = 8, 16 or 32 neighbouring lanes, in all of them: DPP steps
+// between lanes 1 apart, 2 apart, the halves of 8 and of 16.
+template <int CTRL> __device__ __forceinline__ float dpp_f(float v) {
+  const int x = __float_as_int(v);
+  return __int_as_float(__builtin_amdgcn_update_dpp(x, x, CTRL, 0xF, 0xF, false));
+}
+template <int N, typename F> __device__ __forceinline__ float group_reduce(float v, F&& f) {
+  static_assert(N == 8 || N == 16 || N == 32, "lanes");
+  v = f(v, dpp_f<0xB1>(v));
+  v = f(v, dpp_f<0x4E>(v));
+  v = f(v, dpp_f<0x141>(v));
+  if constexpr (N >= 16) v = f(v, dpp_f<0x140>(v));
+  if constexpr (N >= 32) v = f(v, __shfl_xor(v, 16, 64));
+  return v;
+}
+template <int N> __device__ __forceinline__ float group_max(float v) {
+  return group_reduce<N>(v, [](float a, float b) { return fmaxf(a, b); });
+}
+template <int N> __device__ __forceinline__ float group_sum(float v) {
+  return group_reduce<N>(v, [](float a, float b) { return a + b; });
+}
+
 // ---- fp32 x bf16 products on bf16 matrix cores --------------------------------
 // A float is the sum of three bf16 values (its top 8 significant bits, the
 // next 8, the last 8: each the truncation of what the ones before leave), so

@@ -11,11 +11,11 @@ namespace {
 // The product's sizes as plan_dense (plan.hpp) takes them.
 template <int MODE, int PASS>
 DensePlan dense_plan(moe_dtype dt, int M, int N, int K, int64_t lda, int64_t ldb) {
-  return plan_dense({dt == MOE_F32, is_gated(MODE), MODE == M_GATED_FWD || MODE == M_GATED_DA,
+  return plan_dense({dt == MOE_F32, is_gated(MODE), MODE == M_GATED_FWD || MODE == M_GATED_DA || MODE == M_VOCAB,
                      b_layout(PASS) == L_KM, is_dw(MODE), M, N, K, lda, ldb}, persistent_grid(), g_tile_mode);
 }
 
-// Sums the `splits` slots of an [M, N] product in order, adds the addend and
+// Sums the `splits` slots of an [M, N] product in order, adds the addend (and acc, fp32) and
 // writes rows [0, split_row) to c1 and the others to c2, ldc elements apart.
 struct JoinArgs {
   const float* partial;
@@ -24,6 +24,7 @@ struct JoinArgs {
   const char* add; int64_t ldadd;   // bytes
   char *c1, *c2; int64_t ldc;       // bytes
   int split_row;
+  const float* acc;
 };
 template <typename T>
 __global__ __launch_bounds__(256) void dense_join_kernel(const JoinArgs a) {
@@ -36,6 +37,10 @@ __global__ __launch_bounds__(256) void dense_join_kernel(const JoinArgs a) {
     float4 v = *reinterpret_cast<const float4*>(p);
     for (int s = 1; s < a.splits; ++s) {
       const float4 u = *reinterpret_cast<const float4*>(p + s * a.slot_elems);
+      v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
+    }
+    if (a.acc) {
+      const float4 u = *reinterpret_cast<const float4*>(a.acc + i * 4);
       v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
     }
     if (a.add) {
@@ -91,17 +96,33 @@ moe_status launch_dense(hipStream_t s, moe_dtype dt, const DensePlan& d, int T, 
   }
   if (d.splits == 1) return MOE_OK;
   const bool f32 = VARK ? p.out_f32 : dt == MOE_F32;
-  JoinArgs j{p.partial, p.slot_elems, d.splits, M, p.N, p.add, p.ldadd, p.C, p.C, p.ldc, M};
+  JoinArgs j{p.partial, p.slot_elems, d.splits, M, p.N, p.add, p.ldadd, p.C, p.C, p.ldc, M, nullptr};
   if (VARK) {
     j.c1 = reinterpret_cast<char*>(p.dwA);
     j.c2 = reinterpret_cast<char*>(p.dwB);
     j.ldc = static_cast<int64_t>(p.N) * (f32 ? 4 : 2);
     j.split_row = p.split_row;
+    if (MODE == M_VOCAB_DW) j.acc = p.acc;
   }
   const int jgrid = static_cast<int>(std::min<int64_t>(8 * num_cus(), (p.slot_elems / 4 + 255) / 256));
   MOE_TIMED("split_reduce", s);
   if (f32) dense_join_kernel<float><<<jgrid, 256, 0, s>>>(j);
   else dense_join_kernel<uint16_t><<<jgrid, 256, 0, s>>>(j);
+  MOE_LAUNCH_CHECK();
+  return MOE_OK;
+}
+
+// Zeros by a kernel, which a captured graph replays like any other.
+__global__ __launch_bounds__(256) void zero_kernel(uint4* p, int64_t n) {
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < n;
+       i += static_cast<int64_t>(gridDim.x) * 256)
+    p[i] = make_uint4(0, 0, 0, 0);
+}
+inline moe_status launch_zero(hipStream_t s, void* p, size_t bytes) {   // a multiple of 16
+  const int64_t n = static_cast<int64_t>(bytes / 16);
+  MOE_TIMED("zero_dw", s);
+  zero_kernel<<<static_cast<int>(std::min<int64_t>(8 * num_cus(), (n + 255) / 256)), 256, 0, s>>>(
+      static_cast<uint4*>(p), n);
   MOE_LAUNCH_CHECK();
   return MOE_OK;
 }

@@ -221,7 +221,16 @@ __global__ __launch_bounds__(64 * W) void ffn_few_rows_kernel(const GroupParams 
         }
         // element q: row 4 G + q of the block, column c16
         const int col = n0 + c16;
-        if (col < p.N) {
+        if constexpr (MODE == M_VOCAB) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const int lr = r0 + 16 * wave + 4 * G + q;
+            const float l = static_cast<float>(sum[0][q]);
+            if (lr < m && p.target[lr] == col) p.target_logit[lr] = l;
+            float v[1] = {col < p.N ? l : -INFINITY};
+            vocab_row<16>(p, v, lr, lr < m, n0 / kFewCols, col, c16 == 0);
+          }
+        } else if (col < p.N) {
           float s1 = 1.f, s3 = 1.f;
           if constexpr (I8) {
             s1 = p.b_scale[e * p.s_gstride + col];

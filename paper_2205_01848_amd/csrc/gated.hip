@@ -71,21 +71,6 @@ int gate_act(moe_act act) {
   return act == MOE_RELU ? ACT_RELU : act == MOE_GELU_TANH ? ACT_GELU : ACT_SWIGLU;
 }
 
-// Zeros by a kernel, which a captured graph replays like any other.
-__global__ __launch_bounds__(256) void zero_kernel(uint4* p, int64_t n) {
-  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < n;
-       i += static_cast<int64_t>(gridDim.x) * 256)
-    p[i] = make_uint4(0, 0, 0, 0);
-}
-moe_status launch_zero(hipStream_t s, void* p, size_t bytes) {   // a multiple of 16
-  const int64_t n = static_cast<int64_t>(bytes / 16);
-  MOE_TIMED("zero_dw", s);
-  zero_kernel<<<static_cast<int>(std::min<int64_t>(8 * num_cus(), (n + 255) / 256)), 256, 0, s>>>(
-      static_cast<uint4*>(p), n);
-  MOE_LAUNCH_CHECK();
-  return MOE_OK;
-}
-
 template <int MODE, int PASS>
 moe_status launch_few_dense(hipStream_t s, moe_dtype dt, int T, const GemmParams& p) {
   GroupParams fp{p, 0, nullptr, 0};

@@ -236,7 +236,11 @@ enum Mode {
   M_GATED_FWD = 9,         // H1, H3 -> A = act(H1) H3 [, H3 act'(H1) and act(H1) saved]
   M_GATED_DA = 10,         // dA = dY W2 -> dH1, dH3: dA times the saved factors
   M_ADD_STORE = 11,        // store with an addend (Y, dX), or partial sums
-  M_DENSE_DW = 12          // weight gradient in fp32 or bf16, or partial sums
+  M_DENSE_DW = 12,         // weight gradient in fp32 or bf16, or partial sums
+  // the loss of a vocabulary projection (vocab.hip)
+  M_VOCAB = 13,            // logits: each block of columns' maximum and sum of exponentials
+                           // [, the exponentials saved]
+  M_VOCAB_DW = 14          // M_DENSE_DW, added to the fp32 sums of earlier pieces
 };
 constexpr bool is_dense(int mode) { return mode >= M_GATED_FWD; }
 constexpr bool is_i8(int mode) { return mode >= M_I8_STORE && mode <= M_I8_FWD1_SWIGLU; }
@@ -244,7 +248,8 @@ constexpr bool is_i8(int mode) { return mode >= M_I8_STORE && mode <= M_I8_FWD1_
 constexpr bool is_gated(int mode) {
   return mode == M_FWD1_SWIGLU || mode == M_I8_FWD1_SWIGLU || mode == M_GATED_FWD;
 }
-constexpr bool is_dw(int mode) { return mode == M_DW || mode == M_DENSE_DW; }
+constexpr bool is_dense_dw(int mode) { return mode == M_DENSE_DW || mode == M_VOCAB_DW; }
+constexpr bool is_dw(int mode) { return mode == M_DW || is_dense_dw(mode); }
 // bytes per operand element of the 16x16 kernels
 constexpr int op_bytes(int mode) { return is_i8(mode) ? 1 : 2; }
 
@@ -300,7 +305,17 @@ struct GemmParams {
   RowScales a_scale; const float* b_scale; const float* b2_scale; int64_t s_gstride;
   int out_f32;
   Dense dense;
+  // M_VOCAB: per row n_stat blocks of columns {maximum, sum of exp(l - maximum)}, the
+  // tokens' targets and their logits; C: the exponentials, or NULL.
+  // M_VOCAB_DW: the earlier pieces' sums (NULL: none)
+  float2* stat; int n_stat;
+  const int32_t* target; float* target_logit;
+  const float* acc;
 };
+
+// The exponentials of M_VOCAB in 16 bits: fp16 of 2^15 exp(l - maximum), so that their 11
+// bits hold down to 2^-29.
+constexpr float kVocabScale = 32768.f;
 
 // Tile order, two levels above each XCD's kGroupM x 8 block of tiles.
 // Tiles come in bands of kBandM M-tiles; inside a band, in N-blocks of 8
@@ -359,14 +374,16 @@ __device__ __forceinline__ void decode_banded(int L, int n_mt, int n_nt, int& mt
 // K-contiguous like the forward's operands.
 enum Pass {
   P_FWD_H = 0, P_FWD_Y = 1, P_BWD_DA = 2, P_BWD_DX = 3, P_BWD_DW2 = 4, P_BWD_DW13 = 5,
-  P_BWD_DX_T = 6
+  P_BWD_DX_T = 6, P_VOCAB = 7, P_VOCAB_DX = 8, P_VOCAB_DW = 9
 };
 __host__ __device__ constexpr int a_layout(int pass) {
-  return pass == P_BWD_DW2 || pass == P_BWD_DW13 ? L_KM : L_KC;
+  return pass == P_BWD_DW2 || pass == P_BWD_DW13 || pass == P_VOCAB_DW ? L_KM : L_KC;
 }
 __host__ __device__ constexpr int b_layout(int pass) {
-  return pass == P_BWD_DA || pass == P_BWD_DX || pass == P_BWD_DW2 || pass == P_BWD_DW13 ? L_KM
-                                                                                          : L_KC;
+  return pass == P_BWD_DA || pass == P_BWD_DX || pass == P_BWD_DW2 || pass == P_BWD_DW13 ||
+                 pass == P_VOCAB_DX || pass == P_VOCAB_DW
+             ? L_KM
+             : L_KC;
 }
 
 // ---------------------------------------------------------------------------
@@ -894,6 +911,39 @@ __device__ __forceinline__ void stage16(float* strip, const floatx4 (&acc)[C::RB
     for (int q = 0; q < 4; ++q) strip[(4 * G + q) * C::kP + 16 * j + c16] = acc[i][j][q];
 }
 
+// M_VOCAB: N neighbouring lanes hold a block of columns of row `row`, lane by lane CN logits
+// v from column gc on (-inf behind the last column).  lead: the lane that writes the
+// block's maximum and sum.
+template <int N, int CN>
+__device__ __forceinline__ void vocab_row(const GemmParams& p, float (&v)[CN], int row, bool ok, int block,
+                                          int gc, bool lead) {
+  float m = v[0];
+#pragma unroll
+  for (int e = 1; e < CN; ++e) m = fmaxf(m, v[e]);
+  m = group_max<N>(m);
+  const float from = m == -INFINITY ? 0.f : m;   // (no column, or all of them -inf: zeros)
+  float s = 0.f;
+#pragma unroll
+  for (int e = 0; e < CN; ++e) {
+    v[e] = exp_fast(v[e] - from);
+    s += v[e];
+  }
+  s = group_sum<N>(s);
+  if (!ok) return;
+  if (lead) p.stat[static_cast<int64_t>(row) * p.n_stat + block] = make_float2(m, s);
+  if (gc >= p.N || !p.C) return;
+  char* c = p.C + row * p.ldc;
+  if constexpr (CN == 8) {
+    typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+    half8 h;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) h[e] = static_cast<_Float16>(v[e] * kVocabScale);
+    *reinterpret_cast<half8*>(c + static_cast<int64_t>(gc) * 2) = h;
+  } else {
+    reinterpret_cast<float*>(c)[gc] = v[0];
+  }
+}
+
 // Epilogue of one wave's block (RB x CB blocks of C): 16 accumulator rows at
 // a time go through the wave's LDS strip; a lane then finishes 8 consecutive
 // columns of a row and writes them as one vector (bf16) or two (fp32 weight
@@ -939,7 +989,7 @@ __device__ __forceinline__ void epilogue16(const GemmParams& p,
       for (int r = 0; r < WR; r += RG) {
         const int lm = wr0 + r + el / LR, gc = n0 + wn * WC + (el % LR) * 8;
         if (lm < m_valid && gc < p.N) {
-          if (MODE == M_DENSE_DW && slot < 0 && !p.out_f32) {
+          if (is_dense_dw(MODE) && slot < 0 && !p.out_f32) {
             *reinterpret_cast<uint4*>(dw_dst16(row0 + lm, gc)) = make_uint4(0, 0, 0, 0);
             continue;
           }
@@ -1071,6 +1121,33 @@ __device__ __forceinline__ void epilogue16(const GemmParams& p,
         }
       }
     }
+  } else if constexpr (MODE == M_VOCAB) {
+    // LR lanes hold a row's WC columns, 8 each: their maximum m and sum of exp(l - m)
+    // across the group, the exponentials stored where gradients follow
+    constexpr int LR = WC / 8, RG = 64 / LR;
+    const int block = 2 * (n0 / C::TN) + wn;
+    // the targets of the rows, 16 at a time, one a lane
+    int tg[C::RB];
+#pragma unroll
+    for (int i = 0; i < C::RB; ++i) {
+      const int lm = wr0 + 16 * i + el;
+      tg[i] = el < 16 && lm < m_valid ? p.target[row0 + lm] - (n0 + wn * WC) : -1;
+    }
+#pragma unroll
+    for (int i = 0; i < C::RB; ++i) {
+      stage16<C>(strip, acc, i, el);
+      if (tg[i] >= 0 && tg[i] < WC) p.target_logit[row0 + wr0 + 16 * i + el] = strip[el * kP + tg[i]];
+#pragma unroll
+      for (int it = 0; it < 16 / RG; ++it) {
+        const int r = RG * it + el / LR, c8 = (el % LR) * 8;
+        const int lm = wr0 + 16 * i + r, gc = n0 + wn * WC + c8;
+        const float* sp = strip + r * kP + c8;
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = gc + e < p.N ? sp[e] : -INFINITY;
+        vocab_row<LR>(p, v, row0 + lm, lm < m_valid, block, gc, el % LR == 0);
+      }
+    }
   } else {
     constexpr int LR = WC / 8, RG = 64 / LR;   // lanes per row, rows per pass
     // the addend's rows, kPf passes ahead of their use, as the factors above
@@ -1104,7 +1181,23 @@ __device__ __forceinline__ void epilogue16(const GemmParams& p,
         if (lm < m_valid && gc < p.N) {
           const float* sp = strip + r * kP + c8;
           if constexpr (is_dw(MODE)) {
-            if (MODE == M_DENSE_DW && slot < 0 && !p.out_f32) {
+            if constexpr (MODE == M_VOCAB_DW) {
+              if (p.acc && slot < 0) {
+                const float* q = p.acc + static_cast<int64_t>(row0 + lm) * p.N + gc;
+                const float4 lo = reinterpret_cast<const float4*>(q)[0], hi = reinterpret_cast<const float4*>(q)[1];
+                const float v[8] = {sp[0] + lo.x, sp[1] + lo.y, sp[2] + lo.z, sp[3] + lo.w,
+                                    sp[4] + hi.x, sp[5] + hi.y, sp[6] + hi.z, sp[7] + hi.w};
+                if (!p.out_f32) {
+                  *reinterpret_cast<uint4*>(dw_dst16(row0 + lm, gc)) = pack8(v);
+                } else {
+                  float* dst = dw_dst(row0 + lm, gc);
+                  *reinterpret_cast<float4*>(dst) = make_float4(v[0], v[1], v[2], v[3]);
+                  *reinterpret_cast<float4*>(dst + 4) = make_float4(v[4], v[5], v[6], v[7]);
+                }
+                continue;
+              }
+            }
+            if (is_dense_dw(MODE) && slot < 0 && !p.out_f32) {
               *reinterpret_cast<uint4*>(dw_dst16(row0 + lm, gc)) = pack8(sp);
               continue;
             }
@@ -1763,14 +1856,14 @@ __device__ __forceinline__ void mainloop_f32(const TileOps& op, char* const (&st
 
 // Epilogue of an fp32 tile, straight from the accumulators.
 template <int MODE, int RB, int NB>
-__device__ __forceinline__ void epilogue_f32(const GemmParams& p, const MidTile& t, const AccF32<NB>& c1,
+__device__ __forceinline__ void epilogue_f32(const GemmParams& p, const MidTile& t, AccF32<NB>& c1,
                                              const AccF32<NB>& c3, int lane, int wave) {
   constexpr bool GATED = is_gated(MODE), VARK = is_dw(MODE);
-  const floatx16(&acc)[NB] = c1.v;
+  std::conditional_t<MODE == M_VOCAB_DW, floatx16, const floatx16>(&acc)[NB] = c1.v;
   const floatx16(&acc3)[NB] = c3.v;
   // accumulator q of lane l: column l % 32, row 8 (q / 4) + 4 (l / 32) + q % 4
   const int col = t.n0 + (GATED ? wave & 1 : wave) * 32 + (lane & 31);
-  if (col >= p.N) return;
+  if (MODE != M_VOCAB && col >= p.N) return;
 #pragma unroll
   for (int i = 0; i < NB; ++i) {
     const int blk = GATED ? 2 * i + (wave >> 1) : i;
@@ -1791,12 +1884,29 @@ __device__ __forceinline__ void epilogue_f32(const GemmParams& p, const MidTile&
         }
       }
     }
+    if constexpr (MODE == M_VOCAB) {
+      int tg[16];
+#pragma unroll
+      for (int q = 0; q < 16; ++q) tg[q] = p.target[t.row0 + min(row_of(q), t.m_valid - 1)];
+#pragma unroll
+      for (int q = 0; q < 16; ++q) {
+        const int row = t.row0 + row_of(q);
+        const bool ok = row_of(q) < t.m_valid;
+        if (ok && tg[q] == col) p.target_logit[row] = acc[i][q];
+        float v[1] = {col < p.N ? acc[i][q] : -INFINITY};
+        vocab_row<32>(p, v, row, ok, 4 * (t.n0 / kMidN) + wave, col, (lane & 31) == 0);
+      }
+      continue;
+    }
 #pragma unroll
     for (int q = 0; q < 16; ++q) {
       const int lm = row_of(q);
       if (lm >= t.m_valid) continue;
       const int64_t row = t.row0 + lm;
       if constexpr (VARK) {
+        if constexpr (MODE == M_VOCAB_DW) {
+          if (t.slot < 0 && p.acc) acc[i][q] += p.acc[row * p.N + col];
+        }
         float* dst;
         if (t.slot >= 0) dst = p.partial + static_cast<int64_t>(t.slot) * p.slot_elems + row * p.N;
         else if (row < p.split_row) dst = p.dwA + static_cast<int64_t>(t.g) * p.dw_gstride + row * p.N;
@@ -2148,7 +2258,8 @@ bool use_wt13(const FfnPlan& pl, moe_dtype dt) {
 
 const char* pass_name(int pass) {
   static const char* names[] = {"gemm_fwd_h", "gemm_fwd_y", "gemm_bwd_da", "gemm_bwd_dx",
-                                "gemm_bwd_dw2", "gemm_bwd_dw13", "gemm_bwd_dx"};
+                                "gemm_bwd_dw2", "gemm_bwd_dw13", "gemm_bwd_dx",
+                                "gemm_logits", "gemm_vocab_dx", "gemm_vocab_dw"};
   return names[pass];
 }
 

@@ -103,3 +103,25 @@ def test_adamw_random_bits():
     np.testing.assert_array_equal(O.adamw_random(100, 7, 0, start=500)[1], b[500:600])
     big = O.adamw_random(4, 7, 0, start=(1 << 32) - 2)
     assert (big[0][2:] != a[:2]).any()
+
+
+def test_vocab_loss_is_torchs():
+    rng = np.random.default_rng(6)
+    x, w = rng.standard_normal((7, 12)), rng.standard_normal((31, 12))
+    t, c = np.array([0, 30, -1, 5, 5, -100, 31]), rng.uniform(0.5, 2, 7)
+    o = O.vocab_loss(x, w, t, 0.25, c)
+    tx, tw = (torch.from_numpy(a).requires_grad_() for a in (x, w))
+    tt = torch.from_numpy(np.where(t == 31, -1, t)).clamp(min=-1)
+    loss = torch.nn.functional.cross_entropy(tx @ tw.T, tt, ignore_index=-1, reduction="none")
+    np.testing.assert_allclose(o["loss"], loss.detach().numpy(), rtol=1e-12, atol=1e-14)
+    gx, gw = torch.autograd.grad((loss * torch.from_numpy(c) * 0.25).sum(), (tx, tw))
+    np.testing.assert_allclose(o["dx"], gx.numpy(), rtol=1e-10, atol=1e-13)
+    np.testing.assert_allclose(o["dw"], gw.numpy(), rtol=1e-10, atol=1e-13)
+    assert (o["lse"][[2, 5, 6]] == 0).all()
+    np.testing.assert_allclose(o["lse"][:2], torch.logsumexp(tx @ tw.T, 1).detach().numpy()[:2], rtol=1e-12)
+
+
+def test_vocab_loss_by_hand():
+    o = O.vocab_loss([[0.0, 0.0], [100.0, 0.0]], [[1.0, 0], [0, 1], [0, 0], [0, -1]], [1, 0])
+    assert abs(o["loss"][0] - np.log(4)) < 1e-15 and np.allclose(o["dl"][0], [0.25, -0.75, 0.25, 0.25])
+    assert 0 <= o["loss"][1] < 1e-40 and o["lse"][1] == 100

@@ -32,7 +32,9 @@ NORM = dict(x=z(5, 24), weight=z(24), eps=1e-5, y=z(5, 24), add=z(5, 24), sum=z(
             q=z(5, 32, dt=i8), scale=z(5))
 NORM_BWD = dict(s=z(5, 24), weight=z(24), rstd=z(5), dy=z(5, 24), dx=z(5, 24), dw=z(24), ws=z(4096, dt=u8),
                 dsum=z(5, 24))
-CALLS = [(B.moe_rms_norm_fwd, NORM, "x"), (B.moe_rms_norm_bwd, NORM_BWD, "s")]
+LOSS = dict(x=z(5, 24), w=z(7, 24), targets=z(5, dt=i32), loss=z(5), lse=z(5), status=z(1, dt=i32),
+            ws=z(1 << 16, dt=u8), weights=z(5), dx=z(5, 24), dw=z(7, 24))
+CALLS = [(B.moe_rms_norm_fwd, NORM, "x"), (B.moe_rms_norm_bwd, NORM_BWD, "s"), (B.moe_vocab_loss, LOSS, "x")]
 OPERANDS = [(fn, kw, n) for fn, kw, first in CALLS for n, t in kw.items()
             if torch.is_tensor(t) and n not in ("ws", first)]
 
@@ -45,11 +47,12 @@ def test_sizes_that_fit_reach_the_device_check(fn, kw):
 @pytest.mark.parametrize("fn,kw,name", OPERANDS)
 def test_every_operand_too_small_or_of_another_type(fn, kw, name):
     t = kw[name]
-    refuses(name, fn, **dict(kw, **{name: t[:-1].contiguous()}))
+    if fn is not B.moe_vocab_loss or name != "w":     # (fewer words are another vocabulary)
+        refuses(name, fn, **dict(kw, **{name: t[:-1].contiguous()}))
     refuses(name, fn, **dict(kw, **{name: t.to(torch.float64)}))
 
 
-@pytest.mark.parametrize("fn,kw,name", [o for o in OPERANDS if o[1][o[2]].dim() == 2 and o[2] != "q"])
+@pytest.mark.parametrize("fn,kw,name", [o for o in OPERANDS if o[1][o[2]].dim() == 2 and o[2] != "q" and o[1] is not LOSS or o[2] == "dx"])
 def test_rows_with_gaps(fn, kw, name):
     passes_checks(fn, **dict(kw, **{name: z(5, 32)[:, :24]}))
     refuses(name, fn, **dict(kw, **{name: z(5, 28)[:, :24]}))          # 28 elements apart
@@ -148,3 +151,41 @@ def test_adamw_schedule():
     t = B.adamw_schedule(0.5, 0.5, 0.75, 2, seed=0xFFFFFFFE)
     assert t[:3].tolist() == [0.5, pytest.approx(4 / 3), pytest.approx((1 - 0.5625) ** -0.5)]
     assert t.view(i32)[3] == -2 and B.adamw_schedule(0.5, 0.5, 0.75, 2, seed=5).view(i32)[3] == 5
+
+
+def test_loss_takes_both_gradients_or_none():
+    passes_checks(B.moe_vocab_loss, **dict(LOSS, dx=None, dw=None))
+    refuses("both or neither", B.moe_vocab_loss, **dict(LOSS, dx=None))
+    refuses("both or neither", B.moe_vocab_loss, **dict(LOSS, dw=None))
+    refuses("w has shape", B.moe_vocab_loss, **dict(LOSS, w=z(7, 32)))
+    passes_checks(B.moe_vocab_loss, **dict(LOSS, w=z(9, 24), dw=z(9, 24)))
+
+
+def _loss(lib, dt=1, T=5, d=24, V=7, x=P, ldx=24, w=P, targets=P, scale=1.0, weights=None, loss=P, lse=None, dx=P,
+          lddx=24, dw_dt=1, dw=P, status=P, ws=P, nws=1 << 30):
+    return lib.moe_vocab_loss(None, dt, T, d, V, x, ldx, w, targets, scale, weights, loss, lse, dx, lddx, dw_dt, dw,
+                              status, ws, nws)
+
+
+@pytest.mark.parametrize("kw,st", [
+    (dict(dt=2), EINVAL), (dict(T=-1), EINVAL), (dict(d=20), EINVAL), (dict(d=0), EINVAL), (dict(V=0), EINVAL),
+    (dict(V=1 << 23), EINVAL), (dict(d=1 << 23, ldx=1 << 23, lddx=1 << 23), EINVAL), (dict(x=None), EINVAL),
+    (dict(w=None), EINVAL), (dict(targets=None), EINVAL), (dict(loss=None), EINVAL), (dict(status=None), EINVAL),
+    (dict(dx=None), EINVAL), (dict(dw=None), EINVAL), (dict(ldx=16), EINVAL), (dict(ldx=28), EINVAL), (dict(lddx=23), EINVAL),
+    (dict(scale=math.nan), EINVAL), (dict(scale=math.inf), EINVAL), (dict(dw_dt=2), EINVAL), (dict(dt=0, dw_dt=1), EINVAL),
+    (dict(x=ctypes.c_void_p(4100)), EINVAL), (dict(w=ctypes.c_void_p(4104)), EINVAL), (dict(dx=ctypes.c_void_p(4104)), EINVAL),
+    (dict(ws=None), EWORKSPACE), (dict(nws=64), EWORKSPACE), (dict(ws=ctypes.c_void_p(4104)), EWORKSPACE)], ids=str)
+def test_loss_refuses(kw, st):
+    assert _loss(B.lib(), **kw) == st
+
+
+def test_loss_workspace_is_bounded():
+    """Whatever T: one piece's exponentials (2 GiB), its copy of x, maxima and sums, partial sums."""
+    q = B.moe_vocab_loss_workspace_bytes
+    for dt in (0, 1):
+        assert q(dt, 0, 64, 1000, dt) == q(dt, 0, 64, 1000) == 256
+        assert q(dt, 1 << 20, 64, 131072, dt) <= (1 << 31) * 1.3
+        assert q(dt, 1 << 20, 64, 131072) <= (1 << 28) * 1.1
+    assert q(1, 1 << 20, 64, 131072, 1) - q(1, 1 << 20, 64, 131072, 0) == 131072 * 64 * 4   # fp32 sums of a bf16 dW
+    assert q(1, 8192, 64, 131072, 1) == q(1, 8192, 64, 131072, 0)                           # one piece needs none
+    assert q(2, 8, 64, 100) == q(1, -1, 64, 100) == q(1, 8, 60, 100) == q(1, 8, 64, 0) == q(0, 8, 64, 100, 1) == 0
