@@ -440,9 +440,9 @@ size_t moe_vocab_loss_workspace_bytes(moe_dtype dt, int T, int d, int V,
  * moe_vocab_loss - softmax cross entropy of a projection onto a vocabulary of V
  * words, and both of its gradients:
  *   l = x w^T (float32),  lse_t = log sum_v exp l_tv,  loss_t = lse_t - l_t,target
- *   of sum_t c_t loss_t, c_t = scale weights_t:
- *   dl_tv = c_t (exp(l_tv - lse_t) - [v = target_t]) (bf16: rounded),
- *   dx = dl w, dw = dl^T x, each rounded once
+ *   of scale sum_t weights_t loss_t:
+ *   dl_tv = weights_t (exp(l_tv - lse_t) - [v = target_t]) (bf16: rounded),
+ *   dx = scale dl w, dw = scale dl^T x, each rounded once
  * The logits are never kept: without gradients none is written, with them the
  * workspace holds those of one piece of rows (at most 2 GiB, 256 rows at least),
  * as 16-bit (bf16) or float32 exponentials.

@@ -79,9 +79,10 @@ __device__ __forceinline__ int find_tensor(const AdamArgs& a, int chunk) {
   return lo;
 }
 
-// 8 values from p + i on, `left` of them there (8 or more: all).
+// 8 values from p + i on, `left` of them there (FULL: all).
+template <bool FULL>
 __device__ __forceinline__ void load8(const void* p, bool b16, int64_t i, int64_t left, float (&f)[8]) {
-  if (left >= 8) {
+  if (FULL || left >= 8) {
     if (b16) {
       unpack8(*reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + i), f);
     } else {
@@ -96,8 +97,9 @@ __device__ __forceinline__ void load8(const void* p, bool b16, int64_t i, int64_
   for (int e = 0; e < 8; ++e)
     f[e] = e >= left ? 0.f : b16 ? bf2f(static_cast<const uint16_t*>(p)[i + e]) : static_cast<const float*>(p)[i + e];
 }
+template <bool FULL>
 __device__ __forceinline__ void store8(void* p, bool b16, int64_t i, int64_t left, const float (&f)[8]) {
-  if (left >= 8) {
+  if (FULL || left >= 8) {
     if (b16) {
       *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p) + i) = pack8(f);
     } else {
@@ -114,18 +116,19 @@ __device__ __forceinline__ void store8(void* p, bool b16, int64_t i, int64_t lef
       else static_cast<float*>(p)[i + e] = f[e];
     }
 }
-__device__ __forceinline__ uint2 load_codes(const void* p, int64_t i, int64_t left) {
+template <bool FULL> __device__ __forceinline__ uint2 load_codes(const void* p, int64_t i, int64_t left) {
   const uint8_t* q = static_cast<const uint8_t*>(p) + i;
-  if (left >= 8) return *reinterpret_cast<const uint2*>(q);
+  if (FULL || left >= 8) return *reinterpret_cast<const uint2*>(q);
   uint32_t w[2] = {0, 0};
 #pragma unroll
   for (int e = 0; e < 8; ++e)
     if (e < left) w[e / 4] |= static_cast<uint32_t>(q[e]) << (e % 4 * 8);
   return make_uint2(w[0], w[1]);
 }
+template <bool FULL>
 __device__ __forceinline__ void store_codes(void* p, int64_t i, int64_t left, const uint32_t (&c)[8]) {
   uint8_t* q = static_cast<uint8_t*>(p) + i;
-  if (left >= 8) {
+  if (FULL || left >= 8) {
     *reinterpret_cast<uint2*>(q) = make_uint2(c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24,
                                               c[4] | c[5] << 8 | c[6] << 16 | c[7] << 24);
     return;
@@ -134,8 +137,9 @@ __device__ __forceinline__ void store_codes(void* p, int64_t i, int64_t left, co
   for (int e = 0; e < 8; ++e)
     if (e < left) q[e] = static_cast<uint8_t>(c[e]);
 }
+__device__ __forceinline__ uint32_t code_of(const uint2& c, int e) { return (e < 4 ? c.x : c.y) >> (e % 4 * 8) & 255; }
 
-// What code c of a block with exponent e stands for.
+// What code c of a block with exponent e stands for, base = 8 (e - 15) for m, 16 (e - 15) for v.
 __device__ __forceinline__ float decode_m(uint32_t c, int base) {
   const uint32_t size = c & 127;
   const float x = __uint_as_float(((size + base) << 20) | (c & 128) << 24);
@@ -175,12 +179,114 @@ struct AdamStep {
   uint32_t seed;
 };
 
+// sqrt(v) by the hardware's root, within one unit in the last place (of a v that is tiny as
+// of one 2^64 times its size: the hardware takes subnormal numbers for zero).
+__device__ __forceinline__ float root(float v) {
+  const bool tiny = v < 0x1p-96f;
+  const float s = __builtin_amdgcn_sqrtf(tiny ? v * 0x1p64f : v);
+  return tiny ? s * 0x1p-32f : s;
+}
+
 __device__ __forceinline__ void update(float (&p)[8], const float (&m)[8], const float (&v)[8],
                                        const AdamStep& st, float keep, float eps) {
   const float rate = st.lr * st.c1;
 #pragma unroll
-  for (int e = 0; e < 8; ++e)
-    p[e] = p[e] * keep - rate * m[e] / (__builtin_sqrtf(v[e]) * st.c2 + eps);
+  for (int e = 0; e < 8; ++e) {
+    const float den = __builtin_fmaf(root(v[e]), st.c2, eps);
+    p[e] = __builtin_fmaf(p[e], keep, -(rate * m[e]) * __builtin_amdgcn_rcpf(den));
+  }
+}
+
+// A thread's 8 values with states in 8 bits: the moments in m and v, their codes and
+// exponents written.  All lanes of the wavefront take part (left <= 0: with nothing).
+constexpr int kBeyondM = 255 << 3, kBeyondV = 255 << 4;   // left of the border: not a finite float32
+template <bool FULL>
+__device__ __forceinline__ void step_codes(const AdamArgs& a, const AdamTensor& t, const AdamStep& st, int64_t i,
+                                           int64_t left, const float (&g)[8], float (&m)[8], float (&v)[8]) {
+  const uint2 mc = load_codes<FULL>(t.m, i, left), vc = load_codes<FULL>(t.v, i, left);
+  const int64_t blk = i / kBlock;
+  const bool here = FULL || left > 0;
+  const int mb = here ? (t.m_exp[blk] - 15) * 8 : 0, vb = here ? (t.v_exp[blk] - 15) * 16 : 0;
+  const uint32_t x0 = static_cast<uint32_t>(i) * 0xBB67AE85u + static_cast<uint32_t>(i >> 32) * 0x6A09E667u +
+                      (st.seed ^ t.key);
+  uint32_t mh[8], vh[8];
+  int mt[8], vt[8], mmost = 16 << 3, vmost = 16 << 4;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const double gd = static_cast<double>(g[e]) * st.scale;
+    const double md = mix(a.b1, decode_m(code_of(mc, e), mb), a.a1, gd);
+    const double vd = mix(a.b2, decode_v(code_of(vc, e), vb), a.a2, gd * gd);
+    m[e] = static_cast<float>(md);
+    v[e] = static_cast<float>(vd);
+    const uint32_t rnd = random_bits(x0 + e * 0xBB67AE85u);
+    mh[e] = static_cast<uint32_t>(__double2hiint(md));
+    vh[e] = static_cast<uint32_t>(__double2hiint(vd));
+    mt[e] = static_cast<int>(((mh[e] & 0x7FFFFFFFu) + ((rnd & 0xFFFF) << 1)) >> 17) - ((1023 - 127) << 3);
+    vt[e] = static_cast<int>(((vh[e] & 0x7FFFFFFFu) + (rnd >> 16)) >> 16) - ((1023 - 127) << 4);
+    mmost = max(mmost, mt[e]);
+    vmost = max(vmost, vt[e]);
+  }
+  // (values that are not finite as float32 do not count; they are rare enough to branch on)
+  const bool odd = __any(mmost >= kBeyondM || vmost >= kBeyondV);
+  if (odd) {
+    mmost = 16 << 3;
+    vmost = 16 << 4;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      mmost = max(mmost, mt[e] < kBeyondM ? mt[e] : 0);
+      vmost = max(vmost, vt[e] < kBeyondV ? vt[e] : 0);
+    }
+  }
+  const int mtop = row16_max(mmost) >> 3, vtop = row16_max(vmost) >> 4;
+  uint32_t mq[8], vq[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const int c = mt[e] - (mtop - 15) * 8;
+    mq[e] = c > 0 ? c | (mh[e] >> 24 & 128) : 0;
+    vq[e] = max(vt[e] - (vtop - 15) * 16, static_cast<int>(min(vh[e], 1u)));   // a v above 0 stays so
+  }
+  if (odd) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      if (mt[e] >= kBeyondM) mq[e] = 128;
+      if (vt[e] >= kBeyondV) vq[e] = 255;
+    }
+  }
+  store_codes<FULL>(t.m, i, left, mq);
+  store_codes<FULL>(t.v, i, left, vq);
+  if (here && threadIdx.x % (kBlock / 8) == 0) {
+    t.m_exp[blk] = static_cast<uint8_t>(mtop);
+    t.v_exp[blk] = static_cast<uint8_t>(vtop);
+  }
+}
+
+template <bool FULL>
+__device__ __forceinline__ void step_tile(const AdamArgs& a, const AdamTensor& t, const AdamStep& st, int64_t i,
+                                          float keep) {
+  const int64_t left = t.n - i;
+  float g[8], p[8], m[8], v[8];
+  load8<FULL>(t.g, t.g16, i, left, g);
+  if (t.master) load8<FULL>(t.master, false, i, left, p);
+  else load8<FULL>(t.p, t.p16, i, left, p);
+  if (t.m_exp) {
+    step_codes<FULL>(a, t, st, i, left, g, m, v);
+  } else {
+    load8<FULL>(t.m, false, i, left, m);
+    load8<FULL>(t.v, false, i, left, v);
+    const float b1 = static_cast<float>(a.b1), b2 = static_cast<float>(a.b2);
+    const float a1 = static_cast<float>(a.a1), a2 = static_cast<float>(a.a2);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      g[e] *= st.scale;
+      m[e] = b1 * m[e] + a1 * g[e];
+      v[e] = b2 * v[e] + a2 * (g[e] * g[e]);
+    }
+    store8<FULL>(t.m, false, i, left, m);
+    store8<FULL>(t.v, false, i, left, v);
+  }
+  update(p, m, v, st, keep, a.eps);
+  if (t.master) store8<FULL>(t.master, false, i, left, p);
+  store8<FULL>(t.p, t.p16, i, left, p);
 }
 
 __global__ __launch_bounds__(kAdamThreads) void adamw_kernel(const AdamArgs a) {
@@ -193,94 +299,43 @@ __global__ __launch_bounds__(kAdamThreads) void adamw_kernel(const AdamArgs a) {
   }
   const int ti = find_tensor(a, blockIdx.x);
   const AdamTensor& t = a.t[ti];
-  const int64_t i0 = static_cast<int64_t>(static_cast<int>(blockIdx.x) - t.first) * a.tiles * kTile;
+  int64_t i0 = static_cast<int64_t>(static_cast<int>(blockIdx.x) - t.first) * a.tiles * kTile;
   const float keep = 1.f - st.lr * t.decay;
-  for (int k = 0; k < a.tiles; ++k) {
-    const int64_t i = i0 + k * kTile + threadIdx.x * 8, left = t.n - i;
-    if (i0 + k * kTile >= t.n) break;
-    float g[8], p[8], m[8], v[8];
-    load8(t.g, t.g16, i, left, g);
-    if (t.master) load8(t.master, false, i, left, p);
-    else load8(t.p, t.p16, i, left, p);
-    if (!t.m_exp) {
-      load8(t.m, false, i, left, m);
-      load8(t.v, false, i, left, v);
-      const float b1 = static_cast<float>(a.b1), b2 = static_cast<float>(a.b2);
-      const float a1 = static_cast<float>(a.a1), a2 = static_cast<float>(a.a2);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        g[e] *= st.scale;
-        m[e] = b1 * m[e] + a1 * g[e];
-        v[e] = b2 * v[e] + a2 * (g[e] * g[e]);
-      }
-      store8(t.m, false, i, left, m);
-      store8(t.v, false, i, left, v);
-    } else {
-      const uint2 mc = load_codes(t.m, i, left), vc = load_codes(t.v, i, left);
-      const int64_t blk = i / kBlock;
-      const bool here = left > 0;
-      const int me = here ? t.m_exp[blk] : 15, ve = here ? t.v_exp[blk] : 15;
-      const uint32_t x0 = static_cast<uint32_t>(i) * 0xBB67AE85u + static_cast<uint32_t>(i >> 32) * 0x6A09E667u +
-                          (st.seed ^ t.key);
-      uint32_t mq[8], vq[8];
-      int mt[8], vt[8], mtop = 16, vtop = 16;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const uint32_t cm = (e < 4 ? mc.x : mc.y) >> (e % 4 * 8) & 255, cv = (e < 4 ? vc.x : vc.y) >> (e % 4 * 8) & 255;
-        const double gd = static_cast<double>(g[e]) * st.scale;
-        const double md = mix(a.b1, decode_m(cm, (me - 15) * 8), a.a1, gd);
-        const double vd = mix(a.b2, decode_v(cv, (ve - 15) * 16), a.a2, gd * gd);
-        m[e] = static_cast<float>(md);
-        v[e] = static_cast<float>(vd);
-        const uint32_t rnd = random_bits(x0 + e * 0xBB67AE85u);
-        const uint32_t mh = static_cast<uint32_t>(__double2hiint(md)), vh = static_cast<uint32_t>(__double2hiint(vd));
-        mt[e] = static_cast<int>(((mh & 0x7FFFFFFFu) + ((rnd & 0xFFFF) << 1)) >> 17) - ((1023 - 127) << 3);
-        vt[e] = static_cast<int>(((vh & 0x7FFFFFFFu) + (rnd >> 16)) >> 16) - ((1023 - 127) << 4);
-        mq[e] = mh >> 31 << 7;
-        vq[e] = vd > 0 ? 1 : 0;
-        // (beyond the 32-bit numbers, and NaN: not counted)
-        if (mt[e] < 255 << 3) mtop = max(mtop, mt[e] >> 3);
-        if (vt[e] < 255 << 4) vtop = max(vtop, vt[e] >> 4);
-      }
-      mtop = row16_max(mtop);
-      vtop = row16_max(vtop);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int c = mt[e] - (mtop - 15) * 8, d = vt[e] - (vtop - 15) * 16;
-        mq[e] = mt[e] >= 255 << 3 ? 128 : c > 0 ? mq[e] | c : 0;
-        vq[e] = vt[e] >= 255 << 4 ? 255 : max(d, static_cast<int>(vq[e]));
-      }
-      store_codes(t.m, i, left, mq);
-      store_codes(t.v, i, left, vq);
-      if (here && threadIdx.x % (kBlock / 8) == 0) {
-        t.m_exp[blk] = static_cast<uint8_t>(mtop);
-        t.v_exp[blk] = static_cast<uint8_t>(vtop);
-      }
-    }
-    update(p, m, v, st, keep, a.eps);
-    if (t.master) store8(t.master, false, i, left, p);
-    store8(t.p, t.p16, i, left, p);
+  for (int k = 0; k < a.tiles && i0 < t.n; ++k, i0 += kTile) {
+    if (i0 + kTile <= t.n) step_tile<true>(a, t, st, i0 + threadIdx.x * 8, keep);
+    else step_tile<false>(a, t, st, i0 + threadIdx.x * 8, keep);
   }
 }
 
-// The values of 8-bit states: t.m, t.v to the 32-bit t.p and t.master.
+// The values of 8-bit states: t.m, t.v to the 32-bit t.p and t.master.  Four values a
+// thread and store, so that every store of a wavefront covers whole lines.
 __global__ __launch_bounds__(kAdamThreads) void adamw_unpack_kernel(const AdamArgs a) {
   const int ti = find_tensor(a, blockIdx.x);
   const AdamTensor& t = a.t[ti];
   const int64_t i0 = static_cast<int64_t>(static_cast<int>(blockIdx.x) - t.first) * a.tiles * kTile;
-  for (int k = 0; k < a.tiles; ++k) {
-    const int64_t i = i0 + k * kTile + threadIdx.x * 8, left = t.n - i;
+  for (int k = 0; k < 2 * a.tiles; ++k) {
+    const int64_t i = i0 + k * (kTile / 2) + threadIdx.x * 4, left = t.n - i;
     if (left <= 0) break;
-    const uint2 mc = load_codes(t.m, i, left), vc = load_codes(t.v, i, left);
     const int mb = (t.m_exp[i / kBlock] - 15) * 8, vb = (t.v_exp[i / kBlock] - 15) * 16;
-    float m[8], v[8];
+    const uint8_t *mc = static_cast<const uint8_t*>(t.m) + i, *vc = static_cast<const uint8_t*>(t.v) + i;
+    float* m = static_cast<float*>(t.p) + i;
+    float* v = t.master + i;
+    if (left >= 4) {
+      const uint32_t x = *reinterpret_cast<const uint32_t*>(mc), y = *reinterpret_cast<const uint32_t*>(vc);
+      floatx4 p, q;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      m[e] = decode_m((e < 4 ? mc.x : mc.y) >> (e % 4 * 8) & 255, mb);
-      v[e] = decode_v((e < 4 ? vc.x : vc.y) >> (e % 4 * 8) & 255, vb);
+      for (int e = 0; e < 4; ++e) {
+        p[e] = decode_m(x >> (8 * e) & 255, mb);
+        q[e] = decode_v(y >> (8 * e) & 255, vb);
+      }
+      *reinterpret_cast<floatx4*>(m) = p;
+      *reinterpret_cast<floatx4*>(v) = q;
+    } else {
+      for (int e = 0; e < left; ++e) {
+        m[e] = decode_m(mc[e], mb);
+        v[e] = decode_v(vc[e], vb);
+      }
     }
-    store8(t.p, false, i, left, m);
-    store8(t.master, false, i, left, v);
   }
 }
 

@@ -263,7 +263,7 @@ __global__ __launch_bounds__(KG * kThreads16, RB <= 2 ? 2 : 1) void ffn_gemm16_d
       }
     }
     if (KG == 1 || !kg) {
-      float* strip = reinterpret_cast<float*>((wave < 2 ? b0 : b1) + (wave & 1) * C::kStripBytes);
+      float* strip = reinterpret_cast<float*>((wave < 2 ? b0 : b1) + (wave & 1) * strip_bytes<MODE, C>());
       if constexpr (is_i8(MODE))
         epilogue_i8<MODE, C>(p, acc, sc, strip, row_scales<C>(b0, b1, wave), lane, wm, wn, g, row0, m_valid, n0);
       else

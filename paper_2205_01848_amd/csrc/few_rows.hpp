@@ -228,7 +228,7 @@ __global__ __launch_bounds__(64 * W) void ffn_few_rows_kernel(const GroupParams 
             const float l = static_cast<float>(sum[0][q]);
             if (lr < m && p.target[lr] == col) p.target_logit[lr] = l;
             float v[1] = {col < p.N ? l : -INFINITY};
-            vocab_row<16>(p, v, lr, lr < m, n0 / kFewCols, col, c16 == 0);
+            vocab_row<16, 1, 0>(p, v, lr, lr < m, n0 / kFewCols, c16 == 0);
           }
         } else if (col < p.N) {
           float s1 = 1.f, s3 = 1.f;

@@ -240,7 +240,8 @@ enum Mode {
   // the loss of a vocabulary projection (vocab.hip)
   M_VOCAB = 13,            // logits: each block of columns' maximum and sum of exponentials
                            // [, the exponentials saved]
-  M_VOCAB_DW = 14          // M_DENSE_DW, added to the fp32 sums of earlier pieces
+  M_VOCAB_DW = 14,         // M_DENSE_DW times alpha, added to the fp32 sums of earlier pieces
+  M_VOCAB_DX = 15          // store of alpha times the product, or partial sums
 };
 constexpr bool is_dense(int mode) { return mode >= M_GATED_FWD; }
 constexpr bool is_i8(int mode) { return mode >= M_I8_STORE && mode <= M_I8_FWD1_SWIGLU; }
@@ -308,6 +309,7 @@ struct GemmParams {
   // M_VOCAB: per row n_stat blocks of columns {maximum, sum of exp(l - maximum)}, the
   // tokens' targets and their logits; C: the exponentials, or NULL.
   // M_VOCAB_DW: the earlier pieces' sums (NULL: none)
+  float alpha;
   float2* stat; int n_stat;
   const int32_t* target; float* target_logit;
   const float* acc;
@@ -315,7 +317,7 @@ struct GemmParams {
 
 // The exponentials of M_VOCAB in 16 bits: fp16 of 2^15 exp(l - maximum), so that their 11
 // bits hold down to 2^-29.
-constexpr float kVocabScale = 32768.f;
+constexpr int kVocabLift = 15;
 
 // Tile order, two levels above each XCD's kGroupM x 8 block of tiles.
 // Tiles come in bands of kBandM M-tiles; inside a band, in N-blocks of 8
@@ -900,6 +902,11 @@ static_assert(2 * TileBig::kStripBytes <= kTileBytes, "two staging strips per op
 static_assert(2 * Tile16<1, 4>::kStripBytes <= kMidN * kRowBytes, "two staging strips per buffer");
 static_assert(Tile16<1, 4>::TN == kMidN && Tile16<1, 4>::TM == kMidUnit, "mid tile size");
 
+// LDS of a wave's strip: 16 padded rows; M_VOCAB 32 rows of WC.
+template <int MODE, typename C> constexpr int strip_bytes() {
+  static_assert(2 * 32 * Tile16<1, 4>::WC * 4 <= kMidN * kRowBytes && 2 * 32 * TileBig::WC * 4 <= kTileBytes, "fits");
+  return MODE == M_VOCAB ? 32 * C::WC * 4 : C::kStripBytes;
+}
 // Stage rows 16i .. 16i+15 of the wave's accumulators as fp32, row pitch C::kP.
 template <typename C>
 __device__ __forceinline__ void stage16(float* strip, const floatx4 (&acc)[C::RB][C::CB], int i,
@@ -911,12 +918,12 @@ __device__ __forceinline__ void stage16(float* strip, const floatx4 (&acc)[C::RB
     for (int q = 0; q < 4; ++q) strip[(4 * G + q) * C::kP + 16 * j + c16] = acc[i][j][q];
 }
 
-// M_VOCAB: N neighbouring lanes hold a block of columns of row `row`, lane by lane CN logits
-// v from column gc on (-inf behind the last column).  lead: the lane that writes the
-// block's maximum and sum.
-template <int N, int CN>
+// M_VOCAB: N neighbouring lanes hold a block of columns of row `row`, CN logits v each (-inf
+// for none): their maximum m and the sum of exp(l - m), written by the lane `lead`; v becomes
+// 2^LIFT exp(l - m).
+template <int N, int CN, int LIFT>
 __device__ __forceinline__ void vocab_row(const GemmParams& p, float (&v)[CN], int row, bool ok, int block,
-                                          int gc, bool lead) {
+                                          bool lead) {
   float m = v[0];
 #pragma unroll
   for (int e = 1; e < CN; ++e) m = fmaxf(m, v[e]);
@@ -925,23 +932,12 @@ __device__ __forceinline__ void vocab_row(const GemmParams& p, float (&v)[CN], i
   float s = 0.f;
 #pragma unroll
   for (int e = 0; e < CN; ++e) {
-    v[e] = exp_fast(v[e] - from);
+    v[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(v[e] - from, 1.4426950408889634f, LIFT));
     s += v[e];
   }
   s = group_sum<N>(s);
-  if (!ok) return;
-  if (lead) p.stat[static_cast<int64_t>(row) * p.n_stat + block] = make_float2(m, s);
-  if (gc >= p.N || !p.C) return;
-  char* c = p.C + row * p.ldc;
-  if constexpr (CN == 8) {
-    typedef _Float16 half8 __attribute__((ext_vector_type(8)));
-    half8 h;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) h[e] = static_cast<_Float16>(v[e] * kVocabScale);
-    *reinterpret_cast<half8*>(c + static_cast<int64_t>(gc) * 2) = h;
-  } else {
-    reinterpret_cast<float*>(c)[gc] = v[0];
-  }
+  if (ok && lead)
+    p.stat[static_cast<int64_t>(row) * p.n_stat + block] = make_float2(m, s * (1.f / (1 << LIFT)));
 }
 
 // Epilogue of one wave's block (RB x CB blocks of C): 16 accumulator rows at
@@ -1122,30 +1118,53 @@ __device__ __forceinline__ void epilogue16(const GemmParams& p,
       }
     }
   } else if constexpr (MODE == M_VOCAB) {
-    // LR lanes hold a row's WC columns, 8 each: their maximum m and sum of exp(l - m)
-    // across the group, the exponentials stored where gradients follow
+    // 32 rows at a time through LDS (pitch WC, 16-column groups swapped by the row's place
+    // among 16, so that neither the stores of 4 rows nor the reads meet), then a loop whose
+    // code is that of two passes: LR lanes hold a row's WC columns, 8 each.  Its 100 issue
+    // slots a pass (32 of them the 8 exponentials) take as long as a plain store's traffic
+    // (2048 rows, 1024 -> 32768, 256x256 tiles: 153 us, 158 with the exponentials
+    // stored, 154 for the logits in bf16; all of it unrolled, straight from the
+    // accumulators, 174 / 172 us in the loss's sequence)
     constexpr int LR = WC / 8, RG = 64 / LR;
-    const int block = 2 * (n0 / C::TN) + wn;
-    // the targets of the rows, 16 at a time, one a lane
-    int tg[C::RB];
+    const int block = 2 * (n0 / C::TN) + wn, col0 = n0 + wn * WC;
+    auto place = [](int r, int c) { return r * WC + (c ^ ((r >> 2 & 3) << 4)); };
 #pragma unroll
-    for (int i = 0; i < C::RB; ++i) {
-      const int lm = wr0 + 16 * i + el;
-      tg[i] = el < 16 && lm < m_valid ? p.target[row0 + lm] - (n0 + wn * WC) : -1;
-    }
+    for (int i = 0; i < C::RB; i += 2) {
+      constexpr int kLast = C::RB;
+      const int rows = 16 * (i + 1 < kLast ? 2 : 1), r0 = wr0 + 16 * i;
+      // the rows' targets, one a lane
+      const int mine = el & 31;
+      const int t = el < rows && r0 + mine < m_valid ? p.target[row0 + r0 + mine] - col0 : -1;
 #pragma unroll
-    for (int i = 0; i < C::RB; ++i) {
-      stage16<C>(strip, acc, i, el);
-      if (tg[i] >= 0 && tg[i] < WC) p.target_logit[row0 + wr0 + 16 * i + el] = strip[el * kP + tg[i]];
+      for (int h = 0; h < 2; ++h)
+        if (i + h < kLast) {
 #pragma unroll
-      for (int it = 0; it < 16 / RG; ++it) {
-        const int r = RG * it + el / LR, c8 = (el % LR) * 8;
-        const int lm = wr0 + 16 * i + r, gc = n0 + wn * WC + c8;
-        const float* sp = strip + r * kP + c8;
+          for (int j = 0; j < C::CB; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+              strip[place(16 * h + 4 * (el >> 4) + q, 16 * j + (el & 15))] = acc[i + h < kLast ? i + h : 0][j][q];
+        }
+      if (t >= 0 && t < WC) p.target_logit[row0 + r0 + mine] = strip[place(mine, t)];
+#pragma unroll 2
+      for (int r1 = 0; r1 < rows; r1 += RG) {
+        const int r = r1 + el / LR, c8 = (el % LR) * 8, lm = r0 + r, gc = col0 + c8;
+        const float* sp = strip + place(r, c8);
         float v[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = gc + e < p.N ? sp[e] : -INFINITY;
-        vocab_row<LR>(p, v, row0 + lm, lm < m_valid, block, gc, el % LR == 0);
+        for (int e = 0; e < 8; ++e) v[e] = sp[e];
+        if (col0 + WC > p.N) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (gc + e >= p.N) v[e] = -INFINITY;
+        }
+        vocab_row<LR, 8, kVocabLift>(p, v, row0 + lm, lm < m_valid, block, el % LR == 0);
+        if (lm < m_valid && p.C && gc < p.N) {
+          typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+          half8 o;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) o[e] = static_cast<_Float16>(v[e]);
+          *reinterpret_cast<half8*>(p.C + (row0 + lm) * p.ldc + 2 * gc) = o;
+        }
       }
     }
   } else {
@@ -1182,17 +1201,24 @@ __device__ __forceinline__ void epilogue16(const GemmParams& p,
           const float* sp = strip + r * kP + c8;
           if constexpr (is_dw(MODE)) {
             if constexpr (MODE == M_VOCAB_DW) {
-              if (p.acc && slot < 0) {
-                const float* q = p.acc + static_cast<int64_t>(row0 + lm) * p.N + gc;
-                const float4 lo = reinterpret_cast<const float4*>(q)[0], hi = reinterpret_cast<const float4*>(q)[1];
-                const float v[8] = {sp[0] + lo.x, sp[1] + lo.y, sp[2] + lo.z, sp[3] + lo.w,
-                                    sp[4] + hi.x, sp[5] + hi.y, sp[6] + hi.z, sp[7] + hi.w};
+              if (slot < 0) {
+                float v[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = p.alpha * sp[e];
+                if (p.acc) {
+                  const float* q = p.acc + static_cast<int64_t>(row0 + lm) * p.N + gc;
+                  float o[8];
+                  Elem<float>::load(reinterpret_cast<const uint4*>(q)[0], o);
+                  Elem<float>::load(reinterpret_cast<const uint4*>(q)[1], o + 4);
+#pragma unroll
+                  for (int e = 0; e < 8; ++e) v[e] += o[e];
+                }
                 if (!p.out_f32) {
                   *reinterpret_cast<uint4*>(dw_dst16(row0 + lm, gc)) = pack8(v);
                 } else {
-                  float* dst = dw_dst(row0 + lm, gc);
-                  *reinterpret_cast<float4*>(dst) = make_float4(v[0], v[1], v[2], v[3]);
-                  *reinterpret_cast<float4*>(dst + 4) = make_float4(v[4], v[5], v[6], v[7]);
+                  uint4* dst = reinterpret_cast<uint4*>(dw_dst(row0 + lm, gc));
+                  dst[0] = Elem<float>::store(v);
+                  dst[1] = Elem<float>::store(v + 4);
                 }
                 continue;
               }
@@ -1209,7 +1235,7 @@ __device__ __forceinline__ void epilogue16(const GemmParams& p,
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = sp[e];
             const int64_t grow = row0 + lm;
-            if constexpr (MODE == M_ADD_STORE) {
+            if constexpr (MODE == M_ADD_STORE || MODE == M_VOCAB_DX) {
               if (slot >= 0) {
                 float* dst = p.partial + slot * p.slot_elems + grow * p.N + gc;
                 *reinterpret_cast<float4*>(dst) = make_float4(v[0], v[1], v[2], v[3]);
@@ -1221,6 +1247,10 @@ __device__ __forceinline__ void epilogue16(const GemmParams& p,
                 unpack8(qa[(GB * i + it) % kRing], b);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] += b[e];
+              }
+              if constexpr (MODE == M_VOCAB_DX) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] *= p.alpha;
               }
             }
             if constexpr (MODE == M_FWD1) {
@@ -1495,7 +1525,7 @@ __global__ __launch_bounds__(kThreads16, 1) void ffn_gemm16_kernel(const GemmPar
 
     int z;
     asm volatile("s_mov_b32 %0, 0" : "=s"(z));
-    float* strip = reinterpret_cast<float*>((wave < 2 ? la0 : lb0) + (wave & 1) * C::kStripBytes + z);
+    float* strip = reinterpret_cast<float*>((wave < 2 ? la0 : lb0) + (wave & 1) * strip_bytes<MODE, C>() + z);
     if constexpr (is_i8(MODE))
       epilogue_i8<MODE, C>(p, acc, strip, row_scales<C>(la0, lb0, wave) + z, lane + z, wm, wn, g,
                            row0, m_valid, n0);
@@ -1633,7 +1663,7 @@ __global__ __launch_bounds__(kThreads16, 2) void ffn_gemm16_mid_kernel(const Gem
       floatx4 acc[RB][4];
       mainloop_mid<RB, ALAY, BLAY, GATED, ES>(t.op, la0, lb0, la1, lb1, acc, zt);
       asm volatile("s_mov_b32 %0, 0" : "=s"(z));
-      float* strip = reinterpret_cast<float*>((wave < 2 ? lb0 : lb1) + (wave & 1) * C::kStripBytes + z);
+      float* strip = reinterpret_cast<float*>((wave < 2 ? lb0 : lb1) + (wave & 1) * strip_bytes<MODE, C>() + z);
       if constexpr (is_i8(MODE))
         epilogue_i8<MODE, C>(p, acc, strip, row_scales<C>(lb0, lb1, wave) + z, lane + z, wm, wn, t.g,
                              t.row0, t.m_valid, t.n0);
@@ -1894,7 +1924,8 @@ __device__ __forceinline__ void epilogue_f32(const GemmParams& p, const MidTile&
         const bool ok = row_of(q) < t.m_valid;
         if (ok && tg[q] == col) p.target_logit[row] = acc[i][q];
         float v[1] = {col < p.N ? acc[i][q] : -INFINITY};
-        vocab_row<32>(p, v, row, ok, 4 * (t.n0 / kMidN) + wave, col, (lane & 31) == 0);
+        vocab_row<32, 1, 0>(p, v, row, ok, 4 * (t.n0 / kMidN) + wave, (lane & 31) == 0);
+        if (ok && p.C && col < p.N) reinterpret_cast<float*>(p.C + row * p.ldc)[col] = v[0];
       }
       continue;
     }
@@ -1905,7 +1936,7 @@ __device__ __forceinline__ void epilogue_f32(const GemmParams& p, const MidTile&
       const int64_t row = t.row0 + lm;
       if constexpr (VARK) {
         if constexpr (MODE == M_VOCAB_DW) {
-          if (t.slot < 0 && p.acc) acc[i][q] += p.acc[row * p.N + col];
+          if (t.slot < 0) acc[i][q] = p.alpha * acc[i][q] + (p.acc ? p.acc[row * p.N + col] : 0.f);
         }
         float* dst;
         if (t.slot >= 0) dst = p.partial + static_cast<int64_t>(t.slot) * p.slot_elems + row * p.N;
@@ -1933,6 +1964,9 @@ __device__ __forceinline__ void epilogue_f32(const GemmParams& p, const MidTile&
         } else if constexpr (MODE == M_GATED_DA) {
           *c = acc[i][q] * u1[q];
           c[p.f] = acc[i][q] * u3[q];
+        } else if constexpr (MODE == M_VOCAB_DX) {
+          if (t.slot >= 0) p.partial[t.slot * p.slot_elems + row * p.N + col] = acc[i][q];
+          else *c = p.alpha * acc[i][q];
         } else if constexpr (MODE == M_ADD_STORE) {
           if (t.slot >= 0) {
             p.partial[t.slot * p.slot_elems + row * p.N + col] = acc[i][q];

@@ -68,6 +68,27 @@ inline TileTime tile_time(bool f32, DenseKernel k, int h, DenseClass c) {
   return (c == D_KC ? deep_kc : deep_km)[h - 1];
 }
 
+// The logits' product of a vocabulary loss (vocab.hip), which has many columns and short
+// sums: ns a K step and of launch, prologue and epilogue, of a whole round and of a last
+// one that leaves one of the two places of every CU empty.  Fitted on half of 5049 bf16 and
+// 2710 fp32 products (18 to 8192 rows, 1003 to 131072 columns, K from 64 to 4096, every
+// kernel and height); on the other half the choice takes 2.2 and 1.5 % more than the best
+// measured kernel, by tile_time it would take 12 and 3 %.  Examples, us: 509 rows, 2048 ->
+// 50001, 256x256 / 192 x 128 tiles 132 / 100; 2204 rows, 2048 -> 50001 554 / 449.
+struct VocabTime {
+  int step, fix, half_step, half_fix;
+};
+inline VocabTime vocab_time(bool f32, DenseKernel k, int h) {
+  static const VocabTime mid32[] = {{1159, 5911, 586, 6314}, {2084, 10342, 1040, 10992}, {2925, 15119, 1482, 15774},
+                                    {3829, 19628, 1949, 20570}, {4716, 23975, 2413, 25354}, {5605, 28967, 2897, 30076}};
+  static const VocabTime deep32[] = {{1111, 6118, 552, 6154}, {1966, 10690, 992, 10637}, {}, {1927, 19778, 0, 0}};
+  static const VocabTime mid[] = {{547, 2774, 262, 2523}, {633, 4108, 313, 3367}, {741, 5665, 374, 4487},
+                                  {852, 7133, 408, 5648}, {993, 8455, 453, 6881}, {1130, 9909, 516, 8053}};
+  static const VocabTime deep[] = {{522, 2269, 292, 2346}, {642, 2782, 225, 3664}, {}, {498, 4706, 0, 0}};
+  if (k == K_BIG) return {1400, 17264, 0, 0};
+  return (k == K_MID ? (f32 ? mid32 : mid) : f32 ? deep32 : deep)[h - 1];
+}
+
 // One dense product: M x N results over K.
 struct DenseProduct {
   bool f32;
@@ -76,6 +97,8 @@ struct DenseProduct {
   bool b_km, dw;    // B K-major; both operands K-major (weight gradients)
   int M, N, K;
   int64_t lda, ldb; // row pitches, bytes
+  bool vocab = false;   // vocab_time
+  int most_ranges = 16; // of K
 };
 
 // The kernel, tile height and number of K ranges of a dense product: the host
@@ -94,7 +117,7 @@ inline DensePlan plan_dense(const DenseProduct& p, int cus, int tile_mode) {
   DensePlan best{};
   int64_t t_best = -1;
   // an activation needs the whole sum
-  const int most = p.active ? 1 : std::max(1, std::min(16, steps / 4));
+  const int most = p.active ? 1 : std::max(1, std::min(p.most_ranges, steps / 4));
   for (int want = 1; want <= most; ++want) {
     const int per = cdiv(steps, want), splits = cdiv(steps, per);   // K steps of a range
     if (splits != want) continue;
@@ -114,7 +137,13 @@ inline DensePlan plan_dense(const DenseProduct& p, int cus, int tile_mode) {
       const int64_t tiles = static_cast<int64_t>(n_mt) * nt * splits, places = static_cast<int64_t>(per_cu) * cus;
       const int64_t full = tiles / places, rem = tiles % places;
       const int64_t part = rem == 0 ? 0 : per_cu == 2 && 2 * rem <= places ? t.half : 100;
-      const int64_t time = (100 * full + part) * (static_cast<int64_t>(t.step) * per + t.fix) / 100 + join;
+      int64_t time = (100 * full + part) * (static_cast<int64_t>(t.step) * per + t.fix) / 100 + join;
+      if (p.vocab) {
+        const VocabTime v = vocab_time(f32, k, h);
+        const int64_t whole = static_cast<int64_t>(v.step) * per + v.fix;
+        time = full * whole + (part == 0 ? 0 : per_cu == 2 && 2 * rem <= places
+                                                   ? static_cast<int64_t>(v.half_step) * per + v.half_fix : whole);
+      }
       if (t_best >= 0 && time >= t_best) return;
       t_best = time;
       best = {k, h, n_mt, nt, splits, per * ks};

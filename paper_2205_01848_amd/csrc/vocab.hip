@@ -1,6 +1,7 @@
 // The loss of a vocabulary projection, and its gradients, in pieces of rows:
 //     l = x W^T,  lse_t = log sum_v exp l_tv,  loss_t = lse_t - l_t,target
-//     dl_tv = c_t (exp(l_tv - lse_t) - [v = target_t]),  dx = dl W,  dW = dl^T x.
+//     dl_tv = weight_t (exp(l_tv - lse_t) - [v = target_t]),
+//     dx = scale dl W,  dW = scale dl^T x.
 //
 // The logits' product leaves, for every row and block of 16 to 128 columns, their maximum m
 // and sum of exp(l - m), and the target's logit; a pass over those forms lse and
@@ -8,12 +9,14 @@
 // of the probability.  Without gradients no logit is ever written.
 //
 // With gradients the product also writes exp(l - m) of its piece, in 16 bits (11 of
-// mantissa), and one pass turns them into dl in place: c exp(m - lse) times that, and
-// c (exp(-loss) - 1) at the target.  Then dl W and dl^T x.  So nothing is computed twice:
+// mantissa), and one pass turns them into dl in place: weight exp(m - lse) times that, and
+// weight (exp(-loss) - 1) at the target.  Then dl W and dl^T x.  So nothing is computed twice:
 // 6 T V d operations and 6 bytes of traffic a logit, against 8 T V d for a second product of
 // the logits (8192 tokens, 4096 x 131072: the second product would take 6.3 ms, the
 // two passes over 2.1 GB of exponentials take 1 ms).  Kept as bf16 the exponentials would
-// round twice, and dx be off by sqrt(3) roundings for sqrt(2).
+// round twice, and dx be off by sqrt(3) roundings for sqrt(2).  scale joins the fp32 sums at
+// the end: in dl it would round every token's largest entry, near -scale, the same way (1037
+// tokens, scale 1 / 1037: dx off by 0.0029 of itself, 0.0017 the rounding of the result alone).
 //
 // The rows of ignored tokens are zeros in the products (a copy of x holds them), so that
 // nothing they contain reaches dW.
@@ -66,7 +69,7 @@ bool plan_vocab(moe_dtype dt, int T, int d, int V, bool grad, moe_dtype dw_dt, V
     p.width = g.few ? kFewCols : dt == MOE_F32 ? 32 : p.l.kernel == K_BIG ? TileBig::WC : kMidN / 2;
     p.stats = g.few ? cdiv(V, kFewCols) : p.l.nt * (dt == MOE_F32 ? 4 : 2);
     if (grad) {
-      p.dx = dense_plan<M_ADD_STORE, P_VOCAB_DX>(dt, rows, d, V, pitch, rd);
+      p.dx = dense_plan<M_VOCAB_DX, P_VOCAB_DX>(dt, rows, d, V, pitch, rd);
       p.dw = dense_plan<M_VOCAB_DW, P_VOCAB_DW>(dt, V, d, rows, pitch, rd);
     }
     return p;
@@ -120,7 +123,6 @@ struct VocabRows {
   const float2* stat;
   const int32_t* target;
   const float *target_logit, *weights;
-  float scale;
   float *loss, *lse;
   int32_t* status;
   int rows, V, stats, width, parts;
@@ -130,22 +132,35 @@ struct VocabRows {
 
 // A workgroup takes one of `parts` ranges of a row: the row's sum from its blocks', the loss,
 // and (GRAD) its range of dl.
-template <typename T, bool GRAD>
-__global__ __launch_bounds__(256) void vocab_rows_kernel(const VocabRows a) {
-  __shared__ float2 sums[4];
+template <typename T, bool GRAD, int THREADS>
+__global__ __launch_bounds__(THREADS) void vocab_rows_kernel(const VocabRows a) {
+  __shared__ float2 sums[THREADS / 64];
   const int64_t items = static_cast<int64_t>(a.rows) * a.parts;
   for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
     const int row = static_cast<int>(item / a.parts), part = static_cast<int>(item - static_cast<int64_t>(row) * a.parts);
     const float2* stat = a.stat + static_cast<int64_t>(row) * a.stats;
     float2 s = make_float2(-INFINITY, 0.f);
-    for (int i = threadIdx.x; i < a.stats; i += 256) s = join(s, stat[i]);
+    // (eight at a time, so that a long row waits for few loads)
+    for (int i = threadIdx.x; i < a.stats; i += 8 * THREADS) {
+      float2 b[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        b[k] = i + k * THREADS < a.stats ? stat[i + k * THREADS] : make_float2(-INFINITY, 0.f);
+#pragma unroll
+      for (int o = 4; o > 0; o >>= 1)
+#pragma unroll
+        for (int k = 0; k < o; ++k) b[k] = join(b[k], b[k + o]);
+      s = join(s, b[0]);
+    }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1)
       s = join(s, make_float2(__shfl_xor(s.x, o, 64), __shfl_xor(s.y, o, 64)));
     __syncthreads();   // the last row's sums have been read
     if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = s;
     __syncthreads();
-    s = join(join(sums[0], sums[1]), join(sums[2], sums[3]));
+    s = sums[0];
+#pragma unroll
+    for (int k = 1; k < THREADS / 64; ++k) s = join(s, sums[k]);
     const int target = a.target[row];
     const bool live = target >= 0 && target < a.V;
     const float logs = logf(s.y);
@@ -157,21 +172,20 @@ __global__ __launch_bounds__(256) void vocab_rows_kernel(const VocabRows a) {
     }
     if constexpr (GRAD) {
       constexpr int kVec = Elem<T>::kVec;   // 16 bytes of exponentials and of dl
-      const float c = live ? a.scale * (a.weights ? a.weights[row] : 1.f) : 0.f;
-      const float at = c * expm1f(-loss), f = c / s.y * (sizeof(T) == 2 ? 1.f / kVocabScale : 1.f);
+      const float c = a.weights ? a.weights[row] : 1.f;
+      const float at = c * expm1f(-loss), f = c / s.y * (sizeof(T) == 2 ? 1.f / (1 << kVocabLift) : 1.f);
       const int units = (a.V + kVec - 1) / kVec, per = (units + a.parts - 1) / a.parts;
       uint4* z = reinterpret_cast<uint4*>(a.z + row * a.pitch);
-      for (int u = part * per + threadIdx.x; u < min(units, (part + 1) * per); u += 256) {
+      for (int u = part * per + threadIdx.x; u < min(units, (part + 1) * per); u += THREADS) {
         const int col = u * kVec;
-        const uint4 b = z[u];
         float v[kVec];
         if constexpr (sizeof(T) == 2) {
           typedef _Float16 half8 __attribute__((ext_vector_type(8)));
-          const half8 h = __builtin_bit_cast(half8, b);
+          const half8 h = __builtin_bit_cast(half8, z[u]);
 #pragma unroll
           for (int e = 0; e < kVec; ++e) v[e] = static_cast<float>(h[e]);
         } else {
-          Elem<T>::load(b, v);
+          Elem<T>::load(z[u], v);
         }
         const float g = f * exp_fast(stat[col / a.width].x - s.x);
 #pragma unroll
@@ -193,8 +207,9 @@ moe_status launch_rows(hipStream_t s, VocabRows a) {
   a.parts = a.z ? static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(cdiv(4 * num_cus(), a.rows), units / 512))) : 1;
   const int grid = static_cast<int>(std::min<int64_t>(static_cast<int64_t>(a.rows) * a.parts, 16 * num_cus()));
   MOE_TIMED(a.z ? "vocab_dlogits" : "vocab_rows", s);
-  if (a.z) vocab_rows_kernel<T, true><<<grid, 256, 0, s>>>(a);
-  else vocab_rows_kernel<T, false><<<grid, 256, 0, s>>>(a);
+  if (a.z) vocab_rows_kernel<T, true, 256><<<grid, 256, 0, s>>>(a);
+  else if (a.stats > 2048) vocab_rows_kernel<T, false, 1024><<<grid, 1024, 0, s>>>(a);
+  else vocab_rows_kernel<T, false, 256><<<grid, 256, 0, s>>>(a);
   MOE_LAUNCH_CHECK();
   return MOE_OK;
 }
@@ -274,7 +289,7 @@ extern "C" moe_status moe_vocab_loss(void* stream, moe_dtype dt, int T, int d, i
     } else {
       MOE_TRY(launch_dense<M_VOCAB, P_VOCAB>(s, dt, plan.l, rows, rows, p));
     }
-    VocabRows r{stat, targets + t0, target_logit, weights ? weights + t0 : nullptr, scale, loss + t0,
+    VocabRows r{stat, targets + t0, target_logit, weights ? weights + t0 : nullptr, loss + t0,
                 lse ? lse + t0 : nullptr, status, rows, V, plan.stats, plan.width, 1, grad ? ws : nullptr, g.pitch};
     if (dt == MOE_BF16) MOE_TRY(launch_rows<uint16_t>(s, r));
     else MOE_TRY(launch_rows<float>(s, r));
@@ -288,8 +303,9 @@ extern "C" moe_status moe_vocab_loss(void* stream, moe_dtype dt, int T, int d, i
     q.N = d;
     q.C = static_cast<char*>(dx) + t0 * lddx * es;
     q.ldc = lddx * es;
+    q.alpha = scale;
     q.partial = reinterpret_cast<float*>(ws + g.o_part);
-    MOE_TRY(launch_dense<M_ADD_STORE, P_VOCAB_DX>(s, dt, plan.dx, rows, rows, q));
+    MOE_TRY(launch_dense<M_VOCAB_DX, P_VOCAB_DX>(s, dt, plan.dx, rows, rows, q));
     GemmParams u{};
     u.A = ws;
     u.lda = g.pitch;
@@ -300,6 +316,7 @@ extern "C" moe_status moe_vocab_loss(void* stream, moe_dtype dt, int T, int d, i
     u.out_f32 = !last || dw_dt == MOE_F32;
     u.dwA = u.dwB = u.out_f32 ? sums : static_cast<float*>(dw);
     u.split_row = V;
+    u.alpha = scale;
     u.acc = piece > 0 ? sums : nullptr;
     u.partial = q.partial;
     MOE_TRY(launch_dense<M_VOCAB_DW, P_VOCAB_DW>(s, dt, plan.dw, rows, V, u));
