@@ -15,8 +15,8 @@
 // the logits (8192 tokens, 4096 x 131072: the second product would take 6.3 ms, the
 // two passes over 2.1 GB of exponentials take 1 ms).  Kept as bf16 the exponentials would
 // round twice, and dx be off by sqrt(3) roundings for sqrt(2).  scale joins the fp32 sums at
-// the end: in dl it would round every token's largest entry, near -scale, the same way (1037
-// tokens, scale 1 / 1037: dx off by 0.0029 of itself, 0.0017 the rounding of the result alone).
+// the end: in dl it would round every token's largest entry, near -scale, the same way, by up
+// to 2^-8 (1 / 509 by 0.0019, where dx is off by 0.0018 of itself in all).
 //
 // The rows of ignored tokens are zeros in the products (a copy of x holds them), so that
 // nothing they contain reaches dW.

@@ -363,10 +363,11 @@ class MoELayer:
         return self.y
 
     def forward_i8(self, x, experts: QuantizedExperts, *, w_g=None, bias=None, renorm=0, ids=None,
-                   weights=None, capacity=("dynamic", 1, 1), shared=None):
+                   weights=None, capacity=("dynamic", 1, 1), shared=None, quantized=None):
         """The forward for serving, with the routed experts in 8-bit integers:
         gate (or cached ids) in the layer dtype -> quantise x, a scale per
-        token -> count, capacity, dispatch of the quantised rows (half the
+        token (or take quantized = (q, scale), x's rows in 8 bits as the norm
+        in front of the layer leaves them, RMSNorm(quantized=True)) -> count, capacity, dispatch of the quantised rows (half the
         bytes of bf16) -> int8 FFN -> combine [-> shared expert in the layer
         dtype].  x holds the layer's T tokens or fewer (with ids, weights
         [tokens, k]), and only those are routed and returned.  Arguments as for
@@ -390,6 +391,13 @@ class MoELayer:
                 raise ValueError(f"x has shape {tuple(x.shape)}, a layer with steps of its own takes all {T} tokens")
         if ids is not None and tuple(ids.shape) != (n, k):
             raise ValueError(f"ids have shape {tuple(ids.shape)}, expected {(n, k)}")
+        if quantized is not None:
+            q, scale = quantized
+            if tuple(q.shape) != (n, B.quantized_width(d)) or q.dtype != torch.int8 or not q.is_contiguous():
+                raise ValueError(f"quantised tokens {q.dtype} {tuple(q.shape)}, expected contiguous int8 "
+                                 f"{(n, B.quantized_width(d))}")
+            if tuple(scale.shape) != (n,) or scale.dtype != torch.float32 or not scale.is_contiguous():
+                raise ValueError(f"scales {scale.dtype} {tuple(scale.shape)}, expected contiguous float32 {(n,)}")
         if self.xq is None:
             width = B.quantized_width(d)
             new = lambda rows: torch.empty(rows, width, dtype=torch.int8, device=self.dev)
@@ -403,10 +411,13 @@ class MoELayer:
             ids, weights = self.ids, self.weights
         elif weights is None:
             weights = self.weights
-        xq, scale = self.xq, self.xq_scale
         if n < T:
-            xq, scale, ids = xq[:n], scale[:n], ids[:n]
-        B.moe_quantize_rows(x, xq, scale)
+            ids = ids[:n]
+        if quantized is not None:
+            xq, scale = quantized
+        else:
+            xq, scale = self.xq[:n], self.xq_scale[:n]
+            B.moe_quantize_rows(x, xq, scale)
         # the dispatch moves rows of 16-byte vectors: two int8 values ride as one bf16
         rows, disp = xq.view(torch.bfloat16), self.xq_disp.view(torch.bfloat16)
         kind, num, den = capacity
@@ -498,6 +509,159 @@ class MoELayer:
         if shared is not None:
             self.shared_bwd(x, dy, shared)
         return self.dx
+
+    def gradients(self, w1, w3, w2, *, w_g=None, shared=None):
+        """(weight, gradient) of every weight given, as the backward leaves the
+        gradients: what AdamW takes."""
+        if not self.backward_enabled:
+            raise ValueError("the layer was made without a backward")
+        if w_g is not None and not self.has_gate:
+            raise ValueError("the layer was made without a gate")
+        pairs = [(w1, self.dw1), (w3, self.dw3), (w2, self.dw2), (w_g, self.dw_g if w_g is not None else None)]
+        if shared is not None:
+            self._need_shared(shared)
+            pairs += list(zip(shared, (self.dsw1, self.dsw3, self.dsw2)))
+        return [p for p in pairs if p[0] is not None]
+
+
+class RMSNorm:
+    """Root-mean-square norm of up to T rows of d, after the addition on a residual
+    stream that precedes it (moe_rms_norm_fwd); quantized: also the rows in 8 bits,
+    in q [rows, width] and scale [rows], for MoELayer.forward_i8."""
+
+    def __init__(self, T: int, d: int, dtype: torch.dtype, eps: float = 1e-5, backward: bool = False,
+                 quantized: bool = False, device="cuda"):
+        self.T, self.d, self.eps, self.dtype = T, d, eps, dtype
+        self.dev = torch.device(device)
+        e = lambda *s, t=dtype: torch.empty(*s, dtype=t, device=self.dev)
+        f32 = torch.float32
+        self.y, self.sum = e(T, d), e(T, d)
+        self.q = e(T, B.quantized_width(d), t=torch.int8) if quantized else None
+        self.scale = e(T, t=f32) if quantized else None
+        self.backward_enabled = backward
+        self.rstd = self.s = None
+        if backward:
+            self.rstd, self.dx, self.dw = e(T, t=f32), e(T, d), e(d, t=f32)
+            self.ws = B.workspace(B.moe_rms_norm_bwd_workspace_bytes(T, d), self.dev)
+
+    def forward(self, x, weight, add=None):
+        """y = s rsqrt(mean s^2 + eps) weight for s = x + add (self.sum, the stream's next value) or
+        s = x, which the backward then reads: it has to stay as it is."""
+        n = x.shape[0]
+        if x.dim() != 2 or x.shape[1] != self.d or n > self.T:
+            raise ValueError(f"x has shape {tuple(x.shape)}, the norm takes up to {self.T} rows of {self.d}")
+        cut = lambda t: None if t is None else t[:n]
+        y, total = self.y[:n], None if add is None else self.sum[:n]
+        B.moe_rms_norm_fwd(x, weight, self.eps, y=y, add=add, sum=total, rstd=cut(self.rstd), q=cut(self.q),
+                           scale=cut(self.scale))
+        self.s = x if add is None else total
+        return y
+
+    def quantized(self, n: Optional[int] = None):
+        """(q, scale) of the last forward's first n rows (all T)."""
+        if self.q is None:
+            raise ValueError("the norm was made without rows in 8 bits (quantized)")
+        return self.q[:n], self.scale[:n]
+
+    def backward(self, dy, weight, dsum=None):
+        """The gradient of x (and of add), dsum added to it: what reaches the stream beside the norm.
+        self.dw holds the weight's."""
+        if not self.backward_enabled:
+            raise ValueError("the norm was made without a backward")
+        if self.s is None:
+            raise ValueError("the backward follows a forward")
+        n = self.s.shape[0]
+        dx = self.dx[:n]
+        B.moe_rms_norm_bwd(self.s, weight, self.rstd, dy, dx, self.dw, self.ws, dsum=dsum)
+        return dx
+
+
+class VocabLoss:
+    """Cross entropy of a projection of T tokens of width d onto V words (moe_vocab_loss), and with
+    backward both gradients, in dx and dw (dw_dtype: float32, or the layer's type)."""
+
+    def __init__(self, T: int, d: int, V: int, dtype: torch.dtype, backward: bool = False,
+                 dw_dtype: torch.dtype = torch.float32, device="cuda"):
+        self.T, self.d, self.V, self.dtype = T, d, V, dtype
+        self.dev = torch.device(device)
+        e = lambda *s, t=torch.float32: torch.empty(*s, dtype=t, device=self.dev)
+        code = lambda t: B.MOE_BF16 if t == torch.bfloat16 else B.MOE_F32
+        self.loss, self.lse = e(T), e(T)
+        self.status = torch.zeros(1, dtype=torch.int32, device=self.dev)
+        self.dx, self.dw = (e(T, d, t=dtype), e(V, d, t=dw_dtype)) if backward else (None, None)
+        self.ws = B.workspace(B.moe_vocab_loss_workspace_bytes(code(dtype), T, d, V,
+                                                               code(dw_dtype) if backward else None), self.dev)
+
+    def forward(self, x, w, targets, scale: Optional[float] = None, weights=None):
+        """The tokens' losses [T] (0 where the target is negative), and the gradients of
+        scale sum_t weights_t loss_t; scale: 1 / T by default."""
+        if tuple(x.shape) != (self.T, self.d) or tuple(w.shape) != (self.V, self.d):
+            raise ValueError(f"x and w have shapes {tuple(x.shape)} and {tuple(w.shape)}, expected "
+                             f"{(self.T, self.d)} and {(self.V, self.d)}")
+        B.moe_vocab_loss(x, w, targets, self.loss, self.lse, self.status, self.ws,
+                         scale=1 / max(self.T, 1) if scale is None else scale, weights=weights, dx=self.dx, dw=self.dw)
+        return self.loss
+
+
+class AdamW:
+    """AdamW on (weight, gradient) pairs (MoELayer.gradients, RMSNorm.dw, VocabLoss.dw), whose tensors it
+    keeps.  bits: 32, or 8 for the states of tensors of at least min_8bit values (smaller ones gain
+    nothing by it).  master: bf16 weights get float32 originals, of which they are the roundings.
+    Vectors take no weight decay.  captured: lr, the step's corrections and its seed are read from a device
+    tensor that prepare() fills, so that the step can be part of a graph."""
+
+    def __init__(self, pairs, lr: float = 1e-3, betas=(0.9, 0.95), eps: float = 1e-8, weight_decay: float = 0.1,
+                 bits: int = 32, master: bool = True, min_8bit: int = 4096, captured: bool = False):
+        if bits not in (8, 32):
+            raise ValueError(f"states in 8 or 32 bits, not {bits}")
+        self.lr, self.betas, self.eps, self.step_count = lr, betas, eps, 0
+
+        def tensor(p, g):
+            n = p.numel()
+            zeros = lambda k, t: torch.zeros(k, dtype=t, device=p.device)
+            kw = dict(weight_decay=weight_decay if p.dim() > 1 else 0.0,
+                      master=p.detach().float().reshape(-1) if master and p.dtype == torch.bfloat16 else None)
+            if bits == 8 and n >= min_8bit:
+                u8, blocks = torch.uint8, B.adamw_blocks(n)
+                return B.AdamWTensor(p, g, zeros(n, u8), zeros(n, u8), m_exp=zeros(blocks, u8),
+                                     v_exp=zeros(blocks, u8), **kw)
+            return B.AdamWTensor(p, g, zeros(n, torch.float32), zeros(n, torch.float32), **kw)
+
+        self.list = B.AdamWList([tensor(p, g) for p, g in pairs])
+        self.schedule = None
+        if captured and self.list.tensors:
+            self.schedule = torch.zeros(4, dtype=torch.float32, device=self.list.tensors[0].p.device)
+
+    def prepare(self, lr: Optional[float] = None):
+        """Counts the next step and, where it is captured, sends its numbers to the device (outside the
+        graph, before every replay)."""
+        self.step_count += 1
+        if lr is not None:
+            self.lr = lr
+        if self.schedule is not None:
+            self.schedule.copy_(B.adamw_schedule(self.lr, *self.betas, self.step_count, seed=self.step_count))
+
+    def apply(self, grad_scale=None):
+        """The prepared step; grad_scale [1] on the device multiplies every gradient."""
+        B.moe_adamw(self.list, self.lr, *self.betas, self.eps, max(self.step_count, 1), seed=self.step_count,
+                    grad_scale=grad_scale, schedule=self.schedule)
+
+    def step(self, lr: Optional[float] = None, grad_scale=None):
+        """prepare and apply."""
+        self.prepare(lr)
+        self.apply(grad_scale)
+
+    def moments(self):
+        """(m, v) of every tensor in float32, 8-bit ones as the values they stand for."""
+        out, packed = [], []
+        for t in self.list.tensors:
+            pair = (t.m, t.v) if t.m_exp is None else tuple(torch.empty(t.p.numel(), device=t.p.device) for _ in "mv")
+            out.append(pair)
+            if t.m_exp is not None:
+                packed.append((t, pair))
+        if packed:
+            B.moe_adamw_unpack(B.AdamWList([t for t, _ in packed]), [p for _, p in packed])
+        return out
 
 
 _STEPS = ("gate", "count", "capacity_static", "capacity_dynamic", "dispatch", "ffn_fwd", "combine")
