@@ -8,7 +8,10 @@
  * (expert capacity, drops, dynamic capacity factors), Section 4.2 (sample
  * assignment caching), Eq. 3 (balance term), Eq. 2 and its appendix
  * (specification loss, AggregateSpec), Section 3 with its implementation
- * appendix (metric-driven changes at the launch frontier).
+ * appendix (metric-driven changes at the launch frontier).  Around that layer:
+ * rows and experts in 8-bit integers, a dense gated block, the norm in front of
+ * it, the loss of a vocabulary projection behind the last one, and the AdamW
+ * step of the weights.
  *
  * Conventions shared by every call
  * --------------------------------
@@ -838,14 +841,15 @@ int moe_timing_report(char* buf, size_t len);
  * chosen on the device from the rows per expert) -- the latter for products
  * with few tiles per CU.  The int8 products and the dense gated block also
  * take tiles with more stages in flight (32 to 128 rows and 128 columns) and,
- * for few rows, a kernel without tiles.  1: 256x256 only; 2: 128-column tiles
- * only.  float32 experts run on 128-column tiles in every mode, a float32
- * dense block in modes 1 and 2.
+ * for few rows, a kernel without tiles; so do the vocabulary loss's.  1:
+ * 256x256 only; 2: 128-column tiles only.  float32 experts run on 128-column
+ * tiles in every mode, a float32 dense block or loss in modes 1 and 2.
  * The experts' results are identical bit for bit in every mode: their bf16
  * and float32 kernels add every output's products in the same order, and
  * int8 sums are exact.  A dense gated block's (and with it those of a layer
- * with a shared expert) agree up to the order of float32 sums: another mode
- * may split a sum over K into other ranges, or between more wavefronts.
+ * with a shared expert) and the vocabulary loss's agree up to the order of
+ * float32 sums: another mode may split a sum over K into other ranges, or
+ * between more wavefronts.
  * Process-wide; read when a product is launched.  Returns MOE_EINVAL for
  * other modes. [host]
  */

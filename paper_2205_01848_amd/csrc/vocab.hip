@@ -18,8 +18,8 @@
 // the end: in dl it would round every token's largest entry, near -scale, the same way, by up
 // to 2^-8 (1 / 509 by 0.0019, where dx is off by 0.0018 of itself in all).
 //
-// The rows of ignored tokens are zeros in the products (a copy of x holds them), so that
-// nothing they contain reaches dW.
+// dW's product reads a copy of x that the pass makes, with zeros in the rows of ignored
+// tokens, so that nothing they contain reaches it.
 //
 // A piece holds at most kPieceBytes of exponentials; dW of further pieces is added to the
 // fp32 sums of those before, in order.
@@ -96,22 +96,6 @@ bool plan_vocab(moe_dtype dt, int T, int d, int V, bool grad, moe_dtype dw_dt, V
   return true;
 }
 
-// x with zeros in the rows of ignored tokens, rows contiguous.
-template <typename T>
-__global__ __launch_bounds__(256) void vocab_x_kernel(const T* __restrict__ x, int64_t ldx, int rows, int d, int V,
-                                                      const int32_t* __restrict__ target, T* __restrict__ to) {
-  const int units = d / Elem<T>::kVec;
-  const int64_t all = static_cast<int64_t>(rows) * units;
-  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < all;
-       i += static_cast<int64_t>(gridDim.x) * 256) {
-    const int64_t row = i / units, u = i - row * units;
-    const int t = target[row];
-    uint4 v = make_uint4(0, 0, 0, 0);
-    if (t >= 0 && t < V) v = *reinterpret_cast<const uint4*>(x + row * ldx + u * Elem<T>::kVec);
-    reinterpret_cast<uint4*>(to)[i] = v;
-  }
-}
-
 // Maxima and sums of exponentials joined: {m, s} stands for s e^m.
 __device__ __forceinline__ float2 join(float2 a, float2 b) {
   const float m = fmaxf(a.x, b.x);
@@ -128,6 +112,10 @@ struct VocabRows {
   int rows, V, stats, width, parts;
   char* z;             // exponentials in, dl out; NULL: no gradients
   int64_t pitch;
+  const char* x;       // and x, copied to x_live with zeros in the rows of ignored tokens
+  int64_t ldx;         // bytes
+  char* x_live;
+  int x_units;         // vectors of a row
 };
 
 // A workgroup takes one of `parts` ranges of a row: the row's sum from its blocks', the loss,
@@ -171,6 +159,11 @@ __global__ __launch_bounds__(THREADS) void vocab_rows_kernel(const VocabRows a) 
       if (target >= a.V) atomicOr(a.status, MOE_STATUS_BAD_TARGET);
     }
     if constexpr (GRAD) {
+      if (part == 0) {
+        const uint4* from = reinterpret_cast<const uint4*>(a.x + row * a.ldx);
+        uint4* to = reinterpret_cast<uint4*>(a.x_live) + static_cast<int64_t>(row) * a.x_units;
+        for (int u = threadIdx.x; u < a.x_units; u += THREADS) to[u] = live ? from[u] : make_uint4(0, 0, 0, 0);
+      }
       constexpr int kVec = Elem<T>::kVec;   // 16 bytes of exponentials and of dl
       const float c = a.weights ? a.weights[row] : 1.f;
       const float at = c * expm1f(-loss), f = c / s.y * (sizeof(T) == 2 ? 1.f / (1 << kVocabLift) : 1.f);
@@ -214,17 +207,6 @@ moe_status launch_rows(hipStream_t s, VocabRows a) {
   return MOE_OK;
 }
 
-template <typename T>
-moe_status launch_x(hipStream_t s, const void* x, int64_t ldx, int rows, int d, int V, const int32_t* target,
-                    void* to) {
-  const int64_t all = static_cast<int64_t>(rows) * (d / Elem<T>::kVec);
-  MOE_TIMED("vocab_x", s);
-  vocab_x_kernel<T><<<static_cast<int>(std::min<int64_t>(8 * num_cus(), (all + 255) / 256)), 256, 0, s>>>(
-      static_cast<const T*>(x), ldx, rows, d, V, target, static_cast<T*>(to));
-  MOE_LAUNCH_CHECK();
-  return MOE_OK;
-}
-
 }  // namespace
 }  // namespace moe
 
@@ -260,17 +242,9 @@ extern "C" moe_status moe_vocab_loss(void* stream, moe_dtype dt, int T, int d, i
     const bool last = piece + 1 == g.pieces;
     const VocabPiece& plan = last ? g.last : g.full;
     const char* xp = static_cast<const char*>(x) + t0 * ldx * es;
-    int64_t xld = ldx;
-    if (grad) {
-      char* to = ws + g.o_x;
-      if (dt == MOE_BF16) MOE_TRY(launch_x<uint16_t>(s, xp, ldx, rows, d, V, targets + t0, to));
-      else MOE_TRY(launch_x<float>(s, xp, ldx, rows, d, V, targets + t0, to));
-      xp = to;
-      xld = d;
-    }
     GemmParams p{};
     p.A = xp;
-    p.lda = xld * es;
+    p.lda = ldx * es;
     p.B = static_cast<const char*>(w);
     p.ldb = d * es;
     p.K = d;
@@ -290,7 +264,8 @@ extern "C" moe_status moe_vocab_loss(void* stream, moe_dtype dt, int T, int d, i
       MOE_TRY(launch_dense<M_VOCAB, P_VOCAB>(s, dt, plan.l, rows, rows, p));
     }
     VocabRows r{stat, targets + t0, target_logit, weights ? weights + t0 : nullptr, loss + t0,
-                lse ? lse + t0 : nullptr, status, rows, V, plan.stats, plan.width, 1, grad ? ws : nullptr, g.pitch};
+                lse ? lse + t0 : nullptr, status, rows, V, plan.stats, plan.width, 1, grad ? ws : nullptr, g.pitch,
+                xp, ldx * es, ws + g.o_x, static_cast<int>(d * es / 16)};
     if (dt == MOE_BF16) MOE_TRY(launch_rows<uint16_t>(s, r));
     else MOE_TRY(launch_rows<float>(s, r));
     if (!grad) continue;
@@ -310,7 +285,7 @@ extern "C" moe_status moe_vocab_loss(void* stream, moe_dtype dt, int T, int d, i
     u.A = ws;
     u.lda = g.pitch;
     u.M_out = V;
-    u.B = xp;
+    u.B = ws + g.o_x;
     u.ldb = d * es;
     u.N = d;
     u.out_f32 = !last || dw_dt == MOE_F32;

@@ -226,3 +226,26 @@ def test_captured_steps_take_their_schedule_from_the_device():
         for a, b in zip(*cases):
             for k in a.wide:
                 assert torch.equal(a.wide[k], b.wide[k]), (step, k)
+
+
+def test_elements_past_32_bits():
+    """A tensor of more than 2^32 values: its parts around 2^31 and 2^32 and its end, codes and all."""
+    n = (1 << 32) + 300
+    g = torch.Generator(device="cuda").manual_seed(0)
+    u8 = lambda k: torch.zeros(k, dtype=torch.uint8, device=dev())
+    p, grad = torch.zeros(n, dtype=torch.bfloat16, device=dev()), torch.zeros(n, dtype=torch.bfloat16, device=dev())
+    parts = [slice(0, 1024), slice((1 << 31) - 512, (1 << 31) + 512), slice((1 << 32) - 512, n - 300 + 256), slice(n - 300 + 256, n)]
+    for s in parts:
+        grad[s] = torch.randn(s.stop - s.start, generator=g, device="cuda").to(torch.bfloat16)
+    t = B.AdamWTensor(p, grad, u8(n), u8(n), m_exp=u8(B.adamw_blocks(n)), v_exp=u8(B.adamw_blocks(n)))
+    B.moe_adamw(B.AdamWList([t]), **HYPER, seed=9)
+    for s in parts:
+        k, blocks = s.stop - s.start, slice(s.start // 128, -(-s.stop // 128))
+        gr = to_np(grad[s])
+        _, m, v = O.adamw(np.zeros(k), gr, np.zeros(k), np.zeros(k), 0.01, 0.9, 0.99, 1e-7, 7)
+        rm, rv = O.adamw_random(k, 9, 0, start=s.start)
+        for x, r, mant, code, e in ((m, rm, 3, t.m, t.m_exp), (v, rv, 4, t.v, t.v_exp)):
+            c, ee = O.adamw_encode(x, r, mant)
+            np.testing.assert_array_equal(code[s].cpu().numpy(), c)
+            np.testing.assert_array_equal(e[blocks].cpu().numpy(), ee)
+        assert (p[s][grad[s] != 0] != 0).all()

@@ -45,11 +45,11 @@ def _call(x, w, t, dt, grad, dw_dt=None, scale=1.0, weights=None, pad=0, ws=None
         o.update(dx=full(T + 1, d + pad, t=DT[dt]), dw=full(V + 1, d, t=DT[dw_dt or dt]))
     n = B.moe_vocab_loss_workspace_bytes(CODE[dt], T, d, V, CODE[dw_dt or dt] if grad else None)
     if ws is None:
-        ws = torch.full((n + 64,), 0x7F, dtype=torch.uint8, device=dev())       # (NaNs, as floats and as fp16)
+        ws = torch.full((n + 64,), 0xFF, dtype=torch.uint8, device=dev())       # (NaNs, as float32, bf16 and fp16)
     B.moe_vocab_loss(x, w, torch.from_numpy(t).to(dev()), o["loss"], o["lse"], o["status"], ws[:n] if n else ws,
                      scale=scale, weights=weights, dx=o["dx"][:T, :d] if grad else None, dw=o["dw"] if grad else None)
     torch.cuda.synchronize()
-    assert (ws[n:] == 0x7F).all()
+    assert (ws[n:] == 0xFF).all()
     return o
 
 
@@ -286,3 +286,38 @@ def test_captured_and_replayed(T, grad):
         torch.cuda.synchronize()
         for name in (a if grad else ("loss", "lse")):
             assert torch.equal(a[name], b[name]), name
+
+
+@pytest.mark.parametrize("T", [3, 40])
+def test_weights_past_32_bits(T):
+    """A vocabulary whose weights (and dW) reach past 2^31 elements and 2^32 bytes."""
+    d, V = 4104, 530000
+    assert V * d > 2 ** 31
+    g = torch.Generator(device="cuda").manual_seed(T)
+    w = torch.empty(V, d, dtype=torch.bfloat16, device=dev())
+    for part in w.split(50000):
+        part.copy_(torch.randn(part.shape, generator=g, device="cuda") * 3 / d ** 0.5)
+    x = torch.randn(T, d, generator=g, device="cuda").to(torch.bfloat16)
+    t = torch.randint(V - 1000, V, (T,), generator=g, device="cuda")
+    t[0] = 5
+    o = _call(x, w, t.int().cpu().numpy(), "bf16", T > 16)
+    X = x.double()
+    l = torch.cat([X @ part.double().T for part in w.split(50000)], 1)
+    lse = torch.logsumexp(l, 1)
+    loss = lse - l.gather(1, t[:, None])[:, 0]
+    # D: the sum of 4104 products' sizes is at most |x| |w| (Cauchy), 1.2 * 64 * 3.2
+    D = 2 * SUM(d) * 1.2 * 64 * 3.2 + 2e-6 + 2 * U * 40
+    assert (o["loss"][:T].double() - loss).abs().max() <= D and (o["lse"][:T].double() - lse).abs().max() <= D
+    if T > 16:
+        p = torch.exp(l - lse[:, None])
+        dl = p.scatter_add(1, t[:, None], torch.full((T, 1), -1.0, dtype=torch.float64, device="cuda"))
+        e = p * (D + 2.0 ** -11) + 2.0 ** -8 * dl.abs() + 2.0 ** -39
+        for rows in (slice(0, 2000), slice(V // 2, V // 2 + 2000), slice(V - 2000, V)):
+            dw = dl[:, rows].T @ X
+            bound = (e[:, rows].T + SUM(T) * dl[:, rows].abs().T) @ X.abs()
+            assert ((o["dw"][:V][rows].double() - dw).abs() <= 1.01 * bound + 2.0 ** -8 * dw.abs()).all()
+        dx, dxe = 0, 0
+        for part, q, r in zip(w.split(50000), dl.split(50000, 1), e.split(50000, 1)):
+            W = part.double()
+            dx, dxe = dx + q @ W, dxe + r @ W.abs() + SUM(V) * q.abs() @ W.abs()
+        assert ((o["dx"][:T, :d].double() - dx).abs() <= 1.01 * dxe + 2.0 ** -8 * dx.abs()).all()
