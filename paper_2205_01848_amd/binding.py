@@ -523,20 +523,21 @@ def _rows(t: Optional[torch.Tensor], name, T, d, dtype, optional=False):
         if optional:
             return 0
         raise MoEError(f"{name} is required")
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise MoEError(f"{name}: element type {t.dtype}, expected {dtype}")
-    if tuple(t.shape) != (T, d):
+    if t.shape != (T, d):
         raise MoEError(f"{name} has shape {tuple(t.shape)}, expected {(T, d)}")
     if T == 0:
         return d
-    if t.stride(1) != 1 and d > 1:
+    ld, one = t.stride()
+    if one != 1 and d > 1:
         raise MoEError(f"{name}: the elements of a row must be contiguous")
     if T == 1:
         return d
-    if t.stride(0) < d or t.stride(0) % 8:
-        raise MoEError(f"{name}: rows are {t.stride(0)} elements apart, a multiple of 8 not below "
+    if ld < d or ld % 8:
+        raise MoEError(f"{name}: rows are {ld} elements apart, a multiple of 8 not below "
                        f"{d} is needed")
-    return t.stride(0)
+    return ld
 
 
 def _at(t: Optional[torch.Tensor]):
@@ -566,12 +567,17 @@ def moe_rms_norm_fwd(x, weight, eps, y=None, add=None, sum=None, rstd=None, q=No
     tensors."""
     (rows, d), dtype = x.shape, x.dtype
     dt = _dt(x)
-    ldx, ldadd, ldsum, ldy = (_rows(t, n, rows, d, dtype, optional=n != "x") for t, n in
-                              ((x, "x"), (add, "add"), (sum, "sum"), (y, "y")))
+    ldx = _rows(x, "x", rows, d, dtype)
+    ldadd = 0 if add is None else _rows(add, "add", rows, d, dtype)
+    ldsum = 0 if sum is None else _rows(sum, "sum", rows, d, dtype)
+    ldy = 0 if y is None else _rows(y, "y", rows, d, dtype)
     _need(weight, d, "weight", dtype)
-    _need(rstd, rows, "rstd", _F32, optional=True)
-    _need(q, rows * quantized_width(d), "q", torch.int8, optional=True)
-    _need(scale, rows, "scale", _F32, optional=True)
+    if rstd is not None:
+        _need(rstd, rows, "rstd", _F32)
+    if q is not None:
+        _need(q, rows * quantized_width(d), "q", torch.int8)
+    if scale is not None:
+        _need(scale, rows, "scale", _F32)
     with _Here(_device_of(x, weight, y, add, sum, rstd, q, scale)) as stream:
         _check(lib().moe_rms_norm_fwd(stream, dt, rows, d, _at(x), ldx, _at(add), ldadd, _ptr(weight),
                                       eps, _at(sum), ldsum, _at(y), ldy, _ptr(rstd), _ptr(q),
@@ -586,8 +592,9 @@ def moe_rms_norm_bwd(s, weight, rstd, dy, dx, dw, ws, dsum=None):
     """Gradients of moe_rms_norm_fwd; dw (float32 or the layer's type) and ws None: dx alone."""
     (rows, d), dtype = s.shape, s.dtype
     dt = _dt(s)
-    lds, lddy, lddx = (_rows(t, n, rows, d, dtype) for t, n in ((s, "s"), (dy, "dy"), (dx, "dx")))
-    lddsum = _rows(dsum, "dsum", rows, d, dtype, optional=True)
+    lds = _rows(s, "s", rows, d, dtype)
+    lddy, lddx = _rows(dy, "dy", rows, d, dtype), _rows(dx, "dx", rows, d, dtype)
+    lddsum = 0 if dsum is None else _rows(dsum, "dsum", rows, d, dtype)
     _need(weight, d, "weight", dtype)
     _need(rstd, rows, "rstd", _F32)
     if dw is not None and dw.dtype not in (dtype, _F32):

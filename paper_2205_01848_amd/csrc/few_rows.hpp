@@ -225,10 +225,15 @@ __global__ __launch_bounds__(64 * W) void ffn_few_rows_kernel(const GroupParams 
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
             const int lr = r0 + 16 * wave + 4 * G + q;
+            const bool ok = lr < m;
             const float l = static_cast<float>(sum[0][q]);
-            if (lr < m && p.target[lr] == col) p.target_logit[lr] = l;
+            if (ok && p.target[lr] == col) p.target_logit[lr] = l;
             float v[1] = {col < p.N ? l : -INFINITY};
-            vocab_row<16, 1, 0>(p, v, lr, lr < m, n0 / kFewCols, c16 == 0);
+            vocab_row<16, 1, ES == 4 ? 0 : kVocabLift>(p, v, lr, ok, n0 / kFewCols, c16 == 0);
+            if (!ok || !p.C || col >= p.N) continue;
+            char* c = p.C + lr * p.ldc;
+            if constexpr (ES == 4) reinterpret_cast<float*>(c)[col] = v[0];
+            else reinterpret_cast<_Float16*>(c)[col] = static_cast<_Float16>(v[0]);
           }
         } else if (col < p.N) {
           float s1 = 1.f, s3 = 1.f;

@@ -17,6 +17,7 @@ struct DensePlan {
   int h;          // units of rows per tile (mid, deep)
   int n_mt, nt;   // tiles along M and N
   int splits, klen;
+  int64_t time = 0;   // as estimated, ns
 };
 
 // Time of a round of tiles on all places of the persistent grid: `step` ns per K
@@ -89,6 +90,18 @@ inline VocabTime vocab_time(bool f32, DenseKernel k, int h) {
   return (k == K_MID ? (f32 ? mid32 : mid) : f32 ? deep32 : deep)[h - 1];
 }
 
+// Whether its few rows rather go through the kernel that streams the weights (few_rows.hpp;
+// up to 16 rows, 32 in fp32): it reads them at 5800 bytes per ns and takes a
+// thirtieth longer for every row, whose values every workgroup reads again; tiles take what
+// the plan says, at least the read at 5300.  Us, few / tiles: 131072 x 4096, 1 or 2 rows 184 /
+// 200, 9 rows 234 / 203; 50001 x 1024, 2 rows 22 / 18; 1717 x 2608, 2 rows 7.4 / 13.1, fp32
+// 9.0 / 51; fp32 8191 x 512, 32 rows 10 / 17.
+inline bool vocab_few(bool f32, int M, int N, int K, const DensePlan& tiles) {
+  if (M > (f32 ? 32 : 16)) return false;
+  const int64_t bytes = static_cast<int64_t>(N) * K * (f32 ? 4 : 2);
+  return bytes * (30 + M) / (30 * 5800) + 3500 < std::max(tiles.time, bytes / 5300);
+}
+
 // One dense product: M x N results over K.
 struct DenseProduct {
   bool f32;
@@ -146,7 +159,7 @@ inline DensePlan plan_dense(const DenseProduct& p, int cus, int tile_mode) {
       }
       if (t_best >= 0 && time >= t_best) return;
       t_best = time;
-      best = {k, h, n_mt, nt, splits, per * ks};
+      best = {k, h, n_mt, nt, splits, per * ks, time};
     };
     const int units = cdiv(M, kMidUnit), nt = cdiv(N, gated ? kMidN / 2 : kMidN);
     if (!f32 && tile_mode != 2) take(K_BIG, 0, cdiv(M, BM), cdiv(N, gated ? BN / 2 : BN), 1);

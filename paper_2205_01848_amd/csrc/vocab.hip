@@ -32,7 +32,6 @@ namespace {
 
 constexpr int64_t kPieceBytes = int64_t(1) << 31;    // of exponentials
 constexpr int64_t kStatBytes = int64_t(1) << 28;     // of maxima and sums, without gradients
-constexpr int kFewVocab = 16;                        // rows that stream W through the kernel for few rows
 
 struct VocabPiece {
   DensePlan l, dx, dw;
@@ -56,7 +55,6 @@ bool plan_vocab(moe_dtype dt, int T, int d, int V, bool grad, moe_dtype dw_dt, V
   g.total = 256;
   g.pitch = pitch;
   if (T == 0) return true;
-  g.few = !grad && g_tile_mode == 0 && T <= (dt == MOE_F32 ? 2 : 1) * kFewVocab;
   const int64_t least = dt == MOE_F32 ? 32 : 64;   // columns of a block, of the kernels for many rows
   const int64_t row = grad ? pitch : (V + least - 1) / least * 8, cap = grad ? kPieceBytes : kStatBytes;
   const int64_t most = std::max<int64_t>(cap / row / BM * BM, BM);
@@ -66,6 +64,7 @@ bool plan_vocab(moe_dtype dt, int T, int d, int V, bool grad, moe_dtype dw_dt, V
   auto piece = [&](int rows) {
     VocabPiece p{};
     p.l = dense_plan<M_VOCAB, P_VOCAB>(dt, rows, V, d, rd, rd);
+    g.few = g_tile_mode == 0 && vocab_few(dt == MOE_F32, T, V, d, p.l);   // (of all rows: then one piece)
     p.width = g.few ? kFewCols : dt == MOE_F32 ? 32 : p.l.kernel == K_BIG ? TileBig::WC : kMidN / 2;
     p.stats = g.few ? cdiv(V, kFewCols) : p.l.nt * (dt == MOE_F32 ? 4 : 2);
     if (grad) {

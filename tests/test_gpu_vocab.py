@@ -85,6 +85,17 @@ def _check(o, x, w, t, dt, dw_dt=None, scale=1.0, weights=None):
 SIZES = [(1, 8, 1, 0), (1, 64, 7, 8), (1, 1024, 5003, 0), (2, 72, 8, 0), (3, 24, 9, 8), (5, 64, 129, 0), (15, 64, 1000, 0),
          (16, 520, 1003, 0), (17, 264, 1003, 8), (33, 128, 257, 0), (64, 1024, 4099, 0), (130, 64, 8191, 24),
          (300, 1024, 2050, 0), (509, 136, 3001, 64), (1030, 512, 5003, 0), (2049, 64, 511, 0)]
+# the tiles of the products these do not take (test_vocab_plans): bf16, then float32
+TILES = {"bf16": [(497, 592, 32682), (20, 328, 138), (356, 72, 11443), (230, 200, 26644), (2698, 64, 3153), (331, 80, 29154),
+                  (22, 2040, 149), (1481, 1296, 2329), (71, 536, 19796)],
+         "f32": [(44, 64, 37519), (329, 64, 12709), (238, 72, 25045), (1494, 64, 6065), (525, 80, 18553), (38, 72, 34014),
+                 (395, 1832, 5237), (19, 224, 26377), (1642, 1184, 165)]}
+
+
+@pytest.mark.parametrize("dt,T,d,V", [(dt, *s) for dt in TILES for s in TILES[dt]])
+def test_tiles(dt, T, d, V):
+    x, w, t = _inputs(T, d, V, 0, dt, np.random.default_rng(V))
+    _check(_call(x, w, t, dt, True), x, w, t, dt)
 
 
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
