@@ -118,7 +118,9 @@ struct VocabRows {
 };
 
 // A workgroup takes one of `parts` ranges of a row: the row's sum from its blocks', the loss,
-// and (GRAD) its range of dl.
+// and (GRAD) its range of dl.  Bound by memory: 4 bytes a logit (8 in fp32), 8192 x 131072 in 0.88
+// ms, 4.9 TB/s.  The row of one token has 8192 blocks: 6 us with 1024 threads and eight
+// loads in flight, 15 with 256 and one.
 template <typename T, bool GRAD, int THREADS>
 __global__ __launch_bounds__(THREADS) void vocab_rows_kernel(const VocabRows a) {
   __shared__ float2 sums[THREADS / 64];
