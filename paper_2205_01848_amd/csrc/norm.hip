@@ -168,6 +168,9 @@ struct NormBwdArgs {
 template <typename T, int G, int U>
 __global__ __launch_bounds__(kNormThreads<G>) void norm_bwd_kernel(const NormBwdArgs a) {
   constexpr int kPer = kNormThreads<G> / G;
+  // dsum with the other rows' loads, but where 1024 threads hold 4 units of fp32 each: of
+  // their 128 registers 63 would go to scratch memory (9 this way)
+  constexpr bool kAhead = sizeof(T) == 2 || G * U < 4096;
   __shared__ SumMax part[2][G / kWave];
   __shared__ float join[kPer > 1 ? kPer * U * G * 8 : 1];
   int turn = 0;
@@ -184,6 +187,7 @@ __global__ __launch_bounds__(kNormThreads<G>) void norm_bwd_kernel(const NormBwd
     if (row >= a.rows) break;
     const T* s = static_cast<const T*>(a.s) + row * a.lds;
     const T* dy = static_cast<const T*>(a.dy) + row * a.lddy;
+    const T* ds = a.dsum ? static_cast<const T*>(a.dsum) + row * a.lddsum : nullptr;
     Unit<T> su[U], gu[U], du[U];
 #pragma unroll
     for (int i = 0; i < U; ++i)
@@ -191,8 +195,7 @@ __global__ __launch_bounds__(kNormThreads<G>) void norm_bwd_kernel(const NormBwd
         su[i].load(s + (t + i * G) * 8);
         gu[i].load(dy + (t + i * G) * 8);
       }
-    if (a.dsum) {
-      const T* ds = static_cast<const T*>(a.dsum) + row * a.lddsum;
+    if (kAhead && ds) {
 #pragma unroll
       for (int i = 0; i < U; ++i)
         if (t + i * G < units) du[i].load(ds + (t + i * G) * 8);
@@ -229,7 +232,8 @@ __global__ __launch_bounds__(kNormThreads<G>) void norm_bwd_kernel(const NormBwd
       wu.get(v);
 #pragma unroll
       for (int e = 0; e < 8; ++e) g[e] = r * (g[e] * v[e] - f[e] * c);
-      if (a.dsum) {
+      if (ds) {
+        if (!kAhead) du[i].load(ds + u * 8);
         du[i].get(f);
 #pragma unroll
         for (int e = 0; e < 8; ++e) g[e] += f[e];
