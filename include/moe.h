@@ -794,14 +794,15 @@ size_t moe_adamw_blocks(int64_t n);
  *   p = p (1 - lr weight_decay)
  *       - lr m / (1 - beta1^step) / (sqrt(v / (1 - beta2^step)) + eps)
  * in float32; moments kept in 8 bits are formed in float64 (each product rounded
- * by itself, g^2 before its factor), used for p before they are rounded, and rounded to the code above or below at random, with the probability that
- * makes the code right on average (a v above 0 is kept above 0, an m 16 octaves
- * below its block's largest becomes 0).  The random bits depend on seed, the
- * tensor's place in the list and the element alone: give every step another seed.
+ * by itself, g^2 before its factor), used for p before they are rounded, and
+ * rounded to the code above or below at random, with the probability that makes
+ * the code right on average (a v above 0 is kept above 0, an m 16 octaves below
+ * its block's largest becomes 0).  The random bits depend on seed, the tensor's
+ * place in the list and the element alone: give every step another seed.
  * An m that is not a finite float32 is kept as NaN; a v that is not, as its block's
  * largest value.
  *   tensors    [host] [count] (read before the call returns)
- *   lr, eps    lr >= 0, eps > 0, finite; 0 <= beta < 1; step >= 1
+ *   lr, eps    lr >= 0, eps >= 2^-126, finite; 0 <= beta < 1; step >= 1
  *   grad_scale NULL, or device [1]: every gradient is multiplied by it (a clipping
  *              factor, the inverse of a loss scale)
  *   schedule   NULL, or device: replaces lr, the corrections of `step`, and seed

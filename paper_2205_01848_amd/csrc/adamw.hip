@@ -403,8 +403,9 @@ extern "C" moe_status moe_adamw(void* stream, int count, const moe_adamw_tensor*
                                 const float* grad_scale, const moe_adamw_schedule* schedule) {
   auto fine = [](double v) { return v >= 0 && v < INFINITY; };
   if (count < 0 || (count > 0 && !tensors) || step < 1) return MOE_EINVAL;
+  // (the hardware takes a subnormal divisor for zero: 0 / eps would be NaN)
   if (!fine(lr) || !fine(beta1) || !fine(beta2) || beta1 >= 1 || beta2 >= 1 || !fine(eps) ||
-      !(static_cast<float>(eps) > 0.f))
+      !(static_cast<float>(eps) >= 0x1p-126f))
     return MOE_EINVAL;
   if ((reinterpret_cast<uintptr_t>(schedule) | reinterpret_cast<uintptr_t>(grad_scale)) & 3) return MOE_EINVAL;
   for (int i = 0; i < count; ++i)

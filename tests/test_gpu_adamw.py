@@ -155,6 +155,18 @@ def test_from_zero_states():
 
 
 @pytest.mark.parametrize("bits", [8, 32])
+def test_least_eps(bits):
+    """v = 0 leaves eps alone to divide by: 0 / eps is 0 for the least eps that is taken."""
+    n, eps = 300, 2.0 ** -126
+    zero = lambda k, t=torch.float32: torch.zeros(k, dtype=t, device=dev())
+    u8 = torch.uint8
+    m, v, e = (zero(n, u8), zero(n, u8), dict(m_exp=zero(3, u8), v_exp=zero(3, u8))) if bits == 8 else (zero(n), zero(n), {})
+    p, g = torch.ones(n, device=dev()), zero(n)
+    B.moe_adamw(B.AdamWList([B.AdamWTensor(p, g, m, v, **e)]), 0.01, 0.9, 0.99, eps, 1)
+    assert (p == 1).all() and not m.any() and not v.any()
+
+
+@pytest.mark.parametrize("bits", [8, 32])
 def test_gradients_that_are_not_finite_stay_in_their_element(bits):
     n, rng = 256, np.random.default_rng(0)
     c = Case(n, rng, bits)

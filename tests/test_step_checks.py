@@ -131,7 +131,7 @@ def _adamw(lib, count=1, lr=0.1, b1=0.9, b2=0.99, eps=1e-8, step=1, scale=None, 
 
 @pytest.mark.parametrize("kw", [
     dict(count=-1), dict(tensors=False), dict(lr=-0.1), dict(lr=math.nan), dict(lr=math.inf), dict(b1=1.0), dict(b1=-0.1),
-    dict(b2=1.0), dict(b2=math.nan), dict(eps=0.0), dict(eps=1e-60), dict(eps=math.inf), dict(step=0), dict(n=-1),
+    dict(b2=1.0), dict(b2=math.nan), dict(eps=0.0), dict(eps=1e-60), dict(eps=1e-40), dict(eps=math.inf), dict(step=0), dict(n=-1),
     dict(p_dtype=2), dict(g_dtype=-1), dict(weight_decay=-1.0), dict(weight_decay=math.nan), dict(m_exp=64), dict(v_exp=64),
     dict(p_dtype=0, master=64), dict(n=5, p=None), dict(n=5, g=None), dict(n=5, m=None), dict(n=5, v=None),
     dict(n=5, p=72), dict(n=5, g=66), dict(n=5, master=68), dict(n=5, m=65), dict(n=5, v=72), dict(n=(1 << 40) + 1),
