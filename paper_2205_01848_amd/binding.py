@@ -978,10 +978,12 @@ class AdamWList:
         self.tensors = list(tensors)
         every = [a for t in self.tensors for a in t.arrays()]
         self.device = _device_of(*every)
-        written = sorted((a.data_ptr(), a.data_ptr() + _nbytes(a)) for t in self.tensors for a in t.arrays()
-                         if a is not t.g and a.numel())
-        if any(a[1] > b[0] for a, b in zip(written, written[1:])):
-            raise MoEError("weights or moments overlap: a tensor is listed twice")
+        ends = {True: 0, False: 0}   # of the arrays so far, written ones and gradients
+        for at, end, written in sorted((a.data_ptr(), a.data_ptr() + _nbytes(a), a is not t.g)
+                                       for t in self.tensors for a in t.arrays() if a.numel()):
+            if at < ends[True] or (written and at < ends[False]):
+                raise MoEError("weights, moments or gradients overlap: a tensor is listed twice")
+            ends[written] = max(ends[written], end)
         self.args = (AdamWTensorArgs * len(self.tensors))(*[
             AdamWTensorArgs(*[_ptr(a) for a in (t.p, t.g, t.master, t.m, t.v, t.m_exp, t.v_exp)], t.p.numel(),
                             t.weight_decay, _dt(t.p), _dt(t.g)) for t in self.tensors])

@@ -71,6 +71,13 @@ def test_adamw(calls):
         AdamW([], bits=16)
     with pytest.raises(B.MoEError, match="listed twice"):
         AdamW([(big, torch.zeros(100, 50)), (big, torch.zeros(100, 50))])
+    memory = torch.zeros(64)
+    AdamW([(torch.zeros(16), memory[:16]), (torch.zeros(16), memory[:16])])      # one gradient of two weights
+    for p, g in ((memory[:16], memory[:16]), (memory[8:24], memory[:16]), (memory[:16], memory[8:24])):
+        with pytest.raises(B.MoEError, match="overlap"):
+            AdamW([(p, g)])
+    with pytest.raises(B.MoEError, match="overlap"):        # another's weight inside a longer gradient
+        AdamW([(torch.zeros(48), memory[:48]), (memory[20:28], torch.zeros(8))])
     with pytest.raises(B.MoEError, match="g holds"):
         AdamW([(big, torch.zeros(99, 50))])
 
