@@ -19,6 +19,7 @@
 // 6.0 TB/s, its backward 111 us, 4.8 TB/s, and dw's partial sums 4.8 us; one row 6 us.
 
 #include <algorithm>
+#include <utility>
 
 #include "quant.hpp"
 
@@ -339,6 +340,11 @@ template <typename T> moe_status launch_bwd(hipStream_t s, const NormBwdArgs& a)
 bool norm_shape_ok(int64_t rows, int d) { return rows >= 0 && width_ok(d) && d <= kMaxNorm; }
 bool norm_pitch_ok(int64_t ld, int d) { return ld >= d && ld % 8 == 0; }
 
+// Rows written over an input's rows: the same ones, or a workgroup would overwrite another's.
+bool in_place_ok(int64_t rows, const void* out, int64_t ldout, const void* in, int64_t ldin) {
+  return out != in || ldout == ldin || rows <= 1;
+}
+
 }  // namespace
 }  // namespace moe
 
@@ -354,6 +360,8 @@ extern "C" moe_status moe_rms_norm_fwd(void* stream, moe_dtype dt, int64_t rows,
     return MOE_EINVAL;
   if (rows == 0) return MOE_OK;
   if ((!y && !q) || !q != !scale || (sum && !add) || (y && y == sum)) return MOE_EINVAL;
+  for (const auto& [out, ld] : {std::pair<const void*, int64_t>{sum, ldsum}, {y, ldy}})
+    if (out && (!in_place_ok(rows, out, ld, x, ldx) || !in_place_ok(rows, out, ld, add, ldadd))) return MOE_EINVAL;
   if (!x || !weight || !aligned16(x) || !aligned16(add) || !aligned16(weight) || !aligned16(sum) ||
       !aligned16(y) || !aligned16(q))
     return MOE_EINVAL;
@@ -378,6 +386,9 @@ extern "C" moe_status moe_rms_norm_bwd(void* stream, moe_dtype dt, int64_t rows,
       !norm_pitch_ok(lddx, d))
     return MOE_EINVAL;
   if (rows > 0 && (!s || !weight || !rstd || !dy || !dx)) return MOE_EINVAL;
+  if (!in_place_ok(rows, dx, lddx, s, lds) || !in_place_ok(rows, dx, lddx, dy, lddy) ||
+      !in_place_ok(rows, dx, lddx, dsum, lddsum))
+    return MOE_EINVAL;
   if (!aligned16(s) || !aligned16(weight) || !aligned16(dy) || !aligned16(dsum) || !aligned16(dx))
     return MOE_EINVAL;
   if (dw && (!workspace || !aligned16(workspace) ||

@@ -231,6 +231,7 @@ extern "C" moe_status moe_vocab_loss(void* stream, moe_dtype dt, int T, int d, i
   if (grad && (!dw || (T > 0 && !dx))) return MOE_EINVAL;   // both
   if (!w || !aligned16(w) || !aligned16(x) || !aligned16(dx) || !aligned16(dw)) return MOE_EINVAL;
   if (T > 0 && (!x || !targets || !loss || !status)) return MOE_EINVAL;
+  if (T > 1 && dx == x && lddx != ldx) return MOE_EINVAL;   // rows of one piece over those of the next
   if (!workspace || workspace_bytes < static_cast<size_t>(g.total) || !aligned16(workspace)) return MOE_EWORKSPACE;
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (T == 0) return grad ? launch_zero(s, dw, static_cast<size_t>(V) * d * esize(dw_dt)) : MOE_OK;

@@ -72,7 +72,10 @@ def _norm(lib, dt=1, rows=5, d=24, x=P, ldx=24, add=P, ldadd=24, w=P, eps=1e-5, 
     dict(x=None), dict(w=None), dict(eps=0.0), dict(eps=-1.0), dict(eps=math.inf), dict(eps=math.nan),
     dict(ldx=16), dict(ldx=28), dict(ldadd=20), dict(ldsum=16), dict(ldy=23), dict(y=None), dict(q=P), dict(scale=P),
     dict(add=None), dict(sum=P), dict(x=ctypes.c_void_p(4100)), dict(y=ctypes.c_void_p(4104)),
-    dict(q=ctypes.c_void_p(4097), scale=P), dict(w=ctypes.c_void_p(4098))], ids=str)
+    dict(q=ctypes.c_void_p(4097), scale=P), dict(w=ctypes.c_void_p(4098)),
+    # over an input whose rows lie otherwise
+    dict(add=ctypes.c_void_p(12288), ldy=32), dict(x=ctypes.c_void_p(12288), ldadd=32),
+    dict(y=ctypes.c_void_p(12288), sum=P, ldsum=32), dict(add=ctypes.c_void_p(8192), ldsum=32, y=None, q=P, scale=P)], ids=str)
 def test_norm_refuses(kw):
     assert _norm(B.lib(), **kw) == EINVAL
 
@@ -87,6 +90,9 @@ def _norm_bwd(lib, dt=1, rows=5, d=24, s=P, lds=24, w=P, rstd=P, dy=P, lddy=24, 
     (dict(rstd=None), EINVAL), (dict(dy=None), EINVAL), (dict(dx=None), EINVAL), (dict(lds=23), EINVAL),
     (dict(lddy=16), EINVAL), (dict(lddsum=25), EINVAL), (dict(lddx=16), EINVAL), (dict(dw_dt=2), EINVAL),
     (dict(dt=0, dw_dt=1), EINVAL), (dict(dx=ctypes.c_void_p(4104)), EINVAL), (dict(ws=None), EWORKSPACE),
+    (dict(lddx=32), EINVAL), (dict(dy=ctypes.c_void_p(8192), dsum=None, lds=32), EINVAL),   # dx over rows that lie otherwise
+    (dict(s=ctypes.c_void_p(8192), dsum=None, lddy=32), EINVAL),
+    (dict(s=ctypes.c_void_p(8192), dy=ctypes.c_void_p(8192), lddsum=32), EINVAL),
     (dict(nws=2 * 24 * 4 - 1), EWORKSPACE), (dict(ws=ctypes.c_void_p(4100)), EWORKSPACE)], ids=str)
 def test_norm_bwd_refuses(kw, st):
     assert _norm_bwd(B.lib(), **kw) == st
@@ -174,6 +180,7 @@ def _loss(lib, dt=1, T=5, d=24, V=7, x=P, ldx=24, w=P, targets=P, scale=1.0, wei
     (dict(dx=None), EINVAL), (dict(dw=None), EINVAL), (dict(ldx=16), EINVAL), (dict(ldx=28), EINVAL), (dict(lddx=23), EINVAL),
     (dict(scale=math.nan), EINVAL), (dict(scale=math.inf), EINVAL), (dict(dw_dt=2), EINVAL), (dict(dt=0, dw_dt=1), EINVAL),
     (dict(x=ctypes.c_void_p(4100)), EINVAL), (dict(w=ctypes.c_void_p(4104)), EINVAL), (dict(dx=ctypes.c_void_p(4104)), EINVAL),
+    (dict(lddx=32), EINVAL), (dict(ldx=32), EINVAL),   # dx over rows of x that lie otherwise
     (dict(ws=None), EWORKSPACE), (dict(nws=64), EWORKSPACE), (dict(ws=ctypes.c_void_p(4104)), EWORKSPACE)], ids=str)
 def test_loss_refuses(kw, st):
     assert _loss(B.lib(), **kw) == st
