@@ -800,7 +800,7 @@ size_t moe_adamw_blocks(int64_t n);
  * its block's largest becomes 0).  The random bits depend on seed, the tensor's
  * place in the list and the element alone: give every step another seed.
  * An m that is not a finite float32 is kept as NaN; a v that is not, as its block's
- * largest value.
+ * largest value, and a finite m beside it as 0: that element's moments begin anew.
  *   tensors    [host] [count] (read before the call returns)
  *   lr, eps    lr >= 0, eps >= 2^-126, finite; 0 <= beta < 1; step >= 1
  *   grad_scale NULL, or device [1]: every gradient is multiplied by it (a clipping

@@ -11,7 +11,7 @@ from .blocks import quantize_rows
 from .moe_oracle import round_to
 
 __all__ = ["rms_norm_fwd", "rms_norm_bwd", "rms_norm_rows_i8", "vocab_loss", "adamw", "adamw_random", "adamw_encode",
-           "adamw_decode"]
+           "adamw_encode_states", "adamw_decode"]
 
 
 # ---- norm ------------------------------------------------------------------------
@@ -95,9 +95,10 @@ def _blocks(a, fill):
     return out.reshape(-1, 128)
 
 
-def adamw_encode(x, rnd, mant):
-    """(code, exponent per block) of values in float64: m (mant 3, with sign) or v (mant 4).  Counted
-    in steps of 2^-mant of the value's octave, the random 16 bits decide on the step begun."""
+def _steps(x, rnd, mant):
+    """(some, octave, steps, beyond): whether a value is a number other than 0, its float32 exponent and
+    its 2^-mant of that octave, the random 16 bits deciding on the one begun, and whether that is
+    no finite float32."""
     x = np.asarray(x, np.float64)
     with np.errstate(invalid="ignore", divide="ignore"):
         size = np.abs(x)
@@ -107,7 +108,13 @@ def adamw_encode(x, rnd, mant):
         octave = octave.astype(np.int64) - 1 + 127                # the float32 exponent
     carry = steps == 2 ** (mant + 1)
     octave, steps = octave + carry, np.where(carry, 2 ** mant, steps)
-    beyond = ~np.isfinite(size) | (some & (octave > 254))
+    return some, octave, steps, ~np.isfinite(size) | (some & (octave > 254))
+
+
+def adamw_encode(x, rnd, mant):
+    """(code, exponent per block) of values in float64: m (mant 3, with sign) or v (mant 4)."""
+    x = np.asarray(x, np.float64)
+    some, octave, steps, beyond = _steps(x, rnd, mant)
     e = np.maximum(_blocks(np.where(some & ~beyond, octave, 16), 16).max(axis=1), 16)
     top = np.repeat(e, 128)[:len(x)]
     code = (octave - (top - 15)) * 2 ** mant + steps - 2 ** mant
@@ -117,6 +124,13 @@ def adamw_encode(x, rnd, mant):
     else:
         code = np.where(beyond, 255, np.where((code == 0) & some, 1, code))
     return code.astype(np.uint8), e.astype(np.uint8)
+
+
+def adamw_encode_states(m, v, rnd_m, rnd_v):
+    """(code of m, its exponents, code of v, its exponents).  An m beside a v beyond float32, which
+    no code stands for, is kept as 0."""
+    lost = _steps(v, rnd_v, 4)[3] & ~_steps(m, rnd_m, 3)[3]
+    return adamw_encode(np.where(lost, 0.0, m), rnd_m, 3) + adamw_encode(v, rnd_v, 4)
 
 
 def adamw_decode(code, e, mant):

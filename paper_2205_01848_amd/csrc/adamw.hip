@@ -15,7 +15,10 @@
 // to nearest, a step of b2 = 0.999 could not move v, whose codes lie 1/32 to 1/16 apart: its
 // change of at most a thousandth a step is lost unless g^2 is more than 30 v, so v
 // would climb with outliers and never come down.  Rounded at random the codes are right on
-// average.  A v above 0 never becomes 0, where the next step would divide m by eps.
+// average.  A v above 0 never becomes 0, where the next step would divide m by eps.  A v
+// beyond float32 (a gradient of 1e21) is kept as its block's largest, and its m as 0: beside
+// a v that has come down to its neighbours' size the next step would divide an m of 1e20 by it.
+// Counted into the block's exponent instead it would hold up every neighbour's v.
 // The random bits are a function of (seed, tensor, element), so a step can be repeated.
 //
 // So that a value's code does not depend on how its sums were rounded, the moments of
@@ -237,6 +240,7 @@ __device__ __forceinline__ void step_codes(const AdamArgs& a, const AdamTensor& 
     vmost = 16 << 4;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
+      if (vt[e] >= kBeyondV && mt[e] < kBeyondM) mt[e] = 0;
       mmost = max(mmost, mt[e] < kBeyondM ? mt[e] : 0);
       vmost = max(vmost, vt[e] < kBeyondV ? vt[e] : 0);
     }
