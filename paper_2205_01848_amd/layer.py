@@ -558,9 +558,15 @@ class RMSNorm:
         return y
 
     def quantized(self, n: Optional[int] = None):
-        """(q, scale) of the last forward's first n rows (all T)."""
+        """(q, scale) of the last forward's rows, or of the first n of them."""
         if self.q is None:
             raise ValueError("the norm was made without rows in 8 bits (quantized)")
+        if n is None and self.s is None:
+            raise ValueError("the rows in 8 bits follow a forward")
+        rows = self.T if self.s is None else self.s.shape[0]
+        n = rows if n is None else n
+        if not 0 <= n <= rows:
+            raise ValueError(f"{n} rows in 8 bits, the last forward left {rows}")
         return self.q[:n], self.scale[:n]
 
     def backward(self, dy, weight, dsum=None):
