@@ -967,7 +967,9 @@ class AdamWTensor:
         self.m_exp, self.v_exp, self.weight_decay = m_exp, v_exp, float(weight_decay)
 
     def arrays(self):
-        return [t for t in (self.p, self.g, self.m, self.v, self.master, self.m_exp, self.v_exp) if t is not None]
+        """(array, whether the step writes it) of every array: all but the gradient's."""
+        every = (self.p, self.m, self.v, self.master, self.m_exp, self.v_exp)
+        return [(self.g, False)] + [(a, True) for a in every if a is not None]
 
 
 class AdamWList:
@@ -976,11 +978,12 @@ class AdamWList:
 
     def __init__(self, tensors):
         self.tensors = list(tensors)
-        every = [a for t in self.tensors for a in t.arrays()]
+        every = [a for t in self.tensors for a, _ in t.arrays()]
         self.device = _device_of(*every)
         ends = {True: 0, False: 0}   # of the arrays so far, written ones and gradients
-        for at, end, written in sorted((a.data_ptr(), a.data_ptr() + _nbytes(a), a is not t.g)
-                                       for t in self.tensors for a in t.arrays() if a.numel()):
+        spans = [(a.data_ptr(), a.data_ptr() + _nbytes(a), written)
+                 for t in self.tensors for a, written in t.arrays() if a.numel()]
+        for at, end, written in sorted(spans):
             if at < ends[True] or (written and at < ends[False]):
                 raise MoEError("weights, moments or gradients overlap: a tensor is listed twice")
             ends[written] = max(ends[written], end)
