@@ -194,13 +194,16 @@ __device__ __forceinline__ float root(float v) {
   return tiny ? s * 0x1p-32f : s;
 }
 
+// The decay joins the update, not a factor 1 - lr wd, which has steps of 6e-8 (lr wd = 1e-7 would
+// be 1.2e-7, 2e-8 nothing, for every weight and step alike).  Infinite weights stay what they are.
 __device__ __forceinline__ void update(float (&p)[8], const float (&m)[8], const float (&v)[8],
-                                       const AdamStep& st, float keep, float eps) {
+                                       const AdamStep& st, float decay, float eps) {
   const float rate = st.lr * st.c1;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     const float den = __builtin_fmaf(root(v[e]), st.c2, eps);
-    p[e] = __builtin_fmaf(p[e], keep, -(rate * m[e]) * __builtin_amdgcn_rcpf(den));
+    const float x = rate * m[e] * __builtin_amdgcn_rcpf(den);
+    p[e] -= __builtin_fmaf(decay, __builtin_amdgcn_fmed3f(p[e], -0x1.fffffep127f, 0x1.fffffep127f), x);
   }
 }
 
@@ -270,7 +273,7 @@ __device__ __forceinline__ void step_codes(const AdamArgs& a, const AdamTensor& 
 
 template <bool FULL>
 __device__ __forceinline__ void step_tile(const AdamArgs& a, const AdamTensor& t, const AdamStep& st, int64_t i,
-                                          float keep) {
+                                          float decay) {
   const int64_t left = t.n - i;
   float g[8], p[8], m[8], v[8];
   load8<FULL>(t.g, t.g16, i, left, g);
@@ -292,7 +295,7 @@ __device__ __forceinline__ void step_tile(const AdamArgs& a, const AdamTensor& t
     store8<FULL>(t.m, false, i, left, m);
     store8<FULL>(t.v, false, i, left, v);
   }
-  update(p, m, v, st, keep, a.eps);
+  update(p, m, v, st, decay, a.eps);
   if (t.master) store8<FULL>(t.master, false, i, left, p);
   store8<FULL>(t.p, t.p16, i, left, p);
 }
@@ -308,10 +311,10 @@ __global__ __launch_bounds__(kAdamThreads) void adamw_kernel(const AdamArgs a) {
   const int ti = find_tensor(a, blockIdx.x);
   const AdamTensor& t = a.t[ti];
   int64_t i0 = static_cast<int64_t>(static_cast<int>(blockIdx.x) - t.first) * a.tiles * kTile;
-  const float keep = 1.f - st.lr * t.decay;
+  const float decay = st.lr * t.decay;
   for (int k = 0; k < a.tiles && i0 < t.n; ++k, i0 += kTile) {
-    if (i0 + kTile <= t.n) step_tile<true>(a, t, st, i0 + threadIdx.x * 8, keep);
-    else step_tile<false>(a, t, st, i0 + threadIdx.x * 8, keep);
+    if (i0 + kTile <= t.n) step_tile<true>(a, t, st, i0 + threadIdx.x * 8, decay);
+    else step_tile<false>(a, t, st, i0 + threadIdx.x * 8, decay);
   }
 }
 
