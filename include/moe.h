@@ -446,6 +446,8 @@ size_t moe_vocab_loss_workspace_bytes(moe_dtype dt, int T, int d, int V,
  *   of scale sum_t weights_t loss_t:
  *   dl_tv = weights_t (exp(l_tv - lse_t) - [v = target_t]) (bf16: rounded),
  *   dx = scale dl w, dw = scale dl^T x, each rounded once
+ * A loss is off by a few 2^-24 beside its logits' errors (0 where the target has
+ * more than 1 - 2^-24 of the probability).
  * The logits are never kept: without gradients none is written, with them the
  * workspace holds those of one piece of rows (at most 2 GiB, 256 rows at least),
  * as 16-bit (bf16) or float32 exponentials.

@@ -5,8 +5,10 @@
 //
 // The logits' product leaves, for every row and block of 16 to 128 columns, their maximum m
 // and sum of exp(l - m), and the target's logit; a pass over those forms lse and
-// loss = log sum + (maximum - l_target), which stays exact where the target has nearly all
-// of the probability.  Without gradients no logit is ever written.
+// loss = log sum + (maximum - l_target), in which the size of the logits cancels: a small loss is
+// off by a few 2^-24 (beside the logits' own errors), not by lse 2^-24.  The sum holds the maximum's
+// own 1, so a target with more than 1 - 2^-24 of the probability has loss 0, and 0 in dl, while the
+// other words keep theirs.  Without gradients no logit is ever written.
 //
 // With gradients the product also writes exp(l - m) of its piece, in 16 bits (11 of
 // mantissa), and one pass turns them into dl in place: weight exp(m - lse) times that, and
@@ -16,7 +18,9 @@
 // two passes over 2.1 GB of exponentials take 1 ms).  Kept as bf16 the exponentials would
 // round twice, and dx be off by sqrt(3) roundings for sqrt(2).  scale joins the fp32 sums at
 // the end: in dl it would round every token's largest entry, near -scale, the same way, by up
-// to 2^-8 (1 / 509 by 0.0019, where dx is off by 0.0018 of itself in all).
+// to 2^-8 (1 / 509 by 0.0019).  Without weights the targets' entries, near -1, are nearly exact, and dx and
+// dw are off by 0.0017 to 0.0019 of themselves, 0.0016 of it their own rounding; tokens' weights stay
+// in dl (dw sums over the tokens), whose largest entries then round too: 0.0024, sqrt(2) roundings.
 //
 // dW's product reads a copy of x that the pass makes, with zeros in the rows of ignored
 // tokens, so that nothing they contain reaches it.
