@@ -32,10 +32,10 @@
 // Bound by memory: bf16 weights, fp32 gradients and 8-bit states take 12 bytes a value,
 // 32-bit states and originals beside them 32.  A thread takes 8 neighbouring values, so a
 // block of 128 is a row of 16 lanes, whose maximum four DPP steps find.  277 million
-// values of the first kind: 742 us, 4.5 TB/s (902 with a division by the compiler's exact sequence
-// and guards on every access, as its vector units bound it); unpacking them 507 us,
+// values of the first kind: 740 us, 4.5 TB/s (902 with a division by the compiler's exact sequence
+// and guards on every access, as its vector units bound it); unpacking them 502 us,
 // 5.5 TB/s (703 with 32 bytes a lane and array, half a line a store); 33.6 million of the second:
-// 195 us, 5.5 TB/s.
+// 196 us, 5.5 TB/s.
 
 #include <algorithm>
 #include <cmath>

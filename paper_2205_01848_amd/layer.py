@@ -614,7 +614,8 @@ class AdamW:
     keeps.  bits: 32, or 8 for the states of tensors of at least min_8bit values (smaller ones gain
     nothing by it).  master: bf16 weights get float32 originals, of which they are the roundings.
     Vectors take no weight decay.  captured: lr, the step's corrections and its seed are read from a device
-    tensor that prepare() fills, so that the step can be part of a graph."""
+    tensor that prepare() fills, so that the step can be part of a graph.  What a checkpoint holds, and gets
+    back by copy_: m, v, m_exp, v_exp and master of list.tensors (None where a tensor has none), and step_count."""
 
     def __init__(self, pairs, lr: float = 1e-3, betas=(0.9, 0.95), eps: float = 1e-8, weight_decay: float = 0.1,
                  bits: int = 32, master: bool = True, min_8bit: int = 4096, captured: bool = False):
